@@ -68,7 +68,7 @@ typedef enum {
     EQAT_ERR_ALIGN = 6,     /* pointer not 16-byte (workspace: 256-byte) aligned */
     EQAT_ERR_WORKSPACE = 7, /* workspace missing or too small                    */
     EQAT_ERR_DEVICE = 8,    /* the HIP runtime refused a launch                  */
-    EQAT_ERR_HYPER = 9      /* optimizer constants out of range                  */
+    EQAT_ERR_HYPER = 9      /* optimizer or attention constants out of range     */
 } eqat_status;
 
 typedef enum { EQAT_F32 = 0, EQAT_BF16 = 1 } eqat_dtype;
@@ -393,6 +393,75 @@ eqat_status eqat_fwd_route(const eqat_desc *d, int source, int32_t *route);
  * kernel for few output tiles, 0: another kernel;  asked for with dW, ds or dz (block_ap: eqat_fq_linear_bwd, else the E2E-QP calls): -1 a launch of
  * its own, as alone; else a launch that it shares with dW: 0, 1 256 x 256 tiles (1: contraction of no whole K-tile pairs), else such a token tile }. */
 eqat_status eqat_dx_route(const eqat_desc *d, int block_ap, int32_t *route);
+
+/*
+ * The key-value cache of a served model, in 4 bits.  (Not part of the paper's method: it is what a decoder reads beside the packed weights at every token.)
+ *
+ *   In groups of `group` neighbouring elements of a key or a value (of one token and head), sixteen steps from the least element to the greatest:
+ *     m = f16(min x),  s = f16(max((max x - min x) / 15, 2^-24)),  c = clamp(round((x - m) / s), 0, 15),  x^ = m + s c
+ *   in binary32 (the quotients correctly rounded, round() half to even), f16 the nearest binary16 number.  A group with an element that is not finite, or whose m or s
+ *   is not (|x| beyond 65504), stands as NaN; one that spans less than about 2^-16 is held in steps of 2^-24.
+ *
+ *   Pool       eqat_kv_pool_bytes(desc) bytes of device memory, 256-byte aligned, owned by the caller; of any size (offsets are 64 bits), of any contents at first.
+ *              It is a number of pages of `page_tokens` tokens; how a page is laid out is the library's own.  Bytes per token and head: head_dim + 8 head_dim / group.
+ *   Sequences  An eqat_kv_batch says, in device arrays, where the sequences of a call stand: sequence b holds lens[b] tokens, its position p on page
+ *              table[b * table_stride + p / page_tokens] (at p % page_tokens), and its newest starts[b+1] - starts[b] tokens are the rows starts[b] .. starts[b+1] - 1 of
+ *              the call's tensors: lens counts them in.  Either number may be 0.  The host gives bounds only (tokens = starts[sequences], max_new, max_len), so that a
+ *              captured graph serves lengths and pages that change between its replays.  What lies beyond the bounds, or on a page outside the pool, is taken as not
+ *              there: not written, read as zeros, not attended to; nothing outside the tensors and the pool is touched whatever stands in the arrays.
+ *   Tensors    [tokens, heads, head_dim] with any strides (in elements, of a token and of a head; elements of a head are contiguous), such as slices of the rows of
+ *              a stacked q|k|v projection.  Pointers and strides in bytes are multiples of 16.
+ *   Types      desc.act_dtype (bf16 or fp32) for every tensor; lse is fp32.
+ */
+typedef struct eqat_kv_desc {
+    int64_t pages;          /* of the pool, below 2^31                                          */
+    int32_t heads;          /* of keys and values                                               */
+    int32_t head_dim;       /* 64, 128 or 256                                                   */
+    int32_t group;          /* 32, 64, 128 or 256, at most head_dim, or -1: head_dim            */
+    int32_t page_tokens;    /* a multiple of 32                                                 */
+    int32_t act_dtype;      /* eqat_dtype                                                       */
+} eqat_kv_desc;
+
+typedef struct eqat_kv_batch {
+    const int32_t *table;   /* [sequences, table_stride] pages, device                          */
+    const int32_t *lens;    /* [sequences] tokens held, the newest included, device             */
+    const int32_t *starts;  /* [sequences + 1] first rows, not decreasing, starts[0] = 0, device */
+    int64_t tokens;         /* rows of the call's tensors                                       */
+    int32_t sequences, table_stride;
+    int32_t max_new;        /* no sequence has more newest tokens                               */
+    int32_t max_len;        /* none holds more tokens                                           */
+} eqat_kv_batch;
+
+typedef struct eqat_kv_attn {
+    int32_t q_heads;        /* a multiple of desc.heads: query head h reads head h / (q_heads / heads) */
+    int32_t causal;         /* 0: every query sees all of its sequence; else positions up to its own   */
+    int32_t window;         /* > 0: only the last `window` of the positions up to its own; 0: no limit */
+    float scale;            /* of the scores; 0: 1 / sqrt(head_dim)                                    */
+} eqat_kv_attn;
+
+size_t eqat_kv_pool_bytes(const eqat_kv_desc *d);                       /* 0 for a bad descriptor */
+
+/* The newest tokens of every sequence into the cache.  Strides of K and V in elements: { token, head }. */
+eqat_status eqat_kv_write(const eqat_kv_desc *d, const eqat_kv_batch *b, const void *K, const int64_t *k_strides, const void *V,
+                          const int64_t *v_strides, void *pool, void *stream);
+
+/* The newest tokens of every sequence (all of them where starts[b+1] - starts[b] = lens[b]) as values.  K or V may be NULL (skipped). */
+eqat_status eqat_kv_read(const eqat_kv_desc *d, const eqat_kv_batch *b, void *K, const int64_t *k_strides, void *V, const int64_t *v_strides,
+                         const void *pool, void *stream);
+
+/*
+ * Softmax attention of the newest tokens' queries over what their sequences hold (write first, then attend):
+ *   out[t, h] = sum over j of softmax_j(scale q[t, h] . k^_j) v^_j,   lse[t, h] = ln(sum over j of exp(scale q . k^_j)),
+ * j over the positions that the query, at position lens[b] - (new tokens) + (its place among them), sees.  A query that sees none gives zeros and lse -inf.
+ * NaN or infinities at positions that a query does not see do not reach it.  Scores, softmax and sums are binary32.
+ *   Q, out: [tokens, q_heads, head_dim];  lse: [tokens, q_heads] contiguous, or NULL.
+ *   ws: eqat_kv_workspace_bytes bytes (independent of the batch but for max_new and max_len), 256-byte aligned, ZEROED ONCE by the caller before its first use.  Every call
+ *   leaves the counters in it at zero; calls that share a workspace must not overlap in time.
+ * EQAT_ERR_HYPER for a scale that is negative, infinite or NaN, or a negative window.
+ */
+size_t eqat_kv_workspace_bytes(const eqat_kv_desc *d, const eqat_kv_batch *b, int q_heads);
+eqat_status eqat_kv_attention(const eqat_kv_desc *d, const eqat_kv_batch *b, const eqat_kv_attn *a, const void *Q, const int64_t *q_strides,
+                              void *out, const int64_t *out_strides, float *lse, const void *pool, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Optional per-kernel timing (measurement aid, not part of the paper's method).

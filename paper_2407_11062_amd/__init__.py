@@ -33,6 +33,7 @@ EXPORTS = ["eqat_status_string", "eqat_validate_desc", "eqat_packed_w_bytes", "e
            "eqat_qlinear_fwd_prepared", "eqat_qlinear_bwd_prepared", "eqat_qlinear_fwd_prepared_keep",
            "eqat_qlinear_bwd_prepared_kept", "eqat_unpack_state", "eqat_plan_item", "eqat_shared_item", "eqat_plan_scratch", "eqat_fwd_route", "eqat_dx_route",
            "eqat_recon_loss_workspace_bytes", "eqat_recon_loss", "eqat_recon_loss_static", "eqat_block_ap_update",
+           "eqat_kv_pool_bytes", "eqat_kv_write", "eqat_kv_read", "eqat_kv_workspace_bytes", "eqat_kv_attention",
            "eqat_profile_kernels", "eqat_profile_kernel_name",
            "eqat_profile_start", "eqat_profile_stop"]
 
@@ -47,6 +48,20 @@ class AdamW(ctypes.Structure):
     _fields_ = [("lr_w", ctypes.c_float), ("lr_q", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay_w", ctypes.c_float), ("weight_decay_q", ctypes.c_float),
                 ("step", ctypes.c_int32)]
+
+
+class KvDesc(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("act_dtype", ctypes.c_int32)]
+
+
+class KvBatchDesc(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("tokens", ctypes.c_int64),
+                ("sequences", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("max_new", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class KvAttn(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class EqatError(RuntimeError):
@@ -107,6 +122,12 @@ def lib():
         L.eqat_recon_loss.argtypes = [ctypes.c_int64, ctypes.c_int32, vp, vp, vp, vp, vp, sz, vp]
         L.eqat_recon_loss_static.argtypes = [ctypes.c_int64, ctypes.c_int32, vp, vp, vp, vp, vp]
         L.eqat_block_ap_update.argtypes = [dp, ctypes.POINTER(AdamW)] + [vp] * 13
+        kd, kb = ctypes.POINTER(KvDesc), ctypes.POINTER(KvBatchDesc)
+        L.eqat_kv_pool_bytes.restype, L.eqat_kv_pool_bytes.argtypes = sz, [kd]
+        L.eqat_kv_write.argtypes = [kd, kb, vp, vp, vp, vp, vp, vp]
+        L.eqat_kv_read.argtypes = L.eqat_kv_write.argtypes
+        L.eqat_kv_workspace_bytes.restype, L.eqat_kv_workspace_bytes.argtypes = sz, [kd, kb, ctypes.c_int]
+        L.eqat_kv_attention.argtypes = [kd, kb, ctypes.POINTER(KvAttn), vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.eqat_profile_kernel_name.restype = ctypes.c_char_p
         L.eqat_profile_kernel_name.argtypes = [ctypes.c_int]
         L.eqat_profile_stop.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64), ctypes.c_int]
@@ -417,6 +438,87 @@ def eqat_block_ap_update(hyper: AdamW, bits, group, W=None, dW=None, mW=None, vW
     _check("eqat_block_ap_update", lib().eqat_block_ap_update(
         ctypes.byref(d), ctypes.byref(hyper), _p(W), _p(s), _p(z), _p(dW), _p(ds), _p(dz), _p(mW), _p(vW), _p(ms), _p(vs),
         _p(mz), _p(vz), _stream()))
+
+
+class KvCache:
+    """A pool of pages for keys and values in 4 bits, and its descriptor.  `pool`: the caller's own uint8 device tensor, 256-byte aligned."""
+
+    def __init__(self, heads, head_dim, group, page_tokens, pages, dtype=torch.bfloat16, device="cuda", pool=None):
+        self.heads, self.head_dim, self.dtype = int(heads), int(head_dim), dtype
+        self.desc = KvDesc(int(pages), self.heads, self.head_dim, int(group), int(page_tokens), F32 if dtype == torch.float32 else BF16)
+        self.ref = ctypes.byref(self.desc)
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported dtype {dtype}")
+        n = lib().eqat_kv_pool_bytes(self.ref)
+        if n == 0:
+            raise ValueError(f"eqat_kv_pool_bytes: no cache of {heads} heads of {head_dim}, groups of {group}, {pages} pages of {page_tokens} tokens")
+        self.pool = torch.empty(n, dtype=torch.uint8, device=device) if pool is None else pool
+        if self.pool.numel() < n:
+            raise ValueError(f"the pool needs {n} bytes")
+
+
+class KvBatch:
+    """Where the sequences of a call stand (int32 device tensors, kept and read on the device at every call): the pages of each, how many tokens it holds with the
+    newest, and where the newest tokens' rows start.  tokens, max_new, max_len: the rows in all, and bounds on both numbers of any sequence.  Build once, call often."""
+
+    def __init__(self, table, lens, starts, tokens, max_new, max_len):
+        B = lens.numel()
+        for t in (table, lens, starts):
+            if t.dtype != torch.int32:
+                raise TypeError("table, lens and starts are int32")
+        if table.dim() != 2 or table.shape[0] != B or starts.numel() != B + 1:
+            raise ValueError("table is [sequences, pages], lens [sequences], starts [sequences + 1]")
+        self.keep = (table, lens, starts)            # they must outlive the pointers
+        self.tokens = int(tokens)
+        self.desc = KvBatchDesc(_p(table), _p(lens), _p(starts), self.tokens, B, table.shape[1], int(max_new), int(max_len))
+        self.ref = ctypes.byref(self.desc)
+
+
+def _kv_rows(cache, batch, t, heads):
+    """(pointer, {token, head} strides) of a [tokens, heads, head_dim] tensor whose heads are contiguous"""
+    if t is None:
+        return None, None
+    if t.dtype != cache.dtype or tuple(t.shape) != (batch.tokens, heads, cache.head_dim):
+        raise ValueError(f"expected {cache.dtype} [{batch.tokens}, {heads}, {cache.head_dim}], got {t.dtype} {list(t.shape)}")
+    ts, hs, es = t.stride()
+    if not t.is_cuda or es != 1:
+        raise ValueError("the elements of a head must be contiguous, on the device")
+    return t.data_ptr(), (ctypes.c_int64 * 2)(ts, hs)
+
+
+def eqat_kv_write(cache: KvCache, batch: KvBatch, k, v):
+    """The newest tokens' keys and values [tokens, heads, head_dim] (any token and head strides) into the cache."""
+    (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
+    _check("eqat_kv_write", lib().eqat_kv_write(cache.ref, batch.ref, kp, ks, vp, vs, cache.pool.data_ptr(), _stream()))
+
+
+def eqat_kv_read(cache: KvCache, batch: KvBatch, k=None, v=None, want=("k", "v")):
+    """(k, v): the newest tokens' keys and values as they stand in the cache.  Given tensors are filled; `want` says which to make where neither is given."""
+    if k is None and v is None:
+        k, v = (torch.empty((batch.tokens, cache.heads, cache.head_dim), dtype=cache.dtype, device=cache.pool.device) if name in want else None for name in ("k", "v"))
+    (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
+    _check("eqat_kv_read", lib().eqat_kv_read(cache.ref, batch.ref, kp, ks, vp, vs, cache.pool.data_ptr(), _stream()))
+    return k, v
+
+
+def kv_workspace(cache: KvCache, batch: KvBatch, q_heads) -> torch.Tensor:
+    """The workspace of eqat_kv_attention, zeroed as its first use wants it.  It serves every later call with bounds no larger than this batch's."""
+    n = lib().eqat_kv_workspace_bytes(cache.ref, batch.ref, int(q_heads))
+    return torch.zeros(max(n, 256), dtype=torch.uint8, device=cache.pool.device)
+
+
+def eqat_kv_attention(cache: KvCache, batch: KvBatch, q, scale=0.0, causal=True, window=0, out=None, lse=None, ws=None):
+    """Attention of the newest tokens' queries [tokens, q_heads, head_dim] over what their sequences hold; lse: fp32 [tokens, q_heads] to fill, or None."""
+    q_heads = q.shape[1]
+    out = torch.empty((batch.tokens, q_heads, cache.head_dim), dtype=q.dtype, device=q.device) if out is None else out
+    (qp, qs), (op, os_) = _kv_rows(cache, batch, q, q_heads), _kv_rows(cache, batch, out, q_heads)
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (batch.tokens, q_heads)):
+        raise ValueError("lse is fp32 [tokens, q_heads]")
+    ws = kv_workspace(cache, batch, q_heads) if ws is None else ws
+    a = KvAttn(q_heads, 1 if causal else 0, int(window), float(scale))
+    _check("eqat_kv_attention", lib().eqat_kv_attention(cache.ref, batch.ref, ctypes.byref(a), qp, qs, op, os_, _p(lse), cache.pool.data_ptr(),
+                                                        _p(ws), ws.numel(), _stream()))
+    return out
 
 
 def eqat_profile_start():

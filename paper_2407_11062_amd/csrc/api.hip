@@ -194,7 +194,7 @@ const char *eqat_status_string(int status)
     case EQAT_ERR_ALIGN: return "pointer not 16-byte aligned (workspace: 256-byte)";
     case EQAT_ERR_WORKSPACE: return "workspace missing or too small";
     case EQAT_ERR_DEVICE: return "HIP launch failed";
-    case EQAT_ERR_HYPER: return "optimizer constants out of range (0 <= beta < 1, eps >= 0, step >= 1)";
+    case EQAT_ERR_HYPER: return "constants out of range (optimizer: 0 <= beta < 1, eps >= 0, step >= 1; attention: scale >= 0 and finite, window >= 0)";
     default: return "unknown status";
     }
 }
@@ -206,7 +206,8 @@ int eqat_profile_kernels(void) { return eqat::PK_COUNT; }
 const char *eqat_profile_kernel_name(int k)
 {
     static const char *names[] = {"init_minmax", "quantize", "e2e_prepare", "gemm_fwd", "gemm_dx",
-                                                "gemm_dw", "gemm_bwd", "reduce_partials", "f32_path", "gemv", "recon_loss", "adamw_update"};
+                                                "gemm_dw", "gemm_bwd", "reduce_partials", "f32_path", "gemv", "recon_loss", "adamw_update",
+                                                "kv_write", "kv_read", "kv_attend"};
     static_assert(sizeof(names) / sizeof(names[0]) == eqat::PK_COUNT, "one name per kernel class");
     return (k >= 0 && k < eqat::PK_COUNT) ? names[k] : "?";
 }

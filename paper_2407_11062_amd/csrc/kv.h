@@ -1,0 +1,93 @@
+// The key-value cache in 4 bits: what its kernels share.
+//
+// A pool holds pages; a page holds, head after head, records of 32 tokens (a multiple of them makes a page).  A record is what one wave takes in one step:
+//   keys' codes, values' codes    16 D bytes each, in the order in which the matrix instructions' lanes take them (below)
+//   keys' steps, values' steps    [G][32] words each: s in the low half of a word, m in the high half, both binary16, of (group, token)
+// A wave's lane l is (r, c) = (l % 16, l / 16).  v_mfma_f32_16x16x32_f16 takes eight k-elements of row (or column) r from every lane, those of chunk c; sums come back
+// as column r, rows 4 c .. 4 c + 3.
+//   Keys are the rows of S^T = K^ Q^T: lane (r, c) takes tokens r and 16 + r, and of 32-element step j the elements 32 j + 8 c .. + 7: one word, element e in
+//     half e & 1, nibble e >> 1.
+//   Values are transposed for O^T = V^T P^T: S^T left lane (r, c) the tokens 4 c .. 4 c + 3 and 16 + 4 c .. + 3 of column r, so those are its eight k-elements, and
+//     as row r of product n it takes element 32 (n / 2) + 2 r + n % 2 (16 elements of one group of 32 or more): a word holds, for two neighbouring tokens, one half
+//     each, the elements of products 4 a .. 4 a + 3 in its nibbles.
+// Neither scores nor probabilities ever change lanes.
+//
+// A code is read as a binary16 number without a conversion: the nibble in bits 0 - 3 of a half is c 2^-24, in bits 4 - 7 it is c 2^-20, both denormal, which the
+// matrix instructions take exactly.  A word gives its eight codes in one shift and four masks.
+#pragma once
+#include "common.h"
+
+namespace eqat {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+
+constexpr int kKvRecord = 32;        // tokens
+
+struct KvShape {
+    int heads, head_dim, group, groups, page_records;
+    int64_t pages;
+    bool act_bf16;
+};
+// NS steps of 32 elements to a head, SG of them to a group
+template <int NS, int SG> struct KvRecord {
+    static constexpr int D = 32 * NS, G = NS / SG;
+    static constexpr int kKeys = 0, kValues = 16 * D, kKeySteps = 32 * D, kValueSteps = 32 * D + 128 * G, kBytes = 32 * D + 256 * G;
+};
+inline int64_t kv_record_bytes(int head_dim, int groups) { return 32 * (int64_t)head_dim + 256 * groups; }
+
+// The sequences of a call (device arrays), and the bounds within which the kernels take what stands in them.
+struct KvBatch {
+    const int32_t *table, *lens, *starts;
+    int sequences, table_stride, max_new, max_len;
+    int64_t tokens;
+};
+
+struct KvRows { void *p; int64_t token_stride, head_stride; };       // in elements
+
+// ---- kv_cache.hip ----------------------------------------------------------------------------
+void launch_kv_write(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, void *pool, hipStream_t st);
+void launch_kv_read(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, const void *pool, hipStream_t st);
+
+// ---- kv_attend.hip ---------------------------------------------------------------------------
+struct KvAttend {
+    KvRows q, out;
+    float *lse;
+    int q_heads, window;
+    bool causal;
+    float scale;
+};
+size_t kv_attend_ws_bytes(const KvShape &s, const KvBatch &b, int q_heads);
+void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &a, const void *pool, void *ws, hipStream_t st);
+
+
+// Sequence `b` of a call: its new tokens are rows first .. first + n - 1 of the call's tensors and stand at positions len - n .. len - 1.
+struct KvSeq { int first, n, len; };
+__device__ __forceinline__ KvSeq kv_seq(const KvBatch &k, int page_tokens, int b)
+{
+    const int total = (int)k.tokens;
+    KvSeq s;
+    s.first = min(max(k.starts[b], 0), total);
+    s.n = min(max(min(k.starts[b + 1], total) - s.first, 0), k.max_new);
+    const int64_t most = min((int64_t)k.table_stride * page_tokens, (int64_t)k.max_len);
+    s.len = (int)min((int64_t)max(k.lens[b], 0), most);
+    return s;
+}
+
+// The sequence that row `t` of the call's tensors belongs to: the number of sequences that end at or before it.
+__device__ __forceinline__ int kv_seq_of(const KvBatch &k, int t)
+{
+    int b = 0;
+    if (k.sequences <= 64) {
+        for (int i = 1; i < k.sequences; ++i) b += k.starts[i] <= t ? 1 : 0;
+    } else {
+        int hi = k.sequences - 1;             // starts[b] <= t for the last such b
+        while (b < hi) {
+            const int mid = (b + hi + 1) >> 1;
+            if (k.starts[mid] <= t) b = mid; else hi = mid - 1;
+        }
+    }
+    return b;
+}
+
+}  // namespace eqat
