@@ -399,8 +399,8 @@ eqat_status eqat_dx_route(const eqat_desc *d, int block_ap, int32_t *route);
  *
  *   In groups of `group` neighbouring elements of a key or a value (of one token and head), sixteen steps from the least element to the greatest:
  *     m = f16(min x),  s = f16(max((max x - min x) / 15, 2^-24)),  c = clamp(round((x - m) / s), 0, 15),  x^ = m + s c
- *   in binary32 (the quotients correctly rounded, round() half to even), f16 the nearest binary16 number.  A group with an element that is not finite, or whose m or s
- *   is not (|x| beyond 65504), stands as NaN; one that spans less than about 2^-16 is held in steps of 2^-24.
+ *   in binary32 (the quotients correctly rounded, round() half to even), f16 the nearest binary16 number.  A group with an element that is not finite, or beyond
+ *   binary16 (65504), stands as NaN; one that spans less than about 2^-16 is held in steps of 2^-24.
  *
  *   Pool       eqat_kv_pool_bytes(desc) bytes of device memory, 256-byte aligned, owned by the caller; of any size (offsets are 64 bits), of any contents at first.
  *              It is a number of pages of `page_tokens` tokens; how a page is laid out is the library's own.  Bytes per token and head: head_dim + 8 head_dim / group.

@@ -9,8 +9,7 @@
 // A matrix instruction drops what lies 2^-26 below its largest term, its addend among them.  With fp32 activations the two parts and the records are therefore added
 // up outside, and codes are taken as c - 8 about m + 8 s, which leaves less to cancel between the two sums.  The softmax keeps a running maximum
 // and sum; the maximum moves only when a score passes it by 2 in log2, so that most records rescale nothing (p <= 4, and s < 2^14, so p s stays in binary16).
-#include "gemm_tiles.h"
-#include "kv.h"
+#include "kv_work.h"
 
 namespace eqat {
 namespace {
@@ -20,20 +19,6 @@ constexpr int kRowsOfUnit = 16;                    // rows (query, head of the g
 constexpr int kWorkgroups = 1024;                  // what the division of the work aims at: four workgroups on each of 256 compute units
 constexpr int kFewestRecords = 2 * kWaves;         // of a chunk
 
-struct AttendArgs {
-    KvBatch b;
-    KvRows q, out;
-    float *lse, *parts;                            // parts: [chunk][head][16 rows][D] sums, then [chunk][head][16 rows][2] maxima and totals
-    uint32_t *counters;                            // [unit][head], zero before and after every launch
-    const uint8_t *pool;
-    int64_t pages;
-    int heads, ratio, page_records, window, target, slots;
-    bool causal;
-    float scale;                                   // times log2(e)
-};
-
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-
 // f16(a * s.lo), f16(b * t.lo) in the halves of a register, s, t words whose low half is a binary16 number: the form that the compiler makes v_fma_mixlo_f16 and
 // v_fma_mixhi_f16 of, with the wait states that those owe
 __device__ __forceinline__ uint32_t scaled_pair(float a, uint32_t s, float b, uint32_t t)
@@ -41,29 +26,6 @@ __device__ __forceinline__ uint32_t scaled_pair(float a, uint32_t s, float b, ui
     const half2v r = {(_Float16)__builtin_fmaf(a, (float)__builtin_bit_cast(half2v, s)[0], 0.0f), (_Float16)__builtin_fmaf(b, (float)__builtin_bit_cast(half2v, t)[0], 0.0f)};
     return __builtin_bit_cast(uint32_t, r);
 }
-__device__ __forceinline__ float low_half(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)w); }
-__device__ __forceinline__ float high_half(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(w >> 16)); }
-
-// over the lanes l, l ^ 16, l ^ 32, l ^ 48
-__device__ __forceinline__ float chunks_max(float v)
-{
-    const uint32_t a = __float_as_uint(v);
-    const uintx2 p = __builtin_amdgcn_permlane32_swap(a, a, false, false);
-    const float w = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-    const uint32_t b = __float_as_uint(w);
-    const uintx2 q = __builtin_amdgcn_permlane16_swap(b, b, false, false);
-    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-__device__ __forceinline__ float chunks_sum(float v)
-{
-    const uint32_t a = __float_as_uint(v);
-    const uintx2 p = __builtin_amdgcn_permlane32_swap(a, a, false, false);
-    const float w = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    const uint32_t b = __float_as_uint(w);
-    const uintx2 q = __builtin_amdgcn_permlane16_swap(b, b, false, false);
-    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
-}
-
 // Two codes of a word (kv.h) as binary16: products 0 .. 3 of a value chunk, or the four pairs of a key word.
 // CENTRED (fp32): c - 8, times 16 in the odd pairs: 1024 + c or 1024 + 16 c by the bits, less 1032 or 1152.  Else c 2^-24 or c 2^-20, as the bits are.
 template <bool CENTRED> __device__ __forceinline__ uint32_t pick(uint32_t w, int p)
@@ -77,74 +39,6 @@ template <bool CENTRED> __device__ __forceinline__ float middle(uint32_t step)  
 {
     return CENTRED ? __builtin_fmaf(8.0f, low_half(step), high_half(step)) : high_half(step);
 }
-__device__ __forceinline__ floatx4 mfma(const uintx4 &a, const half8 &b, const floatx4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), b, c, 0, 0, 0); }
-
-// How the work of a call is divided: a unit is up to 16 rows of a sequence (times every head of the cache), its records are cut into chunks of C, and a workgroup
-// takes a chunk.  C follows from the lengths as they are on the device, so that the chunks of all sequences are about `target` in all, however their lengths differ.
-struct Work { int b, unit, chunk, chunks, first, last, part, counter; KvSeq s; bool any; };
-
-struct Extent { int units, lo, hi; };
-__device__ __forceinline__ Extent extent_of(const AttendArgs &a, const KvSeq &s)
-{
-    Extent e;
-    e.units = (s.n * a.ratio + kRowsOfUnit - 1) / kRowsOfUnit;
-    e.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) >> 5 : 0;
-    e.hi = (s.len + 31) >> 5;
-    return e;
-}
-
-__device__ __forceinline__ Work work_of(const AttendArgs &a, int slot)
-{
-    const int lane = threadIdx.x & 63, page_tokens = a.page_records * kKvRecord;
-    uint64_t records = 0;
-    for (int base = 0; base < a.b.sequences; base += 64) {
-        const int b = base + lane;
-        if (b < a.b.sequences) {
-            const Extent e = extent_of(a, kv_seq(a.b, page_tokens, b));
-            records += (uint64_t)e.units * (uint64_t)(e.hi - e.lo);
-        }
-    }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) records += __shfl_xor(records, d);
-    const int C = max((int)((records + a.target - 1) / a.target), kFewestRecords);
-    Work w{};
-    int before = 0, parts = 0, counters = 0;
-    bool found = false;
-    for (int base = 0; base < a.b.sequences; base += 64) {
-        const int b = base + lane;
-        KvSeq s{};
-        Extent e{};
-        if (b < a.b.sequences) { s = kv_seq(a.b, page_tokens, b); e = extent_of(a, s); }
-        const int chunks = e.units > 0 ? max(1, (e.hi - e.lo + C - 1) / C) : 0, mine = e.units * chunks, cut = chunks > 1 ? e.units : 0;
-        int x = mine, y = cut * chunks, z = cut;         // inclusive sums over the lanes
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int xx = __shfl_up(x, d), yy = __shfl_up(y, d), zz = __shfl_up(z, d);
-            if (lane >= d) { x += xx; y += yy; z += zz; }
-        }
-        const int at = slot - before - (x - mine);       // this slot within the sequence of the lane
-        const uint64_t has = __ballot(at >= 0 && at < mine);
-        if (has != 0 && !found) {
-            const int src = __ffsll((unsigned long long)has) - 1;
-            found = true;
-            const int i = __shfl(at, src);
-            w.b = base + src;
-            w.chunks = __shfl(chunks, src);
-            w.unit = i / w.chunks;
-            w.chunk = i - w.unit * w.chunks;
-            w.s.first = __shfl(s.first, src); w.s.n = __shfl(s.n, src); w.s.len = __shfl(s.len, src);
-            const int lo = __shfl(e.lo, src), hi = __shfl(e.hi, src);
-            w.first = lo + w.chunk * C;
-            w.last = min(hi, w.first + C);
-            w.part = parts + __shfl(y - cut * chunks, src) + i;
-            w.counter = counters + __shfl(z - cut, src) + w.unit;
-        }
-        before += __shfl(x, 63); parts += __shfl(y, 63); counters += __shfl(z, 63);
-    }
-    w.any = found && before <= a.slots;                  // more than the host was told of: nothing is computed
-    return w;
-}
-
 template <int NS, int SG, bool F32> __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(const AttendArgs a)
 {
     using R = KvRecord<NS, SG>;
@@ -445,23 +339,20 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(kWaves * 64) vo
         a.lse[(int64_t)(w.s.first + oquery) * ((int64_t)a.heads * a.ratio) + oh] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
-int units_at_most(const KvBatch &b, int ratio)
-{
-    const int64_t each = (int64_t)b.sequences * (((int64_t)b.max_new * ratio + kRowsOfUnit - 1) / kRowsOfUnit);
-    const int64_t all = (b.tokens * ratio + kRowsOfUnit - 1) / kRowsOfUnit + b.sequences;
-    return (int)(each < all ? each : all);
-}
 // chunks that the division aims at, for every head of the cache
 int chunks_aimed_at(const KvShape &s) { return (kWorkgroups + s.heads - 1) / s.heads; }
 
-struct WsLayout { size_t counters, parts, total; };
-WsLayout ws_layout(const KvShape &s)
+// Sequences with more rows than this go to the kernel that rebuilds keys and values (bf16).
+constexpr int kStreamedRows = 64;
+
+struct WsLayout { Scratch streamed, prompts; };
+WsLayout ws_layout(const KvShape &s, const KvBatch &b, int q_heads)
 {
-    const size_t target = (size_t)chunks_aimed_at(s) * s.heads;
     WsLayout l;
-    l.counters = 0;                                           // at most one cut unit per chunk aimed at
-    l.parts = (target * 4 + 255) / 256 * 256;
-    l.total = l.parts + 2 * target * (size_t)(kRowsOfUnit * (s.head_dim * 4 + 8));       // a cut unit has fewer than twice its share of the chunks aimed at
+    l.streamed = scratch_of(0, chunks_aimed_at(s), s.heads, kRowsOfUnit, s.head_dim);
+    l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
+    if (s.act_bf16 && (int64_t)b.max_new * (q_heads / s.heads) > kStreamedRows)
+        l.prompts = scratch_of((l.streamed.end + 255) / 256 * 256, prompt_target(s), s.heads, prompt_unit_rows(s), s.head_dim);
     return l;
 }
 
@@ -474,20 +365,35 @@ template <int NS, int SG> void launch(const KvShape &s, const AttendArgs &a, hip
 
 }  // namespace
 
-size_t kv_attend_ws_bytes(const KvShape &s, const KvBatch &, int) { return ws_layout(s).total; }
+size_t kv_attend_ws_bytes(const KvShape &s, const KvBatch &b, int q_heads) { return ws_layout(s, b, q_heads).prompts.end; }
 
 void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &t, const void *pool, void *ws, hipStream_t st)
 {
-    const WsLayout l = ws_layout(s);
+    const WsLayout l = ws_layout(s, b, t.q_heads);
     AttendArgs a;
     a.b = b; a.q = t.q; a.out = t.out; a.lse = t.lse;
-    a.counters = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ws) + l.counters);
-    a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + l.parts);
     a.pool = static_cast<const uint8_t *>(pool);
     a.pages = s.pages; a.heads = s.heads; a.ratio = t.q_heads / s.heads; a.page_records = s.page_records; a.window = t.window; a.causal = t.causal;
-    a.target = chunks_aimed_at(s);
-    a.slots = a.target + units_at_most(b, a.ratio);
     a.scale = t.scale * 1.4426950408889634f;
+    auto scratch = [&](const Scratch &x) {
+        a.counters = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ws) + x.counters);
+        a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + x.parts);
+    };
+    const bool prompts = s.act_bf16 && (int64_t)b.max_new * a.ratio > kStreamedRows;
+    if (prompts) {
+        a.from_rows = kStreamedRows + 1; a.to_rows = INT32_MAX;
+        scratch(l.prompts);
+        launch_kv_prompt(s, a, st);
+        if (b.tokens == (int64_t)b.sequences * b.max_new) return;        // all sequences have as many new tokens
+    }
+    a.from_rows = 1; a.to_rows = prompts ? kStreamedRows + 1 : INT32_MAX;
+    scratch(l.streamed);
+    a.unit_rows = kRowsOfUnit;
+    a.fewest = kFewestRecords;
+    a.target = chunks_aimed_at(s);
+    KvBatch few = b;
+    if (prompts) few.max_new = kStreamedRows / a.ratio;
+    a.slots = a.target + units_at_most(few, a.ratio, kRowsOfUnit);
     const int sg = s.group / 32;
     switch (s.head_dim) {
     case 64: if (sg == 1) launch<2, 1>(s, a, st); else launch<2, 2>(s, a, st); break;

@@ -26,12 +26,13 @@ template <int LANES> __device__ __forceinline__ float row_max(float v)
     return v;
 }
 
-// A group's step and least element, as they stand in the cache.  `odd` is 0, or NaN where an element is not finite: the whole group then stands as NaN.
+// A group's step and least element, as they stand in the cache.  `odd` is 0, or NaN where an element is not finite: the whole group then stands as NaN,
+// as one with an element beyond binary16 does (so no step passes 131008 / 15, and what a kernel makes of codes and steps stays within binary16 or a rounding of it).
 struct Step { float s, m; uint32_t word; };
 __device__ __forceinline__ Step step_of(float least, float greatest, float odd)
 {
     _Float16 m = (_Float16)least, s = (_Float16)fmaxf((greatest - least) / 15.0f, 0x1p-24f);
-    if (!(fabsf((float)m) + fabsf((float)s) + odd < __builtin_inff())) { m = (_Float16)__builtin_nanf(""); s = m; }
+    if (!(fabsf((float)m) + fabsf((float)(_Float16)greatest) + odd < __builtin_inff())) { m = (_Float16)__builtin_nanf(""); s = m; }
     Step r;
     r.s = (float)s; r.m = (float)m;
     r.word = (uint32_t)__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, m) << 16;

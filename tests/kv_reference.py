@@ -11,7 +11,7 @@ def steps(x, g):
     fifteen = torch.tensor(15.0, dtype=torch.float64)
     m = lo.half()
     s = ((hi - lo).float().double() / fifteen).float().clamp_min(2.0 ** -24).half()
-    bad = ~(torch.isfinite(s) & torch.isfinite(m) & torch.isfinite(y).all(-1))
+    bad = ~torch.isfinite(y.half()).all(-1)                  # not finite, or beyond binary16
     s, m = s.masked_fill(bad, math.nan), m.masked_fill(bad, math.nan)
     c = ((y - m.double().unsqueeze(-1)).float().double() / s.double().unsqueeze(-1)).float().double().round().clamp(0, 15)
     return s.double(), m.double(), c
@@ -26,10 +26,12 @@ def held(x, g):
 def attention(q, k, v, g, scale=None, causal=True, window=0, gone=None):
     """One sequence: q [n, Hq, D] stand at its last n positions, k and v [L, H, D] as they were written; gone: positions that are not there.
     Returns out, lse, and bounds on their errors (apart from the rounding of out to its type): the scores are binary32 sums of |q| (|m| + s c) terms,
-    and the weights of the sums over codes are rounded to 11 bits (bf16) or 22 (fp32)."""
+    and the weights of the sums over codes are rounded to 11 bits (bf16) or 22 (fp32).  A bf16 sequence of more than 64 rows (query, head that shares a head of the
+    cache) has its keys and values rebuilt as binary16: 2^-12 of every |q| |k^| in a score, 2^-12 of a value."""
     n, Hq, D = q.shape
     L, H = k.shape[:2]
     R = Hq // H
+    rebuilt = q.dtype == torch.bfloat16 and n * R > 64
     scale = scale or 1 / math.sqrt(D)
     ks, km, kc = steps(k, g)
     kh = held(k, g)
@@ -62,6 +64,8 @@ def attention(q, k, v, g, scale=None, causal=True, window=0, gone=None):
             p = torch.exp(S - lse[i, h])
             out[i, h] = p @ V[at]
             eps = 2.0 ** -21 * float((size[at, h // R] @ Q[i].abs()).max()) * scale       # of a score: 2^-22 for either of its two sums
+            if rebuilt:
+                eps += 2.0 ** -12 * float((K[at].abs() @ Q[i].abs()).max()) * scale + 2.0 ** -24
             weights = p @ span[at, h // R]
             tol_o[i, h] = weights * (r + 2 * eps + 2.0 ** -19)
             tol_l[i, h] = eps + 2.0 ** -20 * (1 + lse[i, h].abs())

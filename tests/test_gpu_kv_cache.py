@@ -134,14 +134,15 @@ def test_groups_that_are_constant_tiny_huge_or_not_finite(dtype):
         x[6, 0, 70] = -math.inf
         x[7, 0, 100] = 1e6               # beyond binary16: the step is not finite
         x[8, 1, 3] = -7e4                # the least element is not
-        x[9, 0, 3] = 7e4                 # this one is: the step is finite, and so is the least element
+        x[9, 0, 3] = 7e4                 # the greatest is, though step and least element are binary16 numbers
+        x[9, 1, 3], x[9, 1, 4] = 65280.0, -65280.0          # the largest of both types
         x[10, 0, 64:96] = -65504.0
     s = Setup([(11, 11)], 2, D, g, dtype, key_edit=edit, value_edit=edit).fill()
     k, v = eq.eqat_kv_read(s.cache, s.batch(s.lens))
     for got, xs in ((k, s.k), (v, s.v)):
         want = as_type(ref.held(xs[0], g), dtype)
         assert same(got.cpu(), want)
-        assert want[4, 0, :32].isnan().all() and not want[4, 0, 32:].isnan().any() and want[8, 1, :32].isnan().all() and want[9].isfinite().all()
+        assert want[4, 0, :32].isnan().all() and not want[4, 0, 32:].isnan().any() and want[8, 1, :32].isnan().all() and want[9, 0, :32].isnan().all() and want[9, 1].isfinite().all()
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
