@@ -65,6 +65,9 @@ eqat_status check_heads(const KvShape &s, const KvBatch &b, int q_heads)
 {
     if (q_heads < s.heads || q_heads % s.heads != 0 || q_heads > 1 << 20) return EQAT_ERR_SHAPE;
     const int64_t ratio = q_heads / s.heads;
+    // the streamed kernel counts the records of all units of 16 rows; a bf16 sequence of more than 64 rows is not its business
+    const double units = s.act_bf16 ? 4.0 * b.sequences : (double)(b.tokens * ratio) / 16 + b.sequences;
+    if (units * (b.max_len / 32 + 1.0) > 2.0e9) return EQAT_ERR_SHAPE;
     if (b.tokens * q_heads >= kMost || (int64_t)b.max_new * ratio >= kMost || ((int64_t)b.sequences + b.tokens * ratio / 16 + 2048) * s.heads >= kMost) return EQAT_ERR_SHAPE;
     return EQAT_OK;
 }
@@ -117,7 +120,7 @@ size_t eqat_kv_workspace_bytes(const eqat_kv_desc *d, const eqat_kv_batch *b, in
     KvShape s; KvBatch k;
     if (check_desc(d, &s) != EQAT_OK || b == nullptr) return 0;
     k.tokens = b->tokens; k.sequences = b->sequences; k.max_new = b->max_new; k.max_len = b->max_len;
-    if (k.tokens < 0 || k.sequences < 0 || k.max_new < 0 || check_heads(s, k, q_heads) != EQAT_OK) return 0;
+    if (k.tokens < 0 || k.max_len < 0 || k.sequences < 0 || k.max_new < 0 || check_heads(s, k, q_heads) != EQAT_OK) return 0;
     return eqat::kv_attend_ws_bytes(s, k, q_heads);
 }
 

@@ -1,5 +1,8 @@
-// Attention over the 4-bit cache, streamed: every wave takes whole records of 32 tokens straight from memory into registers, for up to 16 rows (query, head) that
-// share a head of the cache.
+// Attention over the 4-bit cache, streamed: a wave takes whole records of 32 tokens, for up to 16 rows (query, head) that share a head of the cache.
+//
+// Bound by the bytes of the cache.  The records that a head of the cache holds for all rows of a call are one row of work, cut into equal shares, one for a workgroup and as
+// many as are resident: a share may end within a unit (16 rows of a sequence) and begin in the next, so lengths that differ leave nobody waiting.  Records come by
+// direct-to-LDS loads into a ring of each wave's own, so that two are on their way while one is worked on, without a register.
 //
 // With x^ = m + s c (kv.h) the sums over elements and tokens part into sums over codes, which are exact in binary16, and sums over the steps:
 //   q . k^_t   = sum over groups g of  s_tg (q_g . c_tg) + m_tg sum(q_g)
@@ -14,10 +17,12 @@
 namespace eqat {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int waves_of(int head_dim) { return head_dim > 128 ? 4 : 8; }         // of a workgroup, one on each compute unit
 constexpr int kRowsOfUnit = 16;                    // rows (query, head of the group) of a unit
-constexpr int kWorkgroups = 1024;                  // what the division of the work aims at: four workgroups on each of 256 compute units
-constexpr int kFewestRecords = 2 * kWaves;         // of a chunk
+constexpr int kFewestRecords = 32;                 // of a share: a join with another workgroup costs about as much (one token at 515: 32 8.3 us, 16 9.5, 8 9.3)
+constexpr int kFewParts = 4;                       // parts of a unit that are fetched together
+constexpr int kResident = 256;                     // workgroups
+constexpr int depth_of(int head_dim) { return head_dim > 128 ? 2 : 3; }          // records of a wave's ring
 
 // f16(a * s.lo), f16(b * t.lo) in the halves of a register, s, t words whose low half is a binary16 number: the form that the compiler makes v_fma_mixlo_f16 and
 // v_fma_mixhi_f16 of, with the wait states that those owe
@@ -39,308 +44,370 @@ template <bool CENTRED> __device__ __forceinline__ float middle(uint32_t step)  
 {
     return CENTRED ? __builtin_fmaf(8.0f, low_half(step), high_half(step)) : high_half(step);
 }
-template <int NS, int SG, bool F32> __global__ __launch_bounds__(kWaves * 64) void k_kv_attend(const AttendArgs a)
+template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * NS) * 64, waves_of(32 * NS) / 4) void k_kv_attend(const AttendArgs a)
 {
     using R = KvRecord<NS, SG>;
     using T = typename std::conditional<F32, float, bf16_t>::type;
-    constexpr int D = R::D, G = R::G, kChunks = NS / 2, kPad = D + 4;
+    constexpr int D = R::D, G = R::G, kChunks = NS / 2, kPad = D + 4, kWaves = waves_of(D), kDepth = depth_of(D), kStepLoads = (G + 3) / 4, kLoads = 2 * kChunks + kStepLoads;
     constexpr float kUnit = F32 ? 1.0f : 0x1p24f;          // what a code's binary16 form is divided by
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];              // the waves' rings; then the waves' sums [wave][row][kPad]
+    __shared__ float s_ml[kWaves][kRowsOfUnit][2];
+    __shared__ uint32_t s_last;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, c = lane >> 4;
-    const int head = blockIdx.x % a.heads;
-    const Work w = work_of(a, blockIdx.x / a.heads);
-    if (!w.any) return;
-    // ---- this lane's row of the queries -----------------------------------------------------------
-    const int row = w.unit * kRowsOfUnit + r, query = row / a.ratio, of_group = row - query * a.ratio;
-    const bool is_row = query < w.s.n;
-    const int pos = w.s.len - w.s.n + query;
-    const int seen_to = is_row && a.causal ? min(w.s.len, pos + 1) : w.s.len;             // positions seen_from .. seen_to - 1 (a row that is none restricts nothing)
-    const int seen_from = is_row && a.window > 0 ? max(0, pos - a.window + 1) : 0;
-    half8 qh[NS], ql[F32 ? NS : 1];
-    float sums[G], k_scale;
-    {
-        const T *q = static_cast<const T *>(a.q.p) + (int64_t)(w.s.first + query) * a.q.token_stride + (int64_t)(head * a.ratio + of_group) * a.q.head_stride;
-        float x[NS][8], top = 0.0f;
+    const int head = blockIdx.x % a.heads, slot = blockIdx.x / a.heads;
+    uint8_t *ring = lds + wave * kDepth * R::kBytes;
+    const uint32_t ring_at = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_addr_of(ring));
+    const Lane sequences = lane_of(a, 0);
+    const Share mine = share_of(a, slot, sequences);
+    Segment w{};
+    for (int at = mine.first; at < mine.last; at = w.to) {
+        w = segment_of(a, mine, at, sequences);
+        if (!w.any) return;
+        // ---- this lane's row of the queries -----------------------------------------------------------
+        const int row = w.unit * kRowsOfUnit + r, query = quotient(row, a.ratio), of_group = row - query * a.ratio;
+        const bool is_row = query < w.s.n;
+        const int pos = w.s.len - w.s.n + query;
+        const int seen_to = is_row && a.causal ? min(w.s.len, pos + 1) : w.s.len;             // positions seen_from .. seen_to - 1 (a row that is none restricts nothing)
+        const int seen_from = is_row && a.window > 0 ? max(0, pos - a.window + 1) : 0;
+        // Records w.rec + wave, + kWaves, ...: lane i looks up where the i-th of 64 of them lies (-1: its page is not there).
+        const int32_t *table = a.b.table + (int64_t)w.b * a.b.table_stride;
+        int place_lo = -1, place_hi = -1;
+        auto look_up = [&](int from) {
+            const int rec = from + lane * kWaves, of_seq = quotient(rec, a.page_records);
+            const int page = rec < w.rec_to ? table[of_seq] : -1;
+            const int64_t at = page >= 0 && page < a.pages ? (((int64_t)page * a.heads + head) * a.page_records + (rec - of_seq * a.page_records)) * R::kBytes : -1;
+            place_lo = (int)at; place_hi = (int)(at >> 32);
+        };
+        const int first_rec = w.rec + wave, records = max(0, (w.rec_to - first_rec + kWaves - 1) / kWaves);
+        look_up(first_rec);
+        T loaded[NS][8];
+        if (is_row) {
+            const T *q = static_cast<const T *>(a.q.p) + (int64_t)(w.s.first + query) * a.q.token_stride + (int64_t)(head * a.ratio + of_group) * a.q.head_stride;
 #pragma unroll
-        for (int j = 0; j < NS; ++j) {
+            for (int j = 0; j < NS; ++j) __builtin_memcpy(loaded[j], __builtin_assume_aligned(q + 32 * j + 8 * c, 16), sizeof(loaded[j]));
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[j][e] = 0.0f;
-            if (is_row) {
-                if constexpr (F32) {
-                    const floatx4 u = *reinterpret_cast<const floatx4 *>(q + 32 * j + 8 * c), v = *reinterpret_cast<const floatx4 *>(q + 32 * j + 8 * c + 4);
+            for (int j = 0; j < NS; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { x[j][e] = u[e]; x[j][4 + e] = v[e]; }
-                } else {
-                    const bf16x8 u = *reinterpret_cast<const bf16x8 *>(q + 32 * j + 8 * c);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[j][e] = (float)u[e];
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[j][e]));
+                for (int e = 0; e < 8; ++e) loaded[j][e] = (T)0.0f;
         }
-        // the row scaled by a power of two to a largest element in [2^13, 2^14): code products are sums of q c 2^-24 or, for the pairs in bits 4 - 7, of (q 2^-4) c 2^-20
-        top = chunks_max(top);
-        const int up = min(max(140 - (int)(__float_as_uint(top) >> 23), -100), 100);
-        const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
+        // The i-th record of this wave into the ring.  The loads are assembly, so nothing but the waits below counts them; a record that is not there is fetched from
+        // the pool's first bytes and not looked at, so that every record counts as many.
+        uint64_t gone = 0;                                     // bit i & 63: the i-th record is not there
+        auto fetch = [&](int i) {
+            if (i > 0 && (i & 63) == 0) look_up(first_rec + i * kWaves);
+            const int64_t place = (int64_t)(uint32_t)__builtin_amdgcn_readlane(place_lo, i & 63) | (int64_t)__builtin_amdgcn_readlane(place_hi, i & 63) << 32;
+            gone = place < 0 ? gone | (uint64_t)1 << (i & 63) : gone & ~((uint64_t)1 << (i & 63));
+            const RawRsrc src = make_raw_rsrc(a.pool + (place < 0 ? 0 : place), R::kBytes);
+            const uint32_t to = ring_at + (uint32_t)(i % kDepth) * R::kBytes;
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            float s = 0.0f;
+            for (int k = 0; k < 2 * kChunks; ++k) load_to_lds16_at(src, to + k * 1024, (uint32_t)(k * 1024 + lane * 16));
 #pragma unroll
-            for (int j = 0; j < SG; ++j)
+            for (int k = 0; k < kStepLoads; ++k)
+                if (G >= 4 || lane < 16 * G) load_to_lds16_at(src, to + R::kKeySteps + k * 1024, (uint32_t)(R::kKeySteps + k * 1024 + lane * 16));
+        };
+        // the queries' loads and the look-up are complete before the first record's are issued: a wait for them would wait for those too
+        __builtin_amdgcn_s_waitcnt(0x0F70);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s += x[g * SG + j][e];
-            sums[g] = chunks_sum(s) * scale * (1.0f / kUnit);
-        }
+        for (int i = 0; i < kDepth - 1; ++i) if (i < records) fetch(i);
+        half8 qh[NS], ql[F32 ? NS : 1];
+        float sums[G], k_scale;
+        {
+            float x[NS][8], top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < NS; ++j)
+            for (int j = 0; j < NS; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = x[j][e] * scale, f = (e >> 1) & 1 ? 0x1p-4f : 1.0f;
-                const _Float16 h = (_Float16)(y * f);
-                qh[j][e] = h;
-                if constexpr (F32) ql[j][e] = (_Float16)(y * f - (float)h);
-            }
-        k_scale = a.scale * __uint_as_float((uint32_t)(127 - up) << 23) * kUnit;
-    }
-    // ---- the records of this wave -----------------------------------------------------------------
-    floatx4 o[2 * NS];
-    float top = -3.0e38f, total = 0.0f, even[G];            // running maximum, sum of p, sum of p m
-    float v_scale = 1.0f;                                   // fp32: what the accumulators are scaled by
-#pragma unroll
-    for (int n = 0; n < 2 * NS; ++n) o[n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int g = 0; g < G; ++g) even[g] = 0.0f;
-    // records that every row of the unit sees in full need no mask
-    int all_from = seen_from, all_to = seen_to;
-#pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) { all_from = max(all_from, __shfl_xor(all_from, d)); all_to = min(all_to, __shfl_xor(all_to, d)); }
-    all_from = __builtin_amdgcn_readfirstlane(all_from); all_to = __builtin_amdgcn_readfirstlane(all_to);
-
-    const int32_t *table = a.b.table + (int64_t)w.b * a.b.table_stride;
-    for (int rec = w.first + wave; rec < w.last; rec += kWaves) {
-        const int page_of_seq = rec / a.page_records, page = __builtin_amdgcn_readfirstlane(table[page_of_seq]);
-        if (page < 0 || page >= a.pages) continue;           // not there
-        const uint8_t *at = a.pool + (((int64_t)page * a.heads + head) * a.page_records + (rec - page_of_seq * a.page_records)) * R::kBytes;
-        uintx4 kc[kChunks], vc[kChunks], ks[G][2], vs[G][2];
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-            kc[i] = *reinterpret_cast<const uintx4 *>(at + R::kKeys + i * 1024 + lane * 16);
-            vc[i] = *reinterpret_cast<const uintx4 *>(at + R::kValues + i * 1024 + lane * 16);
-        }
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                ks[g][h] = *reinterpret_cast<const uintx4 *>(at + R::kKeySteps + g * 128 + h * 64 + c * 16);
-                vs[g][h] = *reinterpret_cast<const uintx4 *>(at + R::kValueSteps + g * 128 + h * 64 + c * 16);
-            }
-        const bool edge = rec * kKvRecord < all_from || (rec + 1) * kKvRecord > all_to;
-        float s[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
+                for (int e = 0; e < 8; ++e) { x[j][e] = (float)loaded[j][e]; top = fmaxf(top, fabsf(x[j][e])); }
+            // the row scaled by a power of two to a largest element in [2^13, 2^14): code products are sums of q c 2^-24 or, for the pairs in bits 4 - 7, of (q 2^-4) c 2^-20
+            top = chunks_max(top);
+            const int up = min(max(140 - (int)(__float_as_uint(top) >> 23), -100), 100);
+            const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f}, low = acc;
+                float s = 0.0f;
 #pragma unroll
-                for (int j = g * SG; j < (g + 1) * SG; ++j) {
-                    const uint32_t word = kc[(h * NS + j) >> 2][(h * NS + j) & 3];
-                    uintx4 codes;
+                for (int j = 0; j < SG; ++j)
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) codes[p] = pick<F32>(word, p);
-                    acc = mfma(codes, qh[j], acc);
-                    if constexpr (F32) low = mfma(codes, ql[j], low);
-                }
-                if constexpr (F32) acc += low;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float t = __builtin_fmaf(middle<F32>(ks[g][h][i]), sums[g], g == 0 ? 0.0f : s[h][i]);
-                    s[h][i] = __builtin_fmaf(low_half(ks[g][h][i]), acc[i], t);
-                }
+                    for (int e = 0; e < 8; ++e) s += x[g * SG + j][e];
+                sums[g] = chunks_sum(s) * scale * (1.0f / kUnit);
             }
-        if (edge) {
-            // what a row does not see must not reach it, NaN among it: neither its score nor, by way of 0 * NaN, its value
+#pragma unroll
+            for (int j = 0; j < NS; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = x[j][e] * scale, f = (e >> 1) & 1 ? 0x1p-4f : 1.0f;
+                    const _Float16 h = (_Float16)(y * f);
+                    qh[j][e] = h;
+                    if constexpr (F32) ql[j][e] = (_Float16)(y * f - (float)h);
+                }
+            k_scale = a.scale * __uint_as_float((uint32_t)(127 - up) << 23) * kUnit;
+        }
+        // ---- the records of this wave -----------------------------------------------------------------
+        floatx4 o[2 * NS];
+        float top = -3.0e38f, total = 0.0f, even[G];            // running maximum, sum of p, sum of p m
+        float v_scale = 1.0f;                                   // fp32: what the accumulators are scaled by
+#pragma unroll
+        for (int n = 0; n < 2 * NS; ++n) o[n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int g = 0; g < G; ++g) even[g] = 0.0f;
+        // records that every row of the unit sees in full need no mask
+        int all_from = seen_from, all_to = seen_to;
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) { all_from = max(all_from, __shfl_xor(all_from, d)); all_to = min(all_to, __shfl_xor(all_to, d)); }
+        all_from = __builtin_amdgcn_readfirstlane(all_from); all_to = __builtin_amdgcn_readfirstlane(all_to);
+
+        for (int i = 0; i < records; ++i) {
+            const int rec = first_rec + i * kWaves;
+            if (i + kDepth - 1 < records) {
+                __builtin_amdgcn_s_waitcnt(0xC07F);               // the reads of the record before this one, into whose place goes
+                fetch(i + kDepth - 1);
+                __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((kDepth - 1) * kLoads));
+            } else {
+                __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+            }
+            asm volatile("" ::: "memory");
+            if (gone >> (i & 63) & 1) continue;
+            const uint8_t *at = ring + (i % kDepth) * R::kBytes;
+            uintx4 kc[kChunks], vc[kChunks], ks[G][2], vs[G][2];
+#pragma unroll
+            for (int k = 0; k < kChunks; ++k) {
+                kc[k] = *reinterpret_cast<const uintx4 *>(at + R::kKeys + k * 1024 + lane * 16);
+                vc[k] = *reinterpret_cast<const uintx4 *>(at + R::kValues + k * 1024 + lane * 16);
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    ks[g][h] = *reinterpret_cast<const uintx4 *>(at + R::kKeySteps + g * 128 + h * 64 + c * 16);
+                    vs[g][h] = *reinterpret_cast<const uintx4 *>(at + R::kValueSteps + g * 128 + h * 64 + c * 16);
+                }
+            const bool edge = rec * kKvRecord < all_from || (rec + 1) * kKvRecord > all_to;
+            float s[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f}, low = acc;
+#pragma unroll
+                    for (int j = g * SG; j < (g + 1) * SG; ++j) {
+                        const uint32_t word = kc[(h * NS + j) >> 2][(h * NS + j) & 3];
+                        uintx4 codes;
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) codes[p] = pick<F32>(word, p);
+                        acc = mfma(codes, qh[j], acc);
+                        if constexpr (F32) low = mfma(codes, ql[j], low);
+                    }
+                    if constexpr (F32) acc += low;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float t = __builtin_fmaf(middle<F32>(ks[g][h][i]), sums[g], g == 0 ? 0.0f : s[h][i]);
+                        s[h][i] = __builtin_fmaf(low_half(ks[g][h][i]), acc[i], t);
+                    }
+                }
+            if (edge) {
+                // what a row does not see must not reach it, NaN among it: neither its score nor, by way of 0 * NaN, its value
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = rec * kKvRecord + h * 16 + c * 4 + i;
+                        const bool seen = t >= seen_from && t < seen_to;
+                        s[h][i] = seen ? s[h][i] : -__builtin_inff();
+#pragma unroll
+                        for (int g = 0; g < G; ++g) vs[g][h][i] = seen ? vs[g][h][i] : 0u;
+                    }
+            }
+            float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+            most = chunks_max(most) * k_scale;
+            if (__any(most > top + 2.0f)) {
+                const float next = fmaxf(top, most), down = exp2_of(top - next);
+                top = next;
+                total *= down;
+#pragma unroll
+                for (int g = 0; g < G; ++g) even[g] *= down;
+#pragma unroll
+                for (int n = 0; n < 2 * NS; ++n) o[n] *= down;
+            }
+            float p[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int t = rec * kKvRecord + h * 16 + c * 4 + i;
-                    const bool seen = t >= seen_from && t < seen_to;
-                    s[h][i] = seen ? s[h][i] : -__builtin_inff();
-#pragma unroll
-                    for (int g = 0; g < G; ++g) vs[g][h][i] = seen ? vs[g][h][i] : 0u;
+                    p[h][i] = exp2_of(__builtin_fmaf(s[h][i], k_scale, -top));
+                    total += p[h][i];
                 }
-        }
-        float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        most = chunks_max(most) * k_scale;
-        if (__any(most > top + 2.0f)) {
-            const float next = fmaxf(top, most), down = exp2_of(top - next);
-            top = next;
-            total *= down;
+            if constexpr (F32) {
+                // two binary16 numbers hold 22 bits of p s only where its low part does not run into denormals: values' steps are brought to about 2^11 by a power of two
+                uint32_t big = 0;
 #pragma unroll
-            for (int g = 0; g < G; ++g) even[g] *= down;
+                for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int n = 0; n < 2 * NS; ++n) o[n] *= down;
-        }
-        float p[2][4];
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+                        for (int i = 0; i < 4; ++i) { const float v = low_half(vs[g][h][i]); big = max(big, v < 65536.0f ? __float_as_uint(v) : 0u); }
+                if (edge) {                      // rows see different tokens
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[h][i] = exp2_of(__builtin_fmaf(s[h][i], k_scale, -top));
-                total += p[h][i];
+                    for (int d = 8; d >= 1; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+                }
+                const float most_step = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(chunks_max(__uint_as_float(big)))));
+                if (most_step * v_scale >= 4096.0f || (v_scale == 1.0f && most_step > 0.0f)) {
+                    const float next = __uint_as_float((uint32_t)(127 + 138 - (int)(__float_as_uint(most_step) >> 23)) << 23);
+#pragma unroll
+                    for (int n = 0; n < 2 * NS; ++n) o[n] *= next / v_scale;
+                    v_scale = next;
+                }
             }
-        if constexpr (F32) {
-            // two binary16 numbers hold 22 bits of p s only where its low part does not run into denormals: values' steps are brought to about 2^11 by a power of two
-            uint32_t big = 0;
 #pragma unroll
-            for (int g = 0; g < G; ++g)
+            for (int g = 0; g < G; ++g) {
+                uintx4 ph, pl;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) { const float v = low_half(vs[g][h][i]); big = max(big, v < 65536.0f ? __float_as_uint(v) : 0u); }
-            if (edge) {                      // rows see different tokens
+                    for (int i = 0; i < 4; ++i) even[g] = __builtin_fmaf(middle<F32>(vs[g][h][i]), p[h][i], even[g]);
 #pragma unroll
-                for (int d = 8; d >= 1; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
-            }
-            const float most_step = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(chunks_max(__uint_as_float(big)))));
-            if (most_step * v_scale >= 4096.0f || (v_scale == 1.0f && most_step > 0.0f)) {
-                const float next = __uint_as_float((uint32_t)(127 + 138 - (int)(__float_as_uint(most_step) >> 23)) << 23);
+                    for (int i = 0; i < 4; i += 2) {
+                        if constexpr (F32) {
+                            float x = p[h][i] * v_scale * low_half(vs[g][h][i]), y = p[h][i + 1] * v_scale * low_half(vs[g][h][i + 1]);
+                            asm("" : "+v"(x), "+v"(y));          // both uses below round the binary32 product (a mixed-precision product rounds once, and not to the same number)
+                            const half2v hi = {(_Float16)x, (_Float16)y}, lo = {(_Float16)(x - (float)hi[0]), (_Float16)(y - (float)hi[1])};
+                            ph[h * 2 + i / 2] = __builtin_bit_cast(uint32_t, hi);
+                            pl[h * 2 + i / 2] = __builtin_bit_cast(uint32_t, lo);
+                        } else {
+                            ph[h * 2 + i / 2] = scaled_pair(p[h][i], vs[g][h][i], p[h][i + 1], vs[g][h][i + 1]);
+                        }
+                    }
+                }
 #pragma unroll
-                for (int n = 0; n < 2 * NS; ++n) o[n] *= next / v_scale;
-                v_scale = next;
-            }
-        }
+                for (int n = 2 * g * SG; n < 2 * (g + 1) * SG; ++n) {
+                    uintx4 codes;
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            uintx4 ph, pl;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) even[g] = __builtin_fmaf(middle<F32>(vs[g][h][i]), p[h][i], even[g]);
-#pragma unroll
-                for (int i = 0; i < 4; i += 2) {
+                    for (int q = 0; q < 4; ++q) codes[q] = pick<F32>(vc[n >> 2][q], n & 3);
                     if constexpr (F32) {
-                        float x = p[h][i] * v_scale * low_half(vs[g][h][i]), y = p[h][i + 1] * v_scale * low_half(vs[g][h][i + 1]);
-                        asm("" : "+v"(x), "+v"(y));          // both uses below round the binary32 product (a mixed-precision product rounds once, and not to the same number)
-                        const half2v hi = {(_Float16)x, (_Float16)y}, lo = {(_Float16)(x - (float)hi[0]), (_Float16)(y - (float)hi[1])};
-                        ph[h * 2 + i / 2] = __builtin_bit_cast(uint32_t, hi);
-                        pl[h * 2 + i / 2] = __builtin_bit_cast(uint32_t, lo);
+                        const floatx4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                        o[n] += mfma(codes, __builtin_bit_cast(half8, ph), zero) + mfma(codes, __builtin_bit_cast(half8, pl), zero);
                     } else {
-                        ph[h * 2 + i / 2] = scaled_pair(p[h][i], vs[g][h][i], p[h][i + 1], vs[g][h][i + 1]);
+                        o[n] = mfma(codes, __builtin_bit_cast(half8, ph), o[n]);
                     }
                 }
             }
+            asm volatile("" ::: "memory");
+        }
+        // ---- the waves' sums joined ---------------------------------------------------------------------
+        float (*s_o)[kRowsOfUnit][kPad] = reinterpret_cast<float (*)[kRowsOfUnit][kPad]>(lds);
+        __syncthreads();                                          // the rings have been read
+        total = chunks_sum(total);
 #pragma unroll
-            for (int n = 2 * g * SG; n < 2 * (g + 1) * SG; ++n) {
-                uintx4 codes;
+        for (int g = 0; g < G; ++g) even[g] = chunks_sum(even[g]);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) codes[q] = pick<F32>(vc[n >> 2][q], n & 3);
-                if constexpr (F32) {
-                    const floatx4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                    o[n] += mfma(codes, __builtin_bit_cast(half8, ph), zero) + mfma(codes, __builtin_bit_cast(half8, pl), zero);
-                } else {
-                    o[n] = mfma(codes, __builtin_bit_cast(half8, ph), o[n]);
+        for (int j = 0; j < NS; ++j) {
+            // products 2 j and 2 j + 1: elements 32 j + 8 c + 0 .. 7
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int n = 2 * j + (i & 1);
+                x[i] = __builtin_fmaf(o[n][i >> 1], (n & 1 ? kUnit / 16.0f : kUnit) / v_scale, even[j / SG]);
+            }
+            *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c]) = floatx4{x[0], x[1], x[2], x[3]};
+            *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c + 4]) = floatx4{x[4], x[5], x[6], x[7]};
+        }
+        if (c == 0) { s_ml[wave][r][0] = top; s_ml[wave][r][1] = total; }
+        __syncthreads();
+        constexpr int kOut = kWaves == 8 && D == 128 ? 4 : D / 16, kOfRow = D / kOut;      // elements of a row that a thread takes, threads of a row
+        const bool joins = tid < kRowsOfUnit * kOfRow;
+        const int orow = joins ? tid / kOfRow : 0, d0 = (tid % kOfRow) * kOut;
+        float m = s_ml[0][orow][0], l = 0.0f, x[kOut] = {};
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) m = fmaxf(m, s_ml[i][orow][0]);
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            const float f = exp2_of(s_ml[i][orow][0] - m);
+            l = __builtin_fmaf(s_ml[i][orow][1], f, l);
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) x[e] = __builtin_fmaf(s_o[i][orow][d0 + e], f, x[e]);
+        }
+        const bool whole = w.unit_from >= mine.first && w.unit_to <= mine.last;
+        bool answers = true;
+        if (!whole) {
+            // Parts and counter are written and read at device scope (the workgroups sit on different XCDs): every wave waits for its stores, the workgroup meets, one
+            // lane counts it in, and the last to arrive adds up all parts in their order.  A workgroup has at most two parts: of the unit that it finds begun, and of the one
+            // that it leaves unfinished.
+            constexpr uint32_t kPart = kRowsOfUnit * D * 4, kStats = kRowsOfUnit * 8;
+            uint8_t *base = reinterpret_cast<uint8_t *>(a.parts), *stats = base + 2 * (int64_t)a.slots * a.heads * kPart;
+            const int from = w.unit_from / mine.size, arrivals = (w.unit_to - 1) / mine.size - from + 1;
+            auto part = [&](int k) { return ((int64_t)(from + k) * 2 + (k == 0 ? 1 : 0)) * a.heads + head; };          // of the k-th workgroup of the unit
+            {
+                const int64_t to = part(slot - from);
+                const __amdgpu_buffer_rsrc_t dst = make_rsrc(base + to * kPart, kPart), st = make_rsrc(stats + to * kStats, kStats);
+#pragma unroll
+                for (int e = 0; e < kOut; e += 4) {
+                    if (!joins) break;
+                    const intx4 v = {__float_as_int(x[e]), __float_as_int(x[e + 1]), __float_as_int(x[e + 2]), __float_as_int(x[e + 3])};
+                    __builtin_amdgcn_raw_buffer_store_b128(v, dst, (orow * D + d0 + e) * 4, 0, kAuxDeviceScope);
+                }
+                const intx2 v = {__float_as_int(m), __float_as_int(l)};
+                if (joins && d0 == 0) __builtin_amdgcn_raw_buffer_store_b64(v, st, orow * 8, 0, kAuxDeviceScope);
+            }
+            wait_all_and_barrier();
+            uint32_t *counter = a.counters + (int64_t)from * a.heads + head;
+            if (tid == 0) {
+                const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                s_last = before == (uint32_t)(arrivals - 1) ? 1u : 0u;
+                if (s_last != 0u) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            answers = s_last != 0u;
+            if (answers) {
+                m = -3.0e38f; l = 0.0f;
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) x[e] = 0.0f;
+                for (int k0 = 0; k0 < arrivals; k0 += kFewParts) {
+                    intx2 ml[kFewParts];
+                    intx4 v[kFewParts][kOut / 4];
+#pragma unroll
+                    for (int k = 0; k < kFewParts; ++k) {                // past the last part: an empty buffer, zeros
+                        const bool is = k0 + k < arrivals;
+                        const int64_t of = part(is ? k0 + k : 0);
+                        const __amdgpu_buffer_rsrc_t src = make_rsrc(base + of * kPart, is ? kPart : 0u), st = make_rsrc(stats + of * kStats, is ? kStats : 0u);
+                        ml[k] = __builtin_amdgcn_raw_buffer_load_b64(st, orow * 8, 0, kAuxDeviceScope);
+#pragma unroll
+                        for (int e = 0; e < kOut; e += 4) v[k][e / 4] = __builtin_amdgcn_raw_buffer_load_b128(src, (orow * D + d0 + e) * 4, 0, kAuxDeviceScope);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kFewParts; ++k) {
+                        const float other = k0 + k < arrivals ? __int_as_float(ml[k][0]) : -3.0e38f;
+                        const float next = fmaxf(m, other), f = exp2_of(m - next), g = exp2_of(other - next);
+                        m = next;
+                        l = __builtin_fmaf(__int_as_float(ml[k][1]), g, l * f);
+#pragma unroll
+                        for (int e = 0; e < kOut; ++e) x[e] = __builtin_fmaf(__int_as_float(v[k][e / 4][e % 4]), g, x[e] * f);
+                    }
                 }
             }
         }
-    }
-    // ---- the waves' sums joined ---------------------------------------------------------------------
-    __shared__ __attribute__((aligned(16))) float s_o[kWaves][kRowsOfUnit][kPad];
-    __shared__ float s_ml[kWaves][kRowsOfUnit][2];
-    total = chunks_sum(total);
-#pragma unroll
-    for (int g = 0; g < G; ++g) even[g] = chunks_sum(even[g]);
-#pragma unroll
-    for (int j = 0; j < NS; ++j) {
-        // products 2 j and 2 j + 1: elements 32 j + 8 c + 0 .. 7
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int n = 2 * j + (i & 1);
-            x[i] = __builtin_fmaf(o[n][i >> 1], (n & 1 ? kUnit / 16.0f : kUnit) / v_scale, even[j / SG]);
-        }
-        *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c]) = floatx4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c + 4]) = floatx4{x[4], x[5], x[6], x[7]};
-    }
-    if (c == 0) { s_ml[wave][r][0] = top; s_ml[wave][r][1] = total; }
-    __syncthreads();
-    constexpr int kOut = D / 16;                              // elements of a row that a thread takes
-    const int orow = tid >> 4, d0 = (tid & 15) * kOut;
-    float m = s_ml[0][orow][0], l = 0.0f, x[kOut] = {};
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) m = fmaxf(m, s_ml[i][orow][0]);
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        const float f = exp2_of(s_ml[i][orow][0] - m);
-        l = __builtin_fmaf(s_ml[i][orow][1], f, l);
-#pragma unroll
-        for (int e = 0; e < kOut; ++e) x[e] = __builtin_fmaf(s_o[i][orow][d0 + e], f, x[e]);
-    }
-    if (w.chunks > 1) {
-        // Parts and counter are written and read at device scope (the workgroups sit on different XCDs): every wave waits for its stores, the workgroup meets, one
-        // lane counts it in, and the last to arrive adds up all parts in their order.
-        __shared__ uint32_t s_last;
-        constexpr uint32_t kPart = kRowsOfUnit * D * 4, kStats = kRowsOfUnit * 8;
-        const int64_t parts = 2 * (int64_t)a.target * a.heads;
-        uint8_t *base = reinterpret_cast<uint8_t *>(a.parts), *stats = base + parts * kPart;
-        const int64_t mine = (int64_t)w.part * a.heads + head;
-        {
-            const __amdgpu_buffer_rsrc_t dst = make_rsrc(base + mine * kPart, kPart), st = make_rsrc(stats + mine * kStats, kStats);
+        const int orow_all = w.unit * kRowsOfUnit + orow, oquery = quotient(orow_all, a.ratio), oh = head * a.ratio + (orow_all - oquery * a.ratio);
+        if (answers && joins && oquery < w.s.n) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;        // a row that sees nothing: zeros
+            T *out = static_cast<T *>(a.out.p) + (int64_t)(w.s.first + oquery) * a.out.token_stride + (int64_t)oh * a.out.head_stride + d0;
 #pragma unroll
             for (int e = 0; e < kOut; e += 4) {
-                const intx4 v = {__float_as_int(x[e]), __float_as_int(x[e + 1]), __float_as_int(x[e + 2]), __float_as_int(x[e + 3])};
-                __builtin_amdgcn_raw_buffer_store_b128(v, dst, (orow * D + d0 + e) * 4, 0, kAuxDeviceScope);
+                if constexpr (F32) {
+                    *reinterpret_cast<floatx4 *>(out + e) = floatx4{x[e] * inv, x[e + 1] * inv, x[e + 2] * inv, x[e + 3] * inv};
+                } else {
+                    bf16x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(x[e + i] * inv);
+                    *reinterpret_cast<bf16x4 *>(out + e) = v;
+                }
             }
-            const intx2 v = {__float_as_int(m), __float_as_int(l)};
-            if ((tid & 15) == 0) __builtin_amdgcn_raw_buffer_store_b64(v, st, orow * 8, 0, kAuxDeviceScope);
+            if (a.lse != nullptr && d0 == 0)
+                a.lse[(int64_t)(w.s.first + oquery) * ((int64_t)a.heads * a.ratio) + oh] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
         }
-        wait_all_and_barrier();
-        uint32_t *counter = a.counters + (int64_t)w.counter * a.heads + head;
-        if (tid == 0) {
-            const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = before == (uint32_t)(w.chunks - 1) ? 1u : 0u;
-            if (s_last != 0u) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (s_last == 0u) return;
-        m = -3.0e38f; l = 0.0f;
-#pragma unroll
-        for (int e = 0; e < kOut; ++e) x[e] = 0.0f;
-        for (int k = 0; k < w.chunks; ++k) {
-            const int64_t from = (int64_t)(w.part - w.chunk + k) * a.heads + head;
-            const __amdgpu_buffer_rsrc_t src = make_rsrc(base + from * kPart, kPart), st = make_rsrc(stats + from * kStats, kStats);
-            const intx2 ml = __builtin_amdgcn_raw_buffer_load_b64(st, orow * 8, 0, kAuxDeviceScope);
-            intx4 v[kOut / 4];
-#pragma unroll
-            for (int e = 0; e < kOut; e += 4) v[e / 4] = __builtin_amdgcn_raw_buffer_load_b128(src, (orow * D + d0 + e) * 4, 0, kAuxDeviceScope);
-            const float next = fmaxf(m, __int_as_float(ml[0])), f = exp2_of(m - next), g = exp2_of(__int_as_float(ml[0]) - next);
-            m = next;
-            l = __builtin_fmaf(__int_as_float(ml[1]), g, l * f);
-#pragma unroll
-            for (int e = 0; e < kOut; ++e) x[e] = __builtin_fmaf(__int_as_float(v[e / 4][e % 4]), g, x[e] * f);
-        }
+        __syncthreads();                                          // the sums have been read: the rings may fill again
     }
-    const int orow_all = w.unit * kRowsOfUnit + orow, oquery = orow_all / a.ratio, oh = head * a.ratio + (orow_all - oquery * a.ratio);
-    if (oquery >= w.s.n) return;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;            // a row that sees nothing: zeros
-    T *out = static_cast<T *>(a.out.p) + (int64_t)(w.s.first + oquery) * a.out.token_stride + (int64_t)oh * a.out.head_stride + d0;
-#pragma unroll
-    for (int e = 0; e < kOut; e += 4) {
-        if constexpr (F32) {
-            *reinterpret_cast<floatx4 *>(out + e) = floatx4{x[e] * inv, x[e + 1] * inv, x[e + 2] * inv, x[e + 3] * inv};
-        } else {
-            bf16x4 v;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(x[e + i] * inv);
-            *reinterpret_cast<bf16x4 *>(out + e) = v;
-        }
-    }
-    if (a.lse != nullptr && (tid & 15) == 0)
-        a.lse[(int64_t)(w.s.first + oquery) * ((int64_t)a.heads * a.ratio) + oh] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
-// chunks that the division aims at, for every head of the cache
-int chunks_aimed_at(const KvShape &s) { return (kWorkgroups + s.heads - 1) / s.heads; }
+// shares of the work of a head of the cache
+int shares_of(const KvShape &s) { return (kResident + s.heads - 1) / s.heads; }
 
 // Sequences with more rows than this go to the kernel that rebuilds keys and values (bf16).
 constexpr int kStreamedRows = 64;
@@ -349,18 +416,23 @@ struct WsLayout { Scratch streamed, prompts; };
 WsLayout ws_layout(const KvShape &s, const KvBatch &b, int q_heads)
 {
     WsLayout l;
-    l.streamed = scratch_of(0, chunks_aimed_at(s), s.heads, kRowsOfUnit, s.head_dim);
+    l.streamed = scratch_of(0, shares_of(s), s.heads, kRowsOfUnit, s.head_dim);
     l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
     if (s.act_bf16 && (int64_t)b.max_new * (q_heads / s.heads) > kStreamedRows)
         l.prompts = scratch_of((l.streamed.end + 255) / 256 * 256, prompt_target(s), s.heads, prompt_unit_rows(s), s.head_dim);
     return l;
 }
 
+template <int NS, int SG, bool F32> void launch_t(const AttendArgs &a, hipStream_t st)
+{
+    constexpr int D = 32 * NS, kWaves = waves_of(D), rings = kWaves * depth_of(D) * KvRecord<NS, SG>::kBytes, sums = kWaves * kRowsOfUnit * (D + 4) * 4, smem = rings > sums ? rings : sums;
+    allow_lds(reinterpret_cast<const void *>(&k_kv_attend<NS, SG, F32>), smem);
+    k_kv_attend<NS, SG, F32><<<dim3((unsigned)a.slots * (unsigned)a.heads), kWaves * 64, smem, st>>>(a);
+}
 template <int NS, int SG> void launch(const KvShape &s, const AttendArgs &a, hipStream_t st)
 {
-    const dim3 grid((unsigned)a.slots * (unsigned)a.heads);
-    if (s.act_bf16) k_kv_attend<NS, SG, false><<<grid, kWaves * 64, 0, st>>>(a);
-    else k_kv_attend<NS, SG, true><<<grid, kWaves * 64, 0, st>>>(a);
+    if (s.act_bf16) launch_t<NS, SG, false>(a, st);
+    else launch_t<NS, SG, true>(a, st);
 }
 
 }  // namespace
@@ -388,12 +460,9 @@ void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &t, con
     }
     a.from_rows = 1; a.to_rows = prompts ? kStreamedRows + 1 : INT32_MAX;
     scratch(l.streamed);
-    a.unit_rows = kRowsOfUnit;
+    a.unit_bits = __builtin_ctz(kRowsOfUnit);
     a.fewest = kFewestRecords;
-    a.target = chunks_aimed_at(s);
-    KvBatch few = b;
-    if (prompts) few.max_new = kStreamedRows / a.ratio;
-    a.slots = a.target + units_at_most(few, a.ratio, kRowsOfUnit);
+    a.slots = shares_of(s);
     const int sg = s.group / 32;
     switch (s.head_dim) {
     case 64: if (sg == 1) launch<2, 1>(s, a, st); else launch<2, 2>(s, a, st); break;

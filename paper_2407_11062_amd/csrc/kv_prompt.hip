@@ -6,8 +6,6 @@
 // Keys and values are halved on their way (m + s c may pass 65504 by a rounding), and held to 11 bits; scores, softmax and sums are binary32, p is binary16.
 #include "kv_work.h"
 
-#include <atomic>
-
 namespace eqat {
 namespace {
 
@@ -366,12 +364,7 @@ template <int NS, int SG> __global__ __launch_bounds__(kPromptWaves * 64, 2) voi
 template <int NS, int SG> void launch(const AttendArgs &a, hipStream_t st)
 {
     constexpr int smem = 2 * 2 * kTile * 32 * NS * 2;
-    static std::atomic<uint64_t> allowed{0};                  // more than the default of LDS has to be asked for once on every device
-    int dev = 0;
-    if (hipGetDevice(&dev) == hipSuccess && dev < 64 && !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_kv_prompt<NS, SG>), hipFuncAttributeMaxDynamicSharedMemorySize, smem) == hipSuccess)
-            allowed.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
-    }
+    allow_lds(reinterpret_cast<const void *>(&k_kv_prompt<NS, SG>), smem);
     k_kv_prompt<NS, SG><<<dim3((unsigned)a.slots * (unsigned)a.heads), kPromptWaves * 64, smem, st>>>(a);
 }
 
@@ -382,10 +375,11 @@ int prompt_unit_rows(const KvShape &s) { return kPromptWaves * columns_of(s.head
 
 void launch_kv_prompt(const KvShape &s, AttendArgs a, hipStream_t st)
 {
-    a.unit_rows = prompt_unit_rows(s);
+    const int rows = prompt_unit_rows(s);
+    a.unit_bits = __builtin_ctz(rows);
     a.fewest = 8;
     a.target = prompt_target(s);
-    a.slots = a.target + units_at_most(a.b, a.ratio, a.unit_rows);
+    a.slots = a.target + units_at_most(a.b, a.ratio, rows);
     const int sg = s.group / 32;
     switch (s.head_dim) {
     case 64: if (sg == 1) launch<2, 1>(a, st); else launch<2, 2>(a, st); break;

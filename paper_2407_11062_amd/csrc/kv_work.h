@@ -3,17 +3,20 @@
 #include "gemm_tiles.h"
 #include "kv.h"
 
+#include <mutex>
+#include <vector>
+
 namespace eqat {
 
 struct AttendArgs {
     KvBatch b;
     KvRows q, out;
-    float *lse, *parts;                            // parts: [chunk][head][unit_rows][D] sums, then [chunk][head][unit_rows][2] maxima and totals
+    float *lse, *parts;                            // parts: [chunk][head][rows of a unit][D] sums, then [chunk][head][rows of a unit][2] maxima and totals
     uint32_t *counters;                            // [unit][head], zero before and after every launch
     const uint8_t *pool;
     int64_t pages;
     int heads, ratio, page_records, window, target, slots;
-    int unit_rows, fewest;                         // rows (query, head of the group) of a unit; records of a chunk at the least
+    int unit_bits, fewest;                         // log2 of the rows (query, head of the group) of a unit; records of a chunk or share at the least
     int from_rows, to_rows;                        // the launch takes the sequences with from_rows <= rows < to_rows
     bool causal;
     float scale;                                   // times log2(e)
@@ -48,7 +51,7 @@ __device__ __forceinline__ float chunks_sum(float v)
 
 __device__ __forceinline__ floatx4 mfma(const uintx4 &a, const half8 &b, const floatx4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), b, c, 0, 0, 0); }
 
-// How the work of a call is divided: a unit is up to unit_rows rows of a sequence (times every head of the cache), its records are cut into chunks of C, and a workgroup
+// How the work of a call is divided: a unit is up to 2^unit_bits rows of a sequence (times every head of the cache), its records are cut into chunks of C, and a workgroup
 // takes a chunk.  C follows from the lengths as they are on the device, so that the chunks of all sequences are about `target` in all, however their lengths differ.
 struct Work { int b, unit, chunk, chunks, first, last, part, counter; KvSeq s; bool any; };
 
@@ -57,61 +60,147 @@ __device__ __forceinline__ Extent extent_of(const AttendArgs &a, const KvSeq &s)
 {
     Extent e;
     const int rows = s.n * a.ratio;
-    e.units = rows >= a.from_rows && rows < a.to_rows ? (rows + a.unit_rows - 1) / a.unit_rows : 0;
+    e.units = rows >= a.from_rows && rows < a.to_rows ? (rows + (1 << a.unit_bits) - 1) >> a.unit_bits : 0;
     e.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) >> 5 : 0;
     e.hi = (s.len + 31) >> 5;
     return e;
 }
 
+// sums over the lanes up to and with this one (row shifts, then the rows' last lanes to the rows behind them)
+template <typename T> __device__ __forceinline__ T lane_sums(T x)
+{
+    auto from = [](T v, auto ctrl, auto rows) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xF, true)); };
+    x += from(x, IC<0x111>{}, IC<0xF>{}); x += from(x, IC<0x112>{}, IC<0xF>{}); x += from(x, IC<0x114>{}, IC<0xF>{}); x += from(x, IC<0x118>{}, IC<0xF>{});
+    x += from(x, IC<0x142>{}, IC<0xA>{}); x += from(x, IC<0x143>{}, IC<0xC>{});
+    return x;
+}
+
 __device__ __forceinline__ Work work_of(const AttendArgs &a, int slot)
 {
     const int lane = threadIdx.x & 63, page_tokens = a.page_records * kKvRecord;
-    uint64_t records = 0;
-    for (int base = 0; base < a.b.sequences; base += 64) {
+    KvSeq s{};
+    Extent e{};
+    auto look = [&](int base) {
         const int b = base + lane;
-        if (b < a.b.sequences) {
-            const Extent e = extent_of(a, kv_seq(a.b, page_tokens, b));
-            records += (uint64_t)e.units * (uint64_t)(e.hi - e.lo);
-        }
-    }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) records += __shfl_xor(records, d);
-    const int C = max((int)((records + a.target - 1) / a.target), a.fewest);
+        s = KvSeq{}; e = Extent{};
+        if (b < a.b.sequences) { s = kv_seq(a.b, page_tokens, b); e = extent_of(a, s); }
+    };
+    float records = 0.0f;                                // in all, up to rounding: every workgroup adds them up in the same order
+    for (int base = 0; base < a.b.sequences; base += 64) { look(base); records += (float)e.units * (float)(e.hi - e.lo); }
+    records = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(records)), 63));
+    // at least records / target whatever the rounding: the room for parts depends on it
+    const int C = max((int)fminf(records / (float)a.target * 1.00001f, 1.0e9f) + 1, a.fewest);
     Work w{};
     int before = 0, parts = 0, counters = 0;
-    bool found = false;
     for (int base = 0; base < a.b.sequences; base += 64) {
-        const int b = base + lane;
-        KvSeq s{};
-        Extent e{};
-        if (b < a.b.sequences) { s = kv_seq(a.b, page_tokens, b); e = extent_of(a, s); }
+        if (a.b.sequences > 64) look(base);
         const int chunks = e.units > 0 ? max(1, (e.hi - e.lo + C - 1) / C) : 0, mine = e.units * chunks, cut = chunks > 1 ? e.units : 0;
-        int x = mine, y = cut * chunks, z = cut;         // inclusive sums over the lanes
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int xx = __shfl_up(x, d), yy = __shfl_up(y, d), zz = __shfl_up(z, d);
-            if (lane >= d) { x += xx; y += yy; z += zz; }
-        }
+        const int x = lane_sums(mine), y = lane_sums(cut * chunks), z = lane_sums(cut);
         const int at = slot - before - (x - mine);       // this slot within the sequence of the lane
         const uint64_t has = __ballot(at >= 0 && at < mine);
-        if (has != 0 && !found) {
+        if (has != 0) {
             const int src = __ffsll((unsigned long long)has) - 1;
-            found = true;
-            const int i = __shfl(at, src);
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
+            const int i = of(at);
+            w.any = true;
             w.b = base + src;
-            w.chunks = __shfl(chunks, src);
-            w.unit = i / w.chunks;
+            w.chunks = of(chunks);
+            w.unit = w.chunks == 1 ? i : i / w.chunks;
             w.chunk = i - w.unit * w.chunks;
-            w.s.first = __shfl(s.first, src); w.s.n = __shfl(s.n, src); w.s.len = __shfl(s.len, src);
-            const int lo = __shfl(e.lo, src), hi = __shfl(e.hi, src);
-            w.first = lo + w.chunk * C;
-            w.last = min(hi, w.first + C);
-            w.part = parts + __shfl(y - cut * chunks, src) + i;
-            w.counter = counters + __shfl(z - cut, src) + w.unit;
+            w.s.first = of(s.first); w.s.n = of(s.n); w.s.len = of(s.len);
+            w.first = of(e.lo) + w.chunk * C;
+            w.last = min(of(e.hi), w.first + C);
+            w.part = parts + of(y - cut * chunks) + i;
+            w.counter = counters + of(z - cut) + w.unit;
         }
-        before += __shfl(x, 63); parts += __shfl(y, 63); counters += __shfl(z, 63);
+        before += __builtin_amdgcn_readlane(x, 63); parts += __builtin_amdgcn_readlane(y, 63); counters += __builtin_amdgcn_readlane(z, 63);
     }
-    w.any = found && before <= a.slots;                  // more than the host was told of: nothing is computed
+    w.any = w.any && before <= a.slots;                  // more than the host was told of: nothing is computed
+    return w;
+}
+
+// x / d for 0 <= x, 0 < d: by a reciprocal, put right, where x is small (the compiler's own is four times as long, and these stand in a row before anything is fetched)
+__device__ __forceinline__ int quotient(int x, int d)
+{
+    if (x >= 1 << 22) return x / d;
+    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));           // off by one at the most
+    const int r = x - q * d;
+    return q + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0);
+}
+
+// The other division, for rows few enough that what counts is the bytes of the cache: the records of all units, one after the other, in equal shares, one for each of
+// the workgroups that are resident.  A share may end within a unit and begin in the next; each stretch of a unit costs a beginning and a join with the others.  Where
+// shares that end with the units (`whole`: units take a whole number of them) are not more than kSpare records larger, it is those.
+constexpr int kSpare = 20;
+struct Share { int first, last, size; bool whole; };
+struct Segment { int b, unit, rec, rec_to, unit_from, unit_to, to; KvSeq s; bool any; };      // a stretch of one unit: records rec .. rec_to - 1; the unit's whole extent within the row of work
+struct Lane { KvSeq s; Extent e; };                          // the sequence of a lane
+
+__device__ __forceinline__ Lane lane_of(const AttendArgs &a, int base)
+{
+    Lane l{};
+    const int b = base + (threadIdx.x & 63);
+    if (b < a.b.sequences) { l.s = kv_seq(a.b, a.page_records * kKvRecord, b); l.e = extent_of(a, l.s); }
+    return l;
+}
+
+// l: the lane's sequence of the first 64
+__device__ __forceinline__ Share share_of(const AttendArgs &a, int slot, Lane l)
+{
+    int records = 0;
+    float about = 0.0f;
+    for (int base = 0; base < a.b.sequences; base += 64) {
+        if (base > 0) l = lane_of(a, base);
+        records += l.e.units * max(1, l.e.hi - l.e.lo);
+        about += (float)l.e.units * (float)max(1, l.e.hi - l.e.lo);
+    }
+    records = __builtin_amdgcn_readlane(lane_sums(records), 63);
+    about = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(about)), 63));
+    if (records == 0 || about > 2.1e9f) return Share{0, 0, 1, true};          // (more than the host was told of: nothing is computed)
+    const int size = max(quotient(records + a.slots - 1, a.slots), a.fewest);
+    for (int larger = size; larger <= size + kSpare; larger += max(1, larger >> 4)) {
+        int shares = 0;
+        for (int base = 0; base < a.b.sequences; base += 64) {
+            if (a.b.sequences > 64) l = lane_of(a, base);
+            shares += l.e.units * max(1, quotient(l.e.hi - l.e.lo + larger - 1, larger));
+        }
+        shares = __builtin_amdgcn_readlane(lane_sums(shares), 63);
+        if (shares <= a.slots) return slot < shares ? Share{slot * larger, (slot + 1) * larger, larger, true} : Share{0, 0, 1, true};
+    }
+    return Share{(int)min((int64_t)slot * size, (int64_t)records), (int)min((int64_t)(slot + 1) * size, (int64_t)records), size, false};
+}
+
+__device__ __forceinline__ Segment segment_of(const AttendArgs &a, const Share &share, int pos, Lane l)
+{
+    Segment w{};
+    int before = 0;
+    for (int base = 0; base < a.b.sequences && !w.any; base += 64) {
+        if (a.b.sequences > 64) l = lane_of(a, base);
+        const int recs = l.e.hi - l.e.lo, shares = share.whole ? max(1, quotient(recs + share.size - 1, share.size)) : 1, each = share.whole ? shares * share.size : max(1, recs);
+        const int mine = l.e.units * each, x = lane_sums(mine), at = pos - before - (x - mine);
+        const uint64_t has = __ballot(at >= 0 && at < mine);
+        if (has != 0) {
+            const int src = __ffsll((unsigned long long)has) - 1;
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
+            const int i = of(at), n = of(each), lo = of(l.e.lo), hi = of(l.e.hi);
+            w.any = true;
+            w.b = base + src;
+            w.unit = i < n ? 0 : quotient(i, n);
+            w.s.first = of(l.s.first); w.s.n = of(l.s.n); w.s.len = of(l.s.len);
+            w.unit_from = pos - (i - w.unit * n);
+            w.unit_to = w.unit_from + n;
+            w.to = min(share.last, w.unit_to);
+            if (share.whole) {                               // a unit's shares are alike
+                const int parts = of(shares), k = quotient(i - w.unit * n, share.size), each_part = quotient(hi - lo + parts - 1, parts);
+                w.rec = lo + k * each_part;
+                w.rec_to = min(hi, w.rec + each_part);
+            } else {
+                w.rec = lo + (i - w.unit * n);
+                w.rec_to = min(hi, w.rec + (w.to - pos));     // a sequence that holds nothing has one record to itself that is none
+            }
+        }
+        before += __builtin_amdgcn_readlane(x, 63);
+    }
     return w;
 }
 
@@ -133,6 +222,20 @@ Scratch scratch_of(size_t at, int target, int heads, int unit_rows, int head_dim
     l.parts = at + (chunks * 4 + 255) / 256 * 256;
     l.end = l.parts + 2 * chunks * (size_t)unit_rows * (size_t)(head_dim * 4 + 8);
     return l;
+}
+
+// more LDS than the default has to be asked for, once on every device
+void allow_lds(const void *kernel, int bytes)
+{
+    struct Asked { const void *kernel; int dev; };
+    static std::mutex mutex;
+    static std::vector<Asked> asked;
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return;
+    std::lock_guard<std::mutex> lock(mutex);
+    for (const Asked &x : asked)
+        if (x.kernel == kernel && x.dev == dev) return;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) asked.push_back(Asked{kernel, dev});
 }
 
 }  // namespace
