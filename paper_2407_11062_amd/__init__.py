@@ -474,22 +474,38 @@ class KvBatch:
         self.ref = ctypes.byref(self.desc)
 
 
+@functools.lru_cache(maxsize=1024)
+def _kv_strides(shape, stride, tokens, heads, head_dim):
+    """{token, head} strides of a [tokens, heads, head_dim] tensor whose heads are contiguous, in memory: (address, the array itself).  The cache is by value."""
+    if tuple(shape) != (tokens, heads, head_dim):
+        raise ValueError(f"expected [{tokens}, {heads}, {head_dim}], got {list(shape)}")
+    if stride[2] != 1:
+        raise ValueError("the elements of a head must be contiguous")
+    both = (ctypes.c_int64 * 2)(stride[0], stride[1])
+    return ctypes.addressof(both), both
+
+
+@functools.lru_cache(maxsize=1024)
+def _kv_attn_ref(q_heads, causal, window, scale):
+    return ctypes.byref(KvAttn(q_heads, causal, window, scale))
+
+
 def _kv_rows(cache, batch, t, heads):
-    """(pointer, {token, head} strides) of a [tokens, heads, head_dim] tensor whose heads are contiguous"""
+    """(pointer, (address of its strides, their array)) of a [tokens, heads, head_dim] tensor"""
     if t is None:
-        return None, None
-    if t.dtype != cache.dtype or tuple(t.shape) != (batch.tokens, heads, cache.head_dim):
-        raise ValueError(f"expected {cache.dtype} [{batch.tokens}, {heads}, {cache.head_dim}], got {t.dtype} {list(t.shape)}")
-    ts, hs, es = t.stride()
-    if not t.is_cuda or es != 1:
-        raise ValueError("the elements of a head must be contiguous, on the device")
-    return t.data_ptr(), (ctypes.c_int64 * 2)(ts, hs)
+        return None, _NO_STRIDES
+    if t.dtype != cache.dtype or not t.is_cuda:
+        raise ValueError(f"expected a {cache.dtype} device tensor, got {t.dtype} on {t.device}")
+    return t.data_ptr(), _kv_strides(t.shape, t.stride(), batch.tokens, heads, cache.head_dim)
+
+
+_NO_STRIDES = (None, None)
 
 
 def eqat_kv_write(cache: KvCache, batch: KvBatch, k, v):
     """The newest tokens' keys and values [tokens, heads, head_dim] (any token and head strides) into the cache."""
     (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
-    _check("eqat_kv_write", lib().eqat_kv_write(cache.ref, batch.ref, kp, ks, vp, vs, cache.pool.data_ptr(), _stream()))
+    _check("eqat_kv_write", lib().eqat_kv_write(cache.ref, batch.ref, kp, ks[0], vp, vs[0], cache.pool.data_ptr(), _stream()))
 
 
 def eqat_kv_read(cache: KvCache, batch: KvBatch, k=None, v=None, want=("k", "v")):
@@ -497,7 +513,7 @@ def eqat_kv_read(cache: KvCache, batch: KvBatch, k=None, v=None, want=("k", "v")
     if k is None and v is None:
         k, v = (torch.empty((batch.tokens, cache.heads, cache.head_dim), dtype=cache.dtype, device=cache.pool.device) if name in want else None for name in ("k", "v"))
     (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
-    _check("eqat_kv_read", lib().eqat_kv_read(cache.ref, batch.ref, kp, ks, vp, vs, cache.pool.data_ptr(), _stream()))
+    _check("eqat_kv_read", lib().eqat_kv_read(cache.ref, batch.ref, kp, ks[0], vp, vs[0], cache.pool.data_ptr(), _stream()))
     return k, v
 
 
@@ -515,8 +531,8 @@ def eqat_kv_attention(cache: KvCache, batch: KvBatch, q, scale=0.0, causal=True,
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (batch.tokens, q_heads)):
         raise ValueError("lse is fp32 [tokens, q_heads]")
     ws = kv_workspace(cache, batch, q_heads) if ws is None else ws
-    a = KvAttn(q_heads, 1 if causal else 0, int(window), float(scale))
-    _check("eqat_kv_attention", lib().eqat_kv_attention(cache.ref, batch.ref, ctypes.byref(a), qp, qs, op, os_, _p(lse), cache.pool.data_ptr(),
+    a = _kv_attn_ref(q_heads, 1 if causal else 0, int(window), float(scale))
+    _check("eqat_kv_attention", lib().eqat_kv_attention(cache.ref, batch.ref, a, qp, qs[0], op, os_[0], _p(lse), cache.pool.data_ptr(),
                                                         _p(ws), ws.numel(), _stream()))
     return out
 

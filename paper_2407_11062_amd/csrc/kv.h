@@ -74,20 +74,22 @@ __device__ __forceinline__ KvSeq kv_seq(const KvBatch &k, int page_tokens, int b
     return s;
 }
 
-// The sequence that row `t` of the call's tensors belongs to: the number of sequences that end at or before it.
-__device__ __forceinline__ int kv_seq_of(const KvBatch &k, int t)
+// sums over the lanes up to and with this one (row shifts, then the rows' last lanes to the rows behind them)
+template <typename T> __device__ __forceinline__ T lane_sums(T x)
 {
-    int b = 0;
-    if (k.sequences <= 64) {
-        for (int i = 1; i < k.sequences; ++i) b += k.starts[i] <= t ? 1 : 0;
-    } else {
-        int hi = k.sequences - 1;             // starts[b] <= t for the last such b
-        while (b < hi) {
-            const int mid = (b + hi + 1) >> 1;
-            if (k.starts[mid] <= t) b = mid; else hi = mid - 1;
-        }
-    }
-    return b;
+    auto from = [](T v, auto ctrl, auto rows) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xF, true)); };
+    x += from(x, IC<0x111>{}, IC<0xF>{}); x += from(x, IC<0x112>{}, IC<0xF>{}); x += from(x, IC<0x114>{}, IC<0xF>{}); x += from(x, IC<0x118>{}, IC<0xF>{});
+    x += from(x, IC<0x142>{}, IC<0xA>{}); x += from(x, IC<0x143>{}, IC<0xC>{});
+    return x;
+}
+
+// x / d for 0 <= x, 0 < d: by a reciprocal, put right, where x is small (the compiler's own is four times as long, and these stand in a row before anything is fetched)
+__device__ __forceinline__ int quotient(int x, int d)
+{
+    if (x >= 1 << 22) return x / d;
+    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));           // off by one at the most
+    const int r = x - q * d;
+    return q + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0);
 }
 
 }  // namespace eqat

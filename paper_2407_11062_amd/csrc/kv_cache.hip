@@ -1,47 +1,67 @@
 // Writing keys and values into the 4-bit cache, and reading them back.
 //
-// Both move bytes: a token and head of 128 elements is 512 bytes of bf16 and 136 (one group) to 160 (four) in the cache.  A row of 16 lanes takes one token and
-// head.  Of the key it takes eight neighbouring elements a lane, one word of the cache; of the value, two neighbouring elements of every 32, one half word of the
-// cache for every 64 (kv.h says why they stand there).
+// Both move bytes: a token and head of 128 elements is 512 bytes of bf16 and 136 (one group) to 160 (four) in the cache.  A wave takes the keys or the values of a record of 32 tokens and one
+// head, sixteen tokens at a time, four lanes to a token: lane c of them has the elements 32 j + 8 c .. + 7 of every j, which are one word of the cache each for a key, and for
+// a value eight half words (kv.h says where they stand).  A lane then stores a key's words of four j as they lie, 16 neighbouring bytes, and a group's least and
+// greatest element are found in a lane and two exchanges.  Half words of values go through LDS into the order of the record where all of it is written, and singly where not.
 #include "kv.h"
 
 namespace eqat {
 namespace {
 
+constexpr int kCacheWaves = 4;
+
 struct CacheArgs {
     KvBatch b;
     KvRows k, v;
     uint8_t *pool;
-    int64_t pages, rows;
+    int64_t pages;
     int heads, page_records;
 };
 
-// maximum over the LANES lanes around this one (a power of two, at most 16)
-template <int LANES> __device__ __forceinline__ float row_max(float v)
-{
-    if constexpr (LANES > 1) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true)));        // quad_perm 1 0 3 2
-    if constexpr (LANES > 2) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, true)));        // quad_perm 2 3 0 1
-    if constexpr (LANES > 4) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, true)));       // the half row mirrored
-    if constexpr (LANES > 8) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, true)));       // the row mirrored
-    return v;
-}
+// of the four lanes of a token; NaN wins (v_minimum3_f32, v_maximum3_f32)
+__device__ __forceinline__ float greater(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float least_of(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+template <int CTRL> __device__ __forceinline__ float of_quad(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ float quad_greatest(float v) { v = greater(v, of_quad<0xB1>(v)); return greater(v, of_quad<0x4E>(v)); }
+__device__ __forceinline__ float quad_least(float v) { v = least_of(v, of_quad<0xB1>(v)); return least_of(v, of_quad<0x4E>(v)); }
 
-// A group's step and least element, as they stand in the cache.  `odd` is 0, or NaN where an element is not finite: the whole group then stands as NaN,
-// as one with an element beyond binary16 does (so no step passes 131008 / 15, and what a kernel makes of codes and steps stays within binary16 or a rounding of it).
+// A group's step and least element, as they stand in the cache: NaN where an element is not finite or beyond binary16 (so no step passes 131008 / 15, and what a kernel
+// makes of codes and steps stays within binary16 or a rounding of it).
 struct Step { float s, m; uint32_t word; };
-__device__ __forceinline__ Step step_of(float least, float greatest, float odd)
+__device__ __forceinline__ Step step_of(float least, float greatest)
 {
     _Float16 m = (_Float16)least, s = (_Float16)fmaxf((greatest - least) / 15.0f, 0x1p-24f);
-    if (!(fabsf((float)m) + fabsf((float)(_Float16)greatest) + odd < __builtin_inff())) { m = (_Float16)__builtin_nanf(""); s = m; }
+    if (!(fabsf((float)m) + fabsf((float)(_Float16)greatest) < __builtin_inff())) { m = (_Float16)__builtin_nanf(""); s = m; }
     Step r;
     r.s = (float)s; r.m = (float)m;
     r.word = (uint32_t)__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, m) << 16;
     return r;
 }
-// round((x - m) / s) within 0 .. 15 (0 where that is NaN), of the correctly rounded quotient
-__device__ __forceinline__ uint32_t code_of(float x, const Step &t)
+
+// Codes round((x - m) / s) of a lane's eight elements, of the correctly rounded quotients, element e in bits sh(e).  A multiply-add that adds 1.5 2^23 rounds a product
+// to a whole number; with the reciprocal of s once 2^-21 too small and once as much too large the two numbers bracket the quotient's, and where they are the same they
+// are it.  Where any is not (ties and beside them) the lane divides.
+template <typename SH> __device__ __forceinline__ uint32_t codes_of(const float *x, const Step &t, SH sh)
 {
-    return (uint32_t)fminf(fmaxf(__builtin_rintf((x - t.m) / t.s), 0.0f), 15.0f);
+    constexpr float kWhole = 12582912.0f;
+    const float r = __builtin_amdgcn_rcpf(t.s), below = r * (1.0f - 0x1p-21f), above = r * (1.0f + 0x1p-21f);
+    uint32_t word = 0, whole = 0;
+    bool unsure = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float d = x[e] - t.m, a = __builtin_fmaf(d, below, kWhole), b = __builtin_fmaf(d, above, kWhole);
+        unsure |= !(a == b);
+        word += __float_as_uint(__builtin_amdgcn_fmed3f(a, kWhole, kWhole + 15.0f)) << sh(e);
+        whole += 0x4B400000u << sh(e);
+    }
+    word -= whole;
+    if (unsure) {
+        word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) word |= (uint32_t)fminf(fmaxf(__builtin_rintf((x[e] - t.m) / t.s), 0.0f), 15.0f) << sh(e);          // (NaN: 0)
+    }
+    return word;
 }
 
 template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8])
@@ -70,170 +90,229 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float (
         *reinterpret_cast<floatx4 *>(p) = a; *reinterpret_cast<floatx4 *>(p + 4) = b;
     }
 }
-template <typename T> struct Two { T v[2]; };
 
-// Where the token of row `row` of the launch stands.  valid: it has a position, on a page of the pool.
-struct Place { bool valid; int head; int64_t token; int slot; int64_t record; };
-__device__ __forceinline__ Place place_of(const CacheArgs &a, int64_t row)
+// The record of a wave: the `index`-th of those that the newest tokens of the sequences touch, and one head.
+struct Place { bool any, there, full; int first, from, to; uint8_t *record; };         // row of position 0 (so row = first + position); positions from .. to - 1 of the record are the call's
+__device__ __forceinline__ Place place_of(const CacheArgs &a, int index, int head, int64_t record_bytes)
 {
     Place p{};
-    p.token = row / a.heads;
-    p.head = (int)(row - p.token * a.heads);
-    if (row >= a.rows) return p;
-    const int b = kv_seq_of(a.b, (int)p.token);
-    const KvSeq s = kv_seq(a.b, a.page_records * kKvRecord, b);
-    const int i = (int)p.token - s.first, pos = s.len - s.n + i;
-    if (i < 0 || i >= s.n || pos < 0) return p;
-    const int rec = pos >> 5, page_of_seq = rec / a.page_records;
-    const int page = a.b.table[(int64_t)b * a.b.table_stride + page_of_seq];
-    p.slot = pos & 31;
-    p.valid = page >= 0 && page < a.pages;
-    p.record = ((int64_t)page * a.heads + p.head) * a.page_records + (rec - page_of_seq * a.page_records);
+    int before = 0;
+    for (int base = 0; base < a.b.sequences && !p.any; base += 64) {
+        const int b = base + (threadIdx.x & 63);
+        KvSeq s{};
+        if (b < a.b.sequences) s = kv_seq(a.b, a.page_records * kKvRecord, b);
+        const int rec0 = max(0, s.len - s.n) >> 5, mine = s.n > 0 && s.len > 0 ? ((s.len - 1) >> 5) - rec0 + 1 : 0, x = lane_sums(mine), at = index - before - (x - mine);
+        const uint64_t has = __ballot(at >= 0 && at < mine);
+        if (has != 0) {
+            const int src = __ffsll((unsigned long long)has) - 1;
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
+            const int rec = of(rec0) + of(at), len = of(s.len), n = of(s.n), of_seq = quotient(rec, a.page_records);
+            const int page = __builtin_amdgcn_readfirstlane(a.b.table[(int64_t)(base + src) * a.b.table_stride + of_seq]);
+            p.any = true;
+            p.first = of(s.first) - (len - n);
+            p.from = max(max(rec * kKvRecord, len - n), 0);
+            p.to = min(rec * kKvRecord + kKvRecord, len);
+            p.full = p.to - p.from == kKvRecord;
+            p.there = page >= 0 && page < a.pages;
+            p.record = a.pool + (((int64_t)(p.there ? page : 0) * a.heads + head) * a.page_records + (rec - of_seq * a.page_records)) * record_bytes;
+        }
+        before += __builtin_amdgcn_readlane(x, 63);
+    }
     return p;
 }
 
-// byte of key word (step j, chunk c) and of value half (products 4 a ..) of a token
-template <int NS> __device__ __forceinline__ uint32_t key_at(int slot, int j, int c)
-{
-    const int w = (slot >> 4) * NS + j;
-    return (uint32_t)((w >> 2) * 1024 + (c * 16 + (slot & 15)) * 16 + (w & 3) * 4);
-}
+// half word of a value: token slot, products 4 a ..
 __device__ __forceinline__ uint32_t value_at(int slot, int a, int r)
 {
     return (uint32_t)(a * 1024 + (((slot & 15) >> 2) * 16 + r) * 16 + ((slot >> 4) * 2 + ((slot & 3) >> 1)) * 4 + (slot & 1) * 2);
 }
+// word of a key: tokens 16 h + t, of lane c of the token; the NS words of it from j = 0 on are neighbours in pieces of four (two, where NS = 2)
+template <int NS> __device__ __forceinline__ uint32_t key_at(int h, int t, int c, int j)
+{
+    const int w = h * NS + j;
+    return (uint32_t)((w >> 2) * 1024 + (c * 16 + t) * 16 + (w & 3) * 4);
+}
 
-template <int NS, int SG, typename T> __global__ __launch_bounds__(256) void k_kv_write(const CacheArgs a)
+// the lanes of a wave see each other's writes to LDS behind this
+__device__ __forceinline__ void wave_meets() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+// the elements of the lane's token `pos`, zeros where it is none of the call's
+template <int NS, typename T> __device__ __forceinline__ void load_token(const KvRows &rows, const Place &at, int pos, int head, int c, float (&x)[NS][8])
+{
+    if (pos >= at.from && pos < at.to) {
+        const T *p = static_cast<const T *>(rows.p) + (int64_t)(at.first + pos) * rows.token_stride + head * rows.head_stride + 8 * c;
+#pragma unroll
+        for (int j = 0; j < NS; ++j) load8(p + 32 * j, x[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[j][e] = 0.0f;
+    }
+}
+
+template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves * 64) void k_kv_write(const CacheArgs a)
 {
     using R = KvRecord<NS, SG>;
-    const int i = threadIdx.x & 15;
-    const Place at = place_of(a, (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4));
-    if (!at.valid) return;
-    uint8_t *rec = a.pool + at.record * R::kBytes;
-    const T *key = static_cast<const T *>(a.k.p) + at.token * a.k.token_stride + at.head * a.k.head_stride;
-    const T *value = static_cast<const T *>(a.v.p) + at.token * a.v.token_stride + at.head * a.v.head_stride;
-    constexpr int kWords = (NS + 3) / 4;               // words of the key that a lane takes: i, i + 16
-    float x[kWords][8], y[NS][2];
-    if (i < 4 * NS) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kCacheWaves / 2][16 * R::D];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, t = lane >> 2, c = lane & 3;
+    const int head = blockIdx.y * (kCacheWaves / 2) + (wave >> 1);
+    const bool values = (wave & 1) != 0;                      // this wave's part of the record
+    if (head >= a.heads) return;
+    const Place at = place_of(a, blockIdx.x, head, R::kBytes);
+    if (!at.any || !at.there) return;
+    const KvRows rows = values ? a.v : a.k;
+    const int token0 = (at.to - 1) & ~(kKvRecord - 1);
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) load8(key + (w * 16 + i) * 8, x[w]);
-    }
+    for (int h = 0; h < 2; ++h) {
+        const int pos = token0 + h * 16 + t;
+        const bool is = pos >= at.from && pos < at.to;
+        if (!__any(is)) continue;
+        float x[NS][8];
+        load_token<NS, T>(rows, at, pos, head, c, x);
+        Step steps[R::G];
 #pragma unroll
-    for (int j = 0; j < NS; ++j) {
-        const Two<T> t = *reinterpret_cast<const Two<T> *>(value + 32 * j + 2 * i);
-        y[j][0] = (float)t.v[0]; y[j][1] = (float)t.v[1];
-    }
-    if (i < 4 * NS) {
-        float lo[kWords], hi[kWords], odd[kWords];
-        constexpr int kLanes = SG < 4 ? 4 * SG : 16;   // lanes of a group
+        for (int g = 0; g < R::G; ++g) {
+            float lo = x[g * SG][0], hi = lo;
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-            float l = x[w][0], h = x[w][0], o = 0.0f;
+            for (int j = g * SG; j < (g + 1) * SG; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { l = fminf(l, x[w][e]); h = fmaxf(h, x[w][e]); o += x[w][e] * 0.0f; }
-            lo[w] = -row_max<kLanes>(-l); hi[w] = row_max<kLanes>(h); odd[w] = row_max<kLanes>(o != o ? 1.0f : 0.0f);
+                for (int e = 0; e < 8; ++e) { lo = least_of(lo, x[j][e]); hi = greater(hi, x[j][e]); }
+            steps[g] = step_of(quad_least(lo), quad_greatest(hi));
+            if (is && c == 0) *reinterpret_cast<uint32_t *>(at.record + (values ? R::kValueSteps : R::kKeySteps) + g * 128 + (h * 16 + t) * 4) = steps[g].word;
         }
-        if constexpr (SG == 8) {
-            lo[0] = lo[1] = fminf(lo[0], lo[1]); hi[0] = hi[1] = fmaxf(hi[0], hi[1]); odd[0] = odd[1] = fmaxf(odd[0], odd[1]);
-        }
+        if (!values) {
+            uint32_t words[NS];
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-            const Step t = step_of(lo[w], hi[w], odd[w] != 0.0f ? __builtin_nanf("") : 0.0f);
-            uint32_t word = 0;
+            for (int j = 0; j < NS; ++j) words[j] = codes_of(x[j], steps[j / SG], [](int e) { return 16 * (e & 1) + 4 * (e >> 1); });
+            if (is) {
+                uint8_t *to = at.record + R::kKeys;
+                if constexpr (NS == 2) *reinterpret_cast<uintx2 *>(to + key_at<NS>(h, t, c, 0)) = uintx2{words[0], words[1]};
+                else
 #pragma unroll
-            for (int e = 0; e < 8; ++e) word |= code_of(x[w][e], t) << (16 * (e & 1) + 4 * (e >> 1));
-            const int j = (w * 16 + i) >> 2;
-            *reinterpret_cast<uint32_t *>(rec + R::kKeys + key_at<NS>(at.slot, j, i & 3)) = word;
-            if ((w * 16 + i) % (4 * SG) == 0) *reinterpret_cast<uint32_t *>(rec + R::kKeySteps + (j / SG) * 128 + at.slot * 4) = t.word;
+                    for (int j = 0; j < NS; j += 4) *reinterpret_cast<uintx4 *>(to + key_at<NS>(h, t, c, j)) = uintx4{words[j], words[j + 1], words[j + 2], words[j + 3]};
+            }
+        } else {
+            uint32_t pairs[NS];                               // byte i: the elements 2 i and 2 i + 1
+#pragma unroll
+            for (int j = 0; j < NS; ++j) pairs[j] = codes_of(x[j], steps[j / SG], [](int e) { return 4 * e; });
+            uint8_t *to = at.full ? lds[wave >> 1] : at.record + R::kValues;
+#pragma unroll
+            for (int n = 0; n < NS / 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                 // row 4 c + i of products 4 n ..: a pair of j = 2 n and one of 2 n + 1
+                    const uint32_t half = (pairs[2 * n] >> (8 * i) & 0xFFu) | (pairs[2 * n + 1] >> (8 * i) & 0xFFu) << 8;
+                    if (is) *reinterpret_cast<uint16_t *>(to + value_at(h * 16 + t, n, 4 * c + i)) = (uint16_t)half;
+                }
         }
     }
-    uint32_t half[NS / 2] = {};
+    if (values && at.full) {
+        wave_meets();
 #pragma unroll
-    for (int g = 0; g < R::G; ++g) {
-        float l = y[g * SG][0], h = l, o = 0.0f;
-#pragma unroll
-        for (int j = 0; j < SG; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) { l = fminf(l, y[g * SG + j][e]); h = fmaxf(h, y[g * SG + j][e]); o += y[g * SG + j][e] * 0.0f; }
-        const Step t = step_of(-row_max<16>(-l), row_max<16>(h), row_max<16>(o != o ? 1.0f : 0.0f) != 0.0f ? __builtin_nanf("") : 0.0f);
-#pragma unroll
-        for (int j = 0; j < SG; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) { const int n = 2 * (g * SG + j) + e; half[n >> 2] |= code_of(y[g * SG + j][e], t) << (4 * (n & 3)); }
-        if (i == 0) *reinterpret_cast<uint32_t *>(rec + R::kValueSteps + g * 128 + at.slot * 4) = t.word;
+        for (int n = 0; n < NS / 2; ++n)
+            *reinterpret_cast<uintx4 *>(at.record + R::kValues + n * 1024 + lane * 16) = *reinterpret_cast<const uintx4 *>(lds[wave >> 1] + n * 1024 + lane * 16);
     }
-#pragma unroll
-    for (int n = 0; n < NS / 2; ++n) *reinterpret_cast<uint16_t *>(rec + R::kValues + value_at(at.slot, n, i)) = (uint16_t)half[n];
 }
 
 __device__ __forceinline__ float stands_for(uint32_t code, uint32_t step)
 {
-    const float s = (float)__builtin_bit_cast(_Float16, (uint16_t)step), m = (float)__builtin_bit_cast(_Float16, (uint16_t)(step >> 16));
-    return __builtin_fmaf(s, (float)code, m);
+    const half2v sm = __builtin_bit_cast(half2v, step);
+    return __builtin_fmaf((float)sm[0], (float)code, (float)sm[1]);
 }
 
-template <int NS, int SG, typename T> __global__ __launch_bounds__(256) void k_kv_read(const CacheArgs a)
+template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves * 64) void k_kv_read(const CacheArgs a)
 {
     using R = KvRecord<NS, SG>;
-    const int i = threadIdx.x & 15;
-    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    if (row >= a.rows) return;
-    const Place at = place_of(a, row);
-    const uint8_t *rec = a.pool + (at.valid ? at.record * R::kBytes : 0);
-    if (a.k.p != nullptr && i < 4 * NS) {
-        T *key = static_cast<T *>(a.k.p) + at.token * a.k.token_stride + at.head * a.k.head_stride;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kCacheWaves / 2][16 * R::D];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, t = lane >> 2, c = lane & 3;
+    const int head = blockIdx.y * (kCacheWaves / 2) + (wave >> 1);
+    const bool values = (wave & 1) != 0;                      // this wave's part of the record
+    const KvRows rows = values ? a.v : a.k;
+    if (head >= a.heads || rows.p == nullptr) return;
+    const Place at = place_of(a, blockIdx.x, head, R::kBytes);
+    if (!at.any) return;
+    const int token0 = (at.to - 1) & ~(kKvRecord - 1);
+    uint32_t steps[2][R::G], words[2][NS];                    // of a key
+    if (at.there) {
 #pragma unroll
-        for (int w = 0; w < (NS + 3) / 4; ++w) {
-            const int j = (w * 16 + i) >> 2;
-            float x[8] = {};
-            if (at.valid) {
-                const uint32_t word = *reinterpret_cast<const uint32_t *>(rec + R::kKeys + key_at<NS>(at.slot, j, i & 3));
-                const uint32_t step = *reinterpret_cast<const uint32_t *>(rec + R::kKeySteps + (j / SG) * 128 + at.slot * 4);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = stands_for((word >> (16 * (e & 1) + 4 * (e >> 1))) & 15u, step);
+            for (int g = 0; g < R::G; ++g) steps[h][g] = *reinterpret_cast<const uint32_t *>(at.record + (values ? R::kValueSteps : R::kKeySteps) + g * 128 + (h * 16 + t) * 4);
+        if (values) {
+            uintx4 v[NS / 2];
+#pragma unroll
+            for (int n = 0; n < NS / 2; ++n) v[n] = *reinterpret_cast<const uintx4 *>(at.record + R::kValues + n * 1024 + lane * 16);
+#pragma unroll
+            for (int n = 0; n < NS / 2; ++n) *reinterpret_cast<uintx4 *>(lds[wave >> 1] + n * 1024 + lane * 16) = v[n];
+            wave_meets();
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint8_t *from = at.record + R::kKeys;
+                if constexpr (NS == 2) { const uintx2 v = *reinterpret_cast<const uintx2 *>(from + key_at<NS>(h, t, c, 0)); words[h][0] = v[0]; words[h][1] = v[1]; }
+                else
+#pragma unroll
+                    for (int j = 0; j < NS; j += 4) {
+                        const uintx4 v = *reinterpret_cast<const uintx4 *>(from + key_at<NS>(h, t, c, j));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) words[h][j + i] = v[i];
+                    }
             }
-            store8(key + (w * 16 + i) * 8, x);
         }
     }
-    if (a.v.p != nullptr) {
-        T *value = static_cast<T *>(a.v.p) + at.token * a.v.token_stride + at.head * a.v.head_stride;
 #pragma unroll
-        for (int j = 0; j < NS; ++j) {
-            Two<T> t{};
-            if (at.valid) {
-                const uint32_t half = *reinterpret_cast<const uint16_t *>(rec + R::kValues + value_at(at.slot, j >> 1, i));
-                const uint32_t step = *reinterpret_cast<const uint32_t *>(rec + R::kValueSteps + (j / SG) * 128 + at.slot * 4);
+    for (int h = 0; h < 2; ++h) {
+        const int pos = token0 + h * 16 + t;
+        if (pos < at.from || pos >= at.to) continue;
+        T *to = static_cast<T *>(rows.p) + (int64_t)(at.first + pos) * rows.token_stride + head * rows.head_stride + 8 * c;
+        float x[NS][8] = {};
+        if (at.there && !values) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) t.v[e] = (T)stands_for((half >> (8 * (j & 1) + 4 * e)) & 15u, step);
-            }
-            *reinterpret_cast<Two<T> *>(value + 32 * j + 2 * i) = t;
+            for (int j = 0; j < NS; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] = stands_for((words[h][j] >> (16 * (e & 1) + 4 * (e >> 1))) & 15u, steps[h][j / SG]);
+        } else if (at.there) {
+#pragma unroll
+            for (int n = 0; n < NS / 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t half = *reinterpret_cast<const uint16_t *>(lds[wave >> 1] + value_at(h * 16 + t, n, 4 * c + i));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { const int j = 2 * n + (e >> 1); x[j][2 * i + (e & 1)] = stands_for((half >> (4 * e)) & 15u, steps[h][j / SG]); }
+                }
         }
+#pragma unroll
+        for (int j = 0; j < NS; ++j) store8(to + 32 * j, x[j]);
     }
 }
 
-template <int NS, int SG> void launch(const KvShape &s, const CacheArgs &a, bool write, hipStream_t st)
+template <int NS, int SG> void launch(const KvShape &s, const CacheArgs &a, int records, bool write, hipStream_t st)
 {
-    const dim3 grid((unsigned)((a.rows + 15) / 16));
+    const dim3 grid((unsigned)records, (unsigned)(s.heads + kCacheWaves / 2 - 1) / (kCacheWaves / 2));
     if (write) {
-        if (s.act_bf16) k_kv_write<NS, SG, bf16_t><<<grid, 256, 0, st>>>(a);
-        else k_kv_write<NS, SG, float><<<grid, 256, 0, st>>>(a);
+        if (s.act_bf16) k_kv_write<NS, SG, bf16_t><<<grid, kCacheWaves * 64, 0, st>>>(a);
+        else k_kv_write<NS, SG, float><<<grid, kCacheWaves * 64, 0, st>>>(a);
     } else {
-        if (s.act_bf16) k_kv_read<NS, SG, bf16_t><<<grid, 256, 0, st>>>(a);
-        else k_kv_read<NS, SG, float><<<grid, 256, 0, st>>>(a);
+        if (s.act_bf16) k_kv_read<NS, SG, bf16_t><<<grid, kCacheWaves * 64, 0, st>>>(a);
+        else k_kv_read<NS, SG, float><<<grid, kCacheWaves * 64, 0, st>>>(a);
     }
 }
 
 void launch_any(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, void *pool, bool write, hipStream_t st)
 {
-    const CacheArgs a{b, k, v, static_cast<uint8_t *>(pool), s.pages, b.tokens * s.heads, s.heads, s.page_records};
-    if (a.rows == 0) return;
+    const CacheArgs a{b, k, v, static_cast<uint8_t *>(pool), s.pages, s.heads, s.page_records};
+    // n newest tokens touch at most (n + 30) / 32 + 1 records
+    const int64_t each = (int64_t)b.sequences * (((int64_t)b.max_new + 30) / 32 + 1), all = b.tokens / 32 + 2 * (int64_t)b.sequences;
+    const int records = (int)(each < all ? each : all);
     const int sg = s.group / 32;
     switch (s.head_dim) {
-    case 64: if (sg == 1) launch<2, 1>(s, a, write, st); else launch<2, 2>(s, a, write, st); break;
-    case 128: if (sg == 1) launch<4, 1>(s, a, write, st); else if (sg == 2) launch<4, 2>(s, a, write, st); else launch<4, 4>(s, a, write, st); break;
+    case 64: if (sg == 1) launch<2, 1>(s, a, records, write, st); else launch<2, 2>(s, a, records, write, st); break;
+    case 128:
+        if (sg == 1) launch<4, 1>(s, a, records, write, st); else if (sg == 2) launch<4, 2>(s, a, records, write, st); else launch<4, 4>(s, a, records, write, st);
+        break;
     default:
-        if (sg == 1) launch<8, 1>(s, a, write, st); else if (sg == 2) launch<8, 2>(s, a, write, st);
-        else if (sg == 4) launch<8, 4>(s, a, write, st); else launch<8, 8>(s, a, write, st);
+        if (sg == 1) launch<8, 1>(s, a, records, write, st); else if (sg == 2) launch<8, 2>(s, a, records, write, st);
+        else if (sg == 4) launch<8, 4>(s, a, records, write, st); else launch<8, 8>(s, a, records, write, st);
     }
 }
 

@@ -66,15 +66,6 @@ __device__ __forceinline__ Extent extent_of(const AttendArgs &a, const KvSeq &s)
     return e;
 }
 
-// sums over the lanes up to and with this one (row shifts, then the rows' last lanes to the rows behind them)
-template <typename T> __device__ __forceinline__ T lane_sums(T x)
-{
-    auto from = [](T v, auto ctrl, auto rows) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xF, true)); };
-    x += from(x, IC<0x111>{}, IC<0xF>{}); x += from(x, IC<0x112>{}, IC<0xF>{}); x += from(x, IC<0x114>{}, IC<0xF>{}); x += from(x, IC<0x118>{}, IC<0xF>{});
-    x += from(x, IC<0x142>{}, IC<0xA>{}); x += from(x, IC<0x143>{}, IC<0xC>{});
-    return x;
-}
-
 __device__ __forceinline__ Work work_of(const AttendArgs &a, int slot)
 {
     const int lane = threadIdx.x & 63, page_tokens = a.page_records * kKvRecord;
@@ -117,15 +108,6 @@ __device__ __forceinline__ Work work_of(const AttendArgs &a, int slot)
     }
     w.any = w.any && before <= a.slots;                  // more than the host was told of: nothing is computed
     return w;
-}
-
-// x / d for 0 <= x, 0 < d: by a reciprocal, put right, where x is small (the compiler's own is four times as long, and these stand in a row before anything is fetched)
-__device__ __forceinline__ int quotient(int x, int d)
-{
-    if (x >= 1 << 22) return x / d;
-    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));           // off by one at the most
-    const int r = x - q * d;
-    return q + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0);
 }
 
 // The other division, for rows few enough that what counts is the bytes of the cache: the records of all units, one after the other, in equal shares, one for each of
