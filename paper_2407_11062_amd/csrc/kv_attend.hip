@@ -418,8 +418,10 @@ WsLayout ws_layout(const KvShape &s, const KvBatch &b, int q_heads)
     WsLayout l;
     l.streamed = scratch_of(0, shares_of(s), s.heads, kRowsOfUnit, s.head_dim);
     l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
-    if (s.act_bf16 && (int64_t)b.max_new * (q_heads / s.heads) > kStreamedRows)
-        l.prompts = scratch_of((l.streamed.end + 255) / 256 * 256, prompt_target(s), s.heads, prompt_unit_rows(s), s.head_dim);
+    if (s.act_bf16 && (int64_t)b.max_new * (q_heads / s.heads) > kStreamedRows) {
+        const PromptPlan p = prompt_plan(s, b, q_heads / s.heads);
+        l.prompts = scratch_of((l.streamed.end + 255) / 256 * 256, p.target, s.heads, p.rows, s.head_dim);
+    }
     return l;
 }
 

@@ -1,34 +1,36 @@
-// Attention over the 4-bit cache for many rows: a workgroup takes 32 rows (query, head that shares a head of the cache) a wave, rebuilds 64 tokens at a time as binary16
-// in LDS, where all its waves read them, and runs both products on the matrix cores.
+// Attention over the 4-bit cache for many rows: a workgroup takes 16 or 32 rows (query, head that shares a head of the cache) a wave, rebuilds 64 tokens at a time as
+// binary16 in LDS, where all its waves read them, and runs both products on the matrix cores.
 //
-// Bound by the matrix cores and by the exponentials beside them, so a key or value is rebuilt once for the 256 rows of the workgroup: three instructions for two elements.
-// It lies in LDS in the order in which the matrix instructions' lanes take it (kv.h), which is the order of the cache: writes and reads are 1 KB of neighbouring bytes.
-// Keys and values are halved on their way (m + s c may pass 65504 by a rounding), and held to 11 bits; scores, softmax and sums are binary32, p is binary16.
+// Bound by the matrix cores, by the exponentials and by the reads of LDS, about evenly, so a key or value is rebuilt once for the rows of the workgroup, and the products
+// for the scores of one tile stand between the exponentials of the one before it.  It lies in LDS in the order in which the matrix instructions' lanes take it (kv.h), which
+// is the order of the cache: writes and reads are 1 KB of neighbouring bytes.
+// Keys and values are halved on their way (m + s c may pass 65504 by a rounding), and held to 11 bits, as are queries with the scale of the scores in them, and p.  The
+// running maximum is the products' addend, so that a score is an exponent as it comes, and the sum of p is one product more, with ones.  Scores and sums are binary32.
 #include "kv_work.h"
 
 namespace eqat {
 namespace {
 
-constexpr int kTile = 64;                          // tokens in LDS at a time, two records; two tiles of them
-constexpr int kPromptWaves = 8;
-// groups of 16 rows of a wave: heads of 256 leave the registers for one
-constexpr int columns_of(int head_dim) { return head_dim > 128 ? 1 : 2; }
+constexpr int kTile = 64;                          // tokens in LDS at a time, two records; two tiles of keys and two of values
+// Rows of a workgroup: 256 (heads of 256: 128, the registers hold no more), or 64 where that leaves compute units without one.
+constexpr int kLargeWaves = 8, kSmallWaves = 4;
+constexpr int large_columns(int head_dim) { return head_dim > 128 ? 1 : 2; }
 
 __device__ __forceinline__ half2v as_half2(uint32_t w) { return __builtin_bit_cast(half2v, w); }
-// two codes of a word (kv.h), pair p, as numbers
-__device__ __forceinline__ half2v codes_of(uint32_t w, int p)
+// two codes of a word (kv.h), pair p, halved: of 1024 + c, or 1024 + 16 c, as the bits are
+__device__ __forceinline__ half2v halves_of(uint32_t w, int p)
 {
-    const half2v x = as_half2(((p >= 2 ? w >> 8 : w) & (p & 1 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u);       // 1024 + c, 1024 + 16 c
-    const half2v sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, off = {(_Float16)-64.0f, (_Float16)-64.0f}, off1 = {(_Float16)-1024.0f, (_Float16)-1024.0f};
-    return p & 1 ? __builtin_elementwise_fma(x, sixteenth, off) : x + off1;
+    const half2v x = as_half2(((p >= 2 ? w >> 8 : w) & (p & 1 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u);
+    const _Float16 by = p & 1 ? 0.03125f : 0.5f, off = p & 1 ? -32.0f : -512.0f;
+    return __builtin_elementwise_fma(x, half2v{by, by}, half2v{off, off});
 }
 
-template <int NS, int SG> __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_kv_prompt(const AttendArgs a)
+template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_kv_prompt(const AttendArgs a)
 {
     using R = KvRecord<NS, SG>;
-    constexpr int kColumns = columns_of(32 * NS), kUnitRows = kPromptWaves * kColumns * 16;
+    constexpr int kUnitRows = kPromptWaves * kColumns * 16;
     constexpr int D = R::D, G = R::G, kChunks = NS / 2, kTileBytes = kTile * D * 2, kStaged = (4 * kChunks + kPromptWaves - 1) / kPromptWaves;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];             // two tiles: keys, values
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];             // two tiles of keys, two of values
     __shared__ uint32_t s_odd[4];                                             // tile & 3: a value of a token that is there is NaN
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, c = lane >> 4;
     const int head = blockIdx.x % a.heads;
@@ -37,21 +39,19 @@ template <int NS, int SG> __global__ __launch_bounds__(kPromptWaves * 64, 2) voi
     const int unit = (w.s.n * a.ratio + kUnitRows - 1) / kUnitRows - 1 - w.unit;        // the last rows, which see most, first
     // ---- this lane's rows -------------------------------------------------------------------------
     half8 q[kColumns][NS];
-    float k_scale[kColumns];
+    float back[kColumns];
+    bool fits = false;
     int seen_from[kColumns], seen_to[kColumns], query[kColumns], of_group[kColumns];
-    int most_to = 0, least_to = 0x7FFFFFFF, most_from = 0, least_from = 0x7FFFFFFF;
+    int least_to = 0x7FFFFFFF, most_from = 0;
 #pragma unroll
     for (int t = 0; t < kColumns; ++t) {
         const int row = unit * kUnitRows + (wave * kColumns + t) * 16 + r;
-        query[t] = row / a.ratio; of_group[t] = row - query[t] * a.ratio;
+        query[t] = quotient(row, a.ratio); of_group[t] = row - query[t] * a.ratio;
         const bool is_row = query[t] < w.s.n;
         const int pos = w.s.len - w.s.n + query[t];
         seen_to[t] = !is_row ? 0 : a.causal ? min(w.s.len, pos + 1) : w.s.len;
         seen_from[t] = is_row && a.window > 0 ? max(0, pos - a.window + 1) : 0;
-        if (is_row) {
-            most_to = max(most_to, seen_to[t]); least_to = min(least_to, seen_to[t]);
-            most_from = max(most_from, seen_from[t]); least_from = min(least_from, seen_from[t]);
-        }
+        if (is_row) { least_to = min(least_to, seen_to[t]); most_from = max(most_from, seen_from[t]); }
         const bf16_t *src = static_cast<const bf16_t *>(a.q.p) + (int64_t)(w.s.first + query[t]) * a.q.token_stride + (int64_t)(head * a.ratio + of_group[t]) * a.q.head_stride;
         float top = 0.0f;
         bf16x8 x[NS];
@@ -62,21 +62,26 @@ template <int NS, int SG> __global__ __launch_bounds__(kPromptWaves * 64, 2) voi
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[j][e]));
         }
-        const int up = min(max(135 - (int)(__float_as_uint(chunks_max(top)) >> 23), -100), 100);         // the row's largest element in [2^8, 2^9)
-        const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
+        // The row with the scale of the scores in it, 2 for the halved keys and log2(e); a power of two more, taken back from the scores, where binary16 would not hold
+        // it well: in rows far larger or smaller than those of a model.
+        const float scale = a.scale * 2.0f, most = chunks_max(top) * scale;
+        const int fit = most > 32768.0f || (most > 0.0f && most < 0x1p-8f) ? min(max(127 - (int)(__float_as_uint(most) >> 23), -100), 100) : 0;
+        const float fitted = __uint_as_float((uint32_t)(127 + fit) << 23);
+        back[t] = __uint_as_float((uint32_t)(127 - fit) << 23);
+        fits |= fit != 0;
 #pragma unroll
         for (int j = 0; j < NS; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[t][j][e] = (_Float16)((float)x[j][e] * scale);
-        k_scale[t] = a.scale * 2.0f * __uint_as_float((uint32_t)(127 - up) << 23);
+            for (int e = 0; e < 8; ++e) q[t][j][e] = (_Float16)((float)x[j][e] * scale * fitted);
     }
 #pragma unroll
     for (int d = 8; d >= 1; d >>= 1) {
-        most_to = max(most_to, __shfl_xor(most_to, d)); least_to = min(least_to, __shfl_xor(least_to, d));
-        most_from = max(most_from, __shfl_xor(most_from, d)); least_from = min(least_from, __shfl_xor(least_from, d));
+        least_to = min(least_to, __shfl_xor(least_to, d));
+        most_from = max(most_from, __shfl_xor(most_from, d));
     }
-    most_to = __builtin_amdgcn_readfirstlane(most_to); least_to = __builtin_amdgcn_readfirstlane(least_to);
-    most_from = __builtin_amdgcn_readfirstlane(most_from); least_from = __builtin_amdgcn_readfirstlane(least_from);
+    const bool any_fits = __any(fits);
+    least_to = __builtin_amdgcn_readfirstlane(least_to);
+    most_from = __builtin_amdgcn_readfirstlane(most_from);
     // ---- the records of the workgroup ---------------------------------------------------------------
     int first = w.first, last = w.last;
     {
@@ -86,143 +91,186 @@ template <int NS, int SG> __global__ __launch_bounds__(kPromptWaves * 64, 2) voi
     }
     const int tiles = max(0, (last - first + 1) >> 1);
     const int32_t *table = a.b.table + (int64_t)w.b * a.b.table_stride;
-    // the next record's place; nullptr where it is past the end or its page is not there
-    int next_rec = first, next_page = first / a.page_records, in_page = first - next_page * a.page_records;
-    auto next_record = [&]() -> const uint8_t * {
-        const uint8_t *at = nullptr;
-        if (next_rec < last) {
-            const int page = __builtin_amdgcn_readfirstlane(table[next_page]);
-            if (page >= 0 && page < a.pages) at = a.pool + (((int64_t)page * a.heads + head) * a.page_records + in_page) * R::kBytes;
+    // the next record's place; nullptr where it is past the end or its page is not there.  Lane i has looked up where the i-th of 64 of them lies.
+    int ahead = 0, place_lo = -1, place_hi = -1;
+    auto next_record = [&]() __attribute__((always_inline)) -> const uint8_t * {
+        if ((ahead & 63) == 0) {
+            const int rec = first + ahead + lane, of_seq = quotient(rec, a.page_records);
+            const int page = rec < last ? table[of_seq] : -1;
+            const int64_t at = page >= 0 && page < a.pages ? (((int64_t)page * a.heads + head) * a.page_records + (rec - of_seq * a.page_records)) * R::kBytes : -1;
+            place_lo = (int)at; place_hi = (int)(at >> 32);
         }
-        ++next_rec;
-        if (++in_page == a.page_records) { in_page = 0; ++next_page; }
-        return at;
+        const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_readlane(place_lo, ahead & 63) | (int64_t)__builtin_amdgcn_readlane(place_hi, ahead & 63) << 32;
+        const bool is = first + ahead < last && at >= 0;
+        ++ahead;
+        return is ? a.pool + at : nullptr;
     };
-    // Chunks of a tile, kStaged a wave: of two records, keys' and values' chunks
+    // Chunks of a tile, kStaged a wave: of two records, keys' and values' chunks.  Keys are fetched for two tiles on, values for the next.  All waves issue the same loads,
+    // whichever they have use for, from the pool's first record where there is none: loads under a branch would be waited for where it ends.
     constexpr int kShared = SG < 4 ? SG : 4;                 // words of a chunk of keys that share their step
-    uintx4 raw[kStaged], steps[kStaged][4];
-    const uint8_t *place[2];                                 // of the records of the tile fetched last
-    auto fetch = [&]() {
-        place[0] = next_record();
-        place[1] = next_record();
+    constexpr int kGroups = SG == 1 ? 2 : 1;                 // groups of a chunk of values
+    uintx4 raw[kStaged], value_steps[kStaged][2 * kGroups];
+    uint32_t key_steps[kStaged][4 / kShared];
+    const uint8_t *here0 = nullptr, *here1 = nullptr, *next0 = nullptr, *next1 = nullptr, *after0 = nullptr, *after1 = nullptr;      // the records of this tile, the next, the one after
+    auto turn = [&]() __attribute__((always_inline)) {
+        here0 = next0; here1 = next1; next0 = after0; next1 = after1;
+        after0 = next_record(); after1 = next_record();
+    };
+    auto of = [](const uint8_t *a, const uint8_t *b, bool second) __attribute__((always_inline)) { return second ? b : a; };          // (by value: a choice of variables would put them in memory)
+    // chunk k of this wave: waves that share a SIMD (w, w + 4) take one of keys and one of values where there are eight
+    struct Chunk { bool is, key; int rec, i; };
+    auto chunk = [&](int k) __attribute__((always_inline)) {
+        const int id = (kPromptWaves == 8 && kChunks == 2 && wave >= 4 ? wave ^ 2 : wave) + k * kPromptWaves, part = id % (2 * kChunks);
+        return Chunk{id < 4 * kChunks, part < kChunks, id / (2 * kChunks) & 1, part % kChunks};
+    };
+    auto fetch = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < kStaged; ++k) {
-            const int id = wave + k * kPromptWaves, rec = id / (2 * kChunks), part = id % (2 * kChunks), i = part % kChunks;
-            if (id >= 4 * kChunks) continue;
-            const uint8_t *at = place[rec];
-            if (at == nullptr) continue;
-            if (part < kChunks) {
-                raw[k] = *reinterpret_cast<const uintx4 *>(at + R::kKeys + i * 1024 + lane * 16);
+            const Chunk x = chunk(k);
+            const uint8_t *at = of(of(next0, next1, x.rec != 0), of(after0, after1, x.rec != 0), x.key);
+            if (at == nullptr) at = a.pool;
+            raw[k] = *reinterpret_cast<const uintx4 *>(at + (x.key ? R::kKeys : R::kValues) + x.i * 1024 + lane * 16);
 #pragma unroll
-                for (int e = 0; e < 4; e += kShared) {
-                    const int word = i * 4 + e, sub = word / NS, j = word % NS;
-                    steps[k][0][e] = *reinterpret_cast<const uint32_t *>(at + R::kKeySteps + (j / SG) * 128 + (sub * 16 + r) * 4);
-                }
-            } else {
-                raw[k] = *reinterpret_cast<const uintx4 *>(at + R::kValues + i * 1024 + lane * 16);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    steps[k][h] = *reinterpret_cast<const uintx4 *>(at + R::kValueSteps + (2 * i / SG) * 128 + h * 64 + c * 16);
-                    if constexpr (SG == 1) steps[k][2 + h] = *reinterpret_cast<const uintx4 *>(at + R::kValueSteps + (2 * i + 1) * 128 + h * 64 + c * 16);
-                }
+            for (int e = 0; e < 4; e += kShared) {
+                const int word = x.i * 4 + e, sub = (word / NS) & 1, j = word % NS;
+                key_steps[k][e / kShared] = *reinterpret_cast<const uint32_t *>(at + R::kKeySteps + (j / SG) * 128 + (sub * 16 + r) * 4);
             }
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) value_steps[k][2 * g + h] = *reinterpret_cast<const uintx4 *>(at + R::kValueSteps + ((2 * x.i + g) / SG) * 128 + h * 64 + c * 16);
         }
     };
     const half2v halved = {(_Float16)0.5f, (_Float16)0.5f};
-    auto rebuild = [&](int tile) {
-        uint8_t *keys = lds + (tile & 1) * 2 * kTileBytes, *values = keys + kTileBytes;
+    // into LDS, keys as those of tile key_tile, values as those of value_tile
+    auto rebuild = [&](int key_tile, int value_tile, bool do_keys, bool do_values) __attribute__((always_inline)) {
+        uint8_t *keys = lds + (key_tile & 1) * kTileBytes, *values = lds + (2 + (value_tile & 1)) * kTileBytes;
 #pragma unroll
         for (int k = 0; k < kStaged; ++k) {
-            const int id = wave + k * kPromptWaves, rec = id / (2 * kChunks), part = id % (2 * kChunks), i = part % kChunks;
-            if (id >= 4 * kChunks) continue;
-            if (part < kChunks) {
-                if (place[rec] == nullptr) continue;         // masked, whatever stands there
+            const Chunk x = chunk(k);
+            if (!x.is) continue;
+            if (x.key) {
+                if (!do_keys || of(after0, after1, x.rec != 0) == nullptr) continue;          // (not there: masked, whatever stands in LDS)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int word = i * 4 + e, sub = word / NS, j = word % NS;
-                    const half2v sm = as_half2(steps[k][0][e & -kShared]) * halved, s = {sm[0], sm[0]}, m = {sm[1], sm[1]};
-                    uintx4 x;
+                    const int word = x.i * 4 + e, sub = word / NS, j = word % NS;
+                    const half2v sm = as_half2(key_steps[k][e / kShared]), m = sm * halved;
+                    uintx4 y;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) x[p] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(codes_of(raw[k][e], p), s, m));
-                    *reinterpret_cast<uintx4 *>(keys + ((rec * 2 + sub) * NS + j) * 1024 + lane * 16) = x;
+                    for (int p = 0; p < 4; ++p) y[p] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(halves_of(raw[k][e], p), half2v{sm[0], sm[0]}, half2v{m[1], m[1]}));
+                    *reinterpret_cast<uintx4 *>(keys + ((x.rec * 2 + sub) * NS + j) * 1024 + lane * 16) = y;
                 }
-            } else {
-                // what no row sees must be a number: 0 p = 0.  A NaN that some row may see is put aside and dealt with apart.
-                const int token = (first + 2 * tile + rec) * kKvRecord + c * 4;
-                bool odd = false;
-                half2v s[SG == 1 ? 2 : 1][4], m[SG == 1 ? 2 : 1][4];
+            } else if (do_values) {
+                // What no row sees must be a number: 0 p = 0.  A NaN that some row may see is put aside and dealt with apart.
+                const int token = (first + 2 * value_tile + x.rec) * kKvRecord;
+                const bool there = of(next0, next1, x.rec != 0) != nullptr;
+                uint32_t most = 0;                            // of the steps in the low halves: NaN is above every number
 #pragma unroll
-                for (int g = 0; g < (SG == 1 ? 2 : 1); ++g)
+                for (int g = 0; g < 2 * kGroups; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = max(most, value_steps[k][g][e] & 0xFFFFu);
+                if (__any(most >= 0x7C00u) || !there || token + kKvRecord > w.s.len) {
+                    bool odd = false;
+#pragma unroll
+                    for (int g = 0; g < 2 * kGroups; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool is = there && token + (g & 1) * 16 + c * 4 + e < w.s.len, nan = (value_steps[k][g][e] & 0x7C00u) == 0x7C00u;
+                            odd |= is && nan;
+                            value_steps[k][g][e] = is && !nan ? value_steps[k][g][e] : 0u;
+                        }
+                    if (__any(odd) && lane == 0) s_odd[value_tile & 3] = 1u;
+                }
+                half2v s[kGroups][4], m[kGroups][4];
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        uint32_t u[2];
-#pragma unroll
-                        for (int o = 0; o < 2; ++o) {
-                            const int at = (e & 1) * 2 + o;
-                            u[o] = steps[k][2 * g + (e >> 1)][at];
-                            const bool is = place[rec] != nullptr && token + (e >> 1) * 16 + at < w.s.len, nan = (u[o] & 0x7C00u) == 0x7C00u;
-                            odd |= is && nan;
-                            u[o] = is && !nan ? u[o] : 0u;
-                        }
-                        s[g][e] = as_half2(__builtin_amdgcn_perm(u[1], u[0], 0x05040100u)) * halved;
-                        m[g][e] = as_half2(__builtin_amdgcn_perm(u[1], u[0], 0x07060302u)) * halved;
+                        const uint32_t u = value_steps[k][2 * g + (e >> 1)][(e & 1) * 2], v = value_steps[k][2 * g + (e >> 1)][(e & 1) * 2 + 1];
+                        s[g][e] = as_half2(__builtin_amdgcn_perm(v, u, 0x05040100u));
+                        m[g][e] = as_half2(__builtin_amdgcn_perm(v, u, 0x07060302u)) * halved;
                     }
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    const int n = 4 * i + p, g = SG == 1 ? p >> 1 : 0;
-                    uintx4 x;
+                    const int n = 4 * x.i + p, g = kGroups == 2 ? p >> 1 : 0;
+                    uintx4 y;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(codes_of(raw[k][e], p), s[g][e], m[g][e]));
-                    *reinterpret_cast<uintx4 *>(values + (rec * 2 * NS + n) * 1024 + lane * 16) = x;
+                    for (int e = 0; e < 4; ++e) y[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(halves_of(raw[k][e], p), s[g][e], m[g][e]));
+                    *reinterpret_cast<uintx4 *>(values + (x.rec * 2 * NS + n) * 1024 + lane * 16) = y;
                 }
-                if (__any(odd) && lane == 0) s_odd[tile & 3] = 1u;
             }
         }
     };
-    floatx4 o[kColumns][2 * NS];
-    float top[kColumns], total[kColumns];
+    floatx4 o[kColumns][2 * NS], sum[kColumns], s[4][kColumns];
+    float top[kColumns];                                     // what a score has had taken off it, in its own fitted units
+    float limit[kColumns];                                   // above which a score moves it: 2, or anything before the row has seen something
+    const floatx4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const uintx4 ones = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
     for (int t = 0; t < kColumns; ++t) {
-        top[t] = -3.0e38f; total[t] = 0.0f;
+        top[t] = 0.0f; limit[t] = -__builtin_inff(); sum[t] = zero;
 #pragma unroll
-        for (int n = 0; n < 2 * NS; ++n) o[t][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int n = 0; n < 2 * NS; ++n) o[t][n] = zero;
     }
+    // the scores of 16 tokens, less top
+    auto scores = [&](int tile, int h) __attribute__((always_inline)) {
+        const uint8_t *keys = lds + (tile & 1) * kTileBytes;
+        uintx4 k[NS];
+#pragma unroll
+        for (int j = 0; j < NS; ++j) k[j] = *reinterpret_cast<const uintx4 *>(keys + (h * NS + j) * 1024 + lane * 16);
+#pragma unroll
+        for (int t = 0; t < kColumns; ++t) s[h][t] = floatx4{-top[t], -top[t], -top[t], -top[t]};
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int t = 0; t < kColumns; ++t) s[h][t] = mfma(k[j], q[t][j], s[h][t]);
+    };
     if (tid < 4) s_odd[tid] = 0u;
     __syncthreads();
-    bool absent0 = true, absent1 = true;                     // of the tile in LDS
-    if (tiles > 0) { fetch(); rebuild(0); absent0 = place[0] == nullptr; absent1 = place[1] == nullptr; }
+    if (tiles > 0) {
+        turn(); fetch(); rebuild(0, 0, true, false);
+        turn(); fetch(); rebuild(1, 0, true, true);
+        turn();                                              // this tile, the next, the one after
+    }
     __syncthreads();
+    if (tiles > 0)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) scores(0, h);
     for (int tile = 0; tile < tiles; ++tile) {
-        if (tile + 1 < tiles) fetch();
+        fetch();                                              // keys of tile + 2, values of tile + 1
         const int token0 = (first + 2 * tile) * kKvRecord;
-        const uint8_t *keys = lds + (tile & 1) * 2 * kTileBytes, *values = keys + kTileBytes;
-        if (token0 < most_to && token0 + kTile > least_from) {                // some row of the wave sees some of it
-            const uint32_t odd = s_odd[tile & 3];
-            floatx4 s[4][kColumns];
+        const uint32_t odd = s_odd[tile & 3];
+        const bool absent0 = here0 == nullptr, absent1 = here1 == nullptr;
+        if (any_fits) {
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
+            for (int h = 0; h < 4; ++h)
 #pragma unroll
-                for (int t = 0; t < kColumns; ++t) s[h][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int t = 0; t < kColumns; ++t) s[h][t] *= back[t];
+        }
+        if (token0 < most_from || token0 + kTile > least_to || absent0 || absent1) {
 #pragma unroll
-                for (int j = 0; j < NS; ++j) {
-                    const uintx4 k = *reinterpret_cast<const uintx4 *>(keys + (h * NS + j) * 1024 + lane * 16);
+            for (int h = 0; h < 4; ++h)
 #pragma unroll
-                    for (int t = 0; t < kColumns; ++t) s[h][t] = mfma(k, q[t][j], s[h][t]);
-                }
-            }
-            if (token0 < most_from || token0 + kTile > least_to || absent0 || absent1) {
+                for (int t = 0; t < kColumns; ++t)
 #pragma unroll
-                for (int h = 0; h < 4; ++h)
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = token0 + h * 16 + c * 4 + i;
+                        const bool seen = at >= seen_from[t] && at < seen_to[t] && !(h < 2 ? absent0 : absent1);
+                        s[h][t][i] = seen ? s[h][t][i] : -__builtin_inff();
+                    }
+        }
+        bool move = false;
 #pragma unroll
-                    for (int t = 0; t < kColumns; ++t)
+        for (int t = 0; t < kColumns; ++t) {
+            float most = s[0][t][0];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int at = token0 + h * 16 + c * 4 + i;
-                            const bool seen = at >= seen_from[t] && at < seen_to[t] && !(h < 2 ? absent0 : absent1);
-                            s[h][t][i] = seen ? s[h][t][i] : -__builtin_inff();
-                        }
-            }
-            uint32_t p[kColumns][2][4];
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, s[h][t][i]);
+            move |= most > limit[t];
+        }
+        if (__any(move)) {
+            // the maximum moves: always to the first tile's, later where a score passes it by 2 (p is at most 4)
 #pragma unroll
             for (int t = 0; t < kColumns; ++t) {
                 float most = s[0][t][0];
@@ -230,63 +278,78 @@ template <int NS, int SG> __global__ __launch_bounds__(kPromptWaves * 64, 2) voi
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) most = fmaxf(most, s[h][t][i]);
-                most = chunks_max(most) * k_scale[t];
-                if (__any(most > top[t] + 2.0f)) {
-                    const float next = fmaxf(top[t], most), down = exp2_of(top[t] - next);
-                    top[t] = next;
-                    total[t] *= down;
+                most = chunks_max(most);
+                const bool moves = most > limit[t];
+                const float by = moves ? most : 0.0f, down = limit[t] > 0.0f ? exp2_of(-by) : 0.0f;
+                top[t] += by / back[t];
+                limit[t] = moves ? 2.0f : limit[t];
+                sum[t] *= down;
 #pragma unroll
-                    for (int n = 0; n < 2 * NS; ++n) o[t][n] *= down;
-                }
+                for (int n = 0; n < 2 * NS; ++n) o[t][n] *= down;
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    float e[4];
+                for (int h = 0; h < 4; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        e[i] = exp2_of(__builtin_fmaf(s[h][t][i], k_scale[t], -top[t]));
-                        total[t] += e[i];
-                    }
-                    p[t][h >> 1][(h & 1) * 2] = __builtin_bit_cast(uint32_t, half2v{(_Float16)e[0], (_Float16)e[1]});
-                    p[t][h >> 1][(h & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, half2v{(_Float16)e[2], (_Float16)e[3]});
-                }
+                    for (int i = 0; i < 4; ++i) s[h][t][i] -= by;
+            }
+        }
+        uint32_t p[kColumns][2][4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+#pragma unroll
+            for (int t = 0; t < kColumns; ++t) {
+                float e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = exp2_of(s[h][t][i]);
+                p[t][h >> 1][(h & 1) * 2] = __builtin_bit_cast(uint32_t, half2v{(_Float16)e[0], (_Float16)e[1]});
+                p[t][h >> 1][(h & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, half2v{(_Float16)e[2], (_Float16)e[3]});
+            }
+            scores(tile + 1, h);                              // (past the last tile: of whatever stands there, not looked at)
+        }
+        const uint8_t *values = lds + (2 + (tile & 1)) * kTileBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            half8 ph[kColumns];
+#pragma unroll
+            for (int t = 0; t < kColumns; ++t) {
+                ph[t] = __builtin_bit_cast(half8, uintx4{p[t][h][0], p[t][h][1], p[t][h][2], p[t][h][3]});
+                sum[t] = mfma(ones, ph[t], sum[t]);
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int n = 0; n < 2 * NS; ++n) {
+                const uintx4 v = *reinterpret_cast<const uintx4 *>(values + (h * 2 * NS + n) * 1024 + lane * 16);
 #pragma unroll
-                for (int n = 0; n < 2 * NS; ++n) {
-                    const uintx4 v = *reinterpret_cast<const uintx4 *>(values + (h * 2 * NS + n) * 1024 + lane * 16);
+                for (int t = 0; t < kColumns; ++t) o[t][n] = mfma(v, ph[t], o[t][n]);
+            }
+        }
+        if (__builtin_amdgcn_readfirstlane(odd) != 0u) {
+            // NaN among the values: it reaches the rows that see its token, in the elements of its group
+            for (int t64 = 0; t64 < kTile; ++t64) {
+                const int at = token0 + t64;
+                const uint8_t *rec = of(here0, here1, t64 >= kKvRecord);
+                if (rec == nullptr || at >= w.s.len) continue;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t step = *reinterpret_cast<const uint32_t *>(rec + R::kValueSteps + g * 128 + (t64 & 31) * 4);
+                    if ((step & 0x7C00u) != 0x7C00u) continue;
 #pragma unroll
                     for (int t = 0; t < kColumns; ++t)
-                        o[t][n] = mfma(v, __builtin_bit_cast(half8, uintx4{p[t][h][0], p[t][h][1], p[t][h][2], p[t][h][3]}), o[t][n]);
-                }
-            if (__builtin_amdgcn_readfirstlane(odd) != 0u) {
-                // NaN among the values: it reaches the rows that see its token, in the elements of its group
-                for (int t64 = 0; t64 < kTile; ++t64) {
-                    const int at = token0 + t64;
-                    if ((t64 < 32 ? absent0 : absent1) || at >= w.s.len) continue;
-                    const int of_seq = (at >> 5) / a.page_records, page = __builtin_amdgcn_readfirstlane(table[of_seq]);
-                    const uint8_t *rec = a.pool + (((int64_t)page * a.heads + head) * a.page_records + ((at >> 5) - of_seq * a.page_records)) * R::kBytes;
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        const uint32_t step = *reinterpret_cast<const uint32_t *>(rec + R::kValueSteps + g * 128 + (t64 & 31) * 4);
-                        if ((step & 0x7C00u) != 0x7C00u) continue;
-#pragma unroll
-                        for (int t = 0; t < kColumns; ++t)
-#pragma unroll
-                            for (int n = 2 * g * SG; n < 2 * (g + 1) * SG; ++n)
-                                if (at >= seen_from[t] && at < seen_to[t]) o[t][n] = floatx4{1.0f, 1.0f, 1.0f, 1.0f} * __builtin_nanf("");
-                    }
+                        for (int n = 2 * g * SG; n < 2 * (g + 1) * SG; ++n)
+                            if (at >= seen_from[t] && at < seen_to[t]) o[t][n] = floatx4{1.0f, 1.0f, 1.0f, 1.0f} * __builtin_nanf("");
                 }
             }
         }
         if (tid == 0) s_odd[(tile + 3) & 3] = 0u;             // read a tile ago, set again two tiles on
-        if (tile + 1 < tiles) { rebuild(tile + 1); absent0 = place[0] == nullptr; absent1 = place[1] == nullptr; }
+        rebuild(tile + 2, tile + 1, true, true);
+        turn();
         __syncthreads();
     }
     // ---- results --------------------------------------------------------------------------------------
+    float total[kColumns];
 #pragma unroll
     for (int t = 0; t < kColumns; ++t) {
-        total[t] = chunks_sum(total[t]);
+        total[t] = sum[t][0];
+        top[t] = limit[t] > 0.0f ? top[t] * back[t] : -3.0e38f;
 #pragma unroll
         for (int n = 0; n < 2 * NS; ++n) o[t][n] *= 2.0f;
     }
@@ -361,31 +424,46 @@ template <int NS, int SG> __global__ __launch_bounds__(kPromptWaves * 64, 2) voi
     }
 }
 
-template <int NS, int SG> void launch(const AttendArgs &a, hipStream_t st)
+template <int NS, int SG, int W, int C> void launch_t(const AttendArgs &a, hipStream_t st)
 {
-    constexpr int smem = 2 * 2 * kTile * 32 * NS * 2;
-    allow_lds(reinterpret_cast<const void *>(&k_kv_prompt<NS, SG>), smem);
-    k_kv_prompt<NS, SG><<<dim3((unsigned)a.slots * (unsigned)a.heads), kPromptWaves * 64, smem, st>>>(a);
+    constexpr int smem = 4 * kTile * 32 * NS * 2;
+    allow_lds(reinterpret_cast<const void *>(&k_kv_prompt<NS, SG, W, C>), smem);
+    k_kv_prompt<NS, SG, W, C><<<dim3((unsigned)a.slots * (unsigned)a.heads), W * 64, smem, st>>>(a);
 }
+template <int NS, int SG> void launch(const AttendArgs &a, bool large, hipStream_t st)
+{
+    if (large) launch_t<NS, SG, kLargeWaves, large_columns(32 * NS)>(a, st);
+    else launch_t<NS, SG, kSmallWaves, 1>(a, st);
+}
+
+int large_rows(const KvShape &s) { return kLargeWaves * large_columns(s.head_dim) * 16; }
+constexpr int kSmallRows = kSmallWaves * 16;
 
 }  // namespace
 
-int prompt_target(const KvShape &s) { return (256 + s.heads - 1) / s.heads; }        // a workgroup on every compute unit
-int prompt_unit_rows(const KvShape &s) { return kPromptWaves * columns_of(s.head_dim) * 16; }
+PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio)
+{
+    PromptPlan p;
+    p.large = (int64_t)units_at_most(b, ratio, large_rows(s)) * s.heads >= 256;
+    p.rows = p.large ? large_rows(s) : kSmallRows;
+    p.target = (256 * (p.large ? 1 : 2) + s.heads - 1) / s.heads;          // a workgroup on every compute unit, or two small ones
+    return p;
+}
 
 void launch_kv_prompt(const KvShape &s, AttendArgs a, hipStream_t st)
 {
-    const int rows = prompt_unit_rows(s);
-    a.unit_bits = __builtin_ctz(rows);
+    const PromptPlan p = prompt_plan(s, a.b, a.ratio);
+    a.unit_bits = __builtin_ctz(p.rows);
     a.fewest = 8;
-    a.target = prompt_target(s);
-    a.slots = a.target + units_at_most(a.b, a.ratio, rows);
+    a.target = p.target;
+    a.slots = p.target + units_at_most(a.b, a.ratio, p.rows);
     const int sg = s.group / 32;
     switch (s.head_dim) {
-    case 64: if (sg == 1) launch<2, 1>(a, st); else launch<2, 2>(a, st); break;
-    case 128: if (sg == 1) launch<4, 1>(a, st); else if (sg == 2) launch<4, 2>(a, st); else launch<4, 4>(a, st); break;
+    case 64: if (sg == 1) launch<2, 1>(a, p.large, st); else launch<2, 2>(a, p.large, st); break;
+    case 128: if (sg == 1) launch<4, 1>(a, p.large, st); else if (sg == 2) launch<4, 2>(a, p.large, st); else launch<4, 4>(a, p.large, st); break;
     default:
-        if (sg == 1) launch<8, 1>(a, st); else if (sg == 2) launch<8, 2>(a, st); else if (sg == 4) launch<8, 4>(a, st); else launch<8, 8>(a, st);
+        if (sg == 1) launch<8, 1>(a, p.large, st); else if (sg == 2) launch<8, 2>(a, p.large, st);
+        else if (sg == 4) launch<8, 4>(a, p.large, st); else launch<8, 8>(a, p.large, st);
     }
 }
 

@@ -223,8 +223,8 @@ void allow_lds(const void *kernel, int bytes)
 }  // namespace
 
 // ---- kv_prompt.hip ---------------------------------------------------------------------------
-int prompt_target(const KvShape &s);
-int prompt_unit_rows(const KvShape &s);
+struct PromptPlan { int rows, target; bool large; };         // rows of a unit; chunks aimed at for a head of the cache
+PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio);
 void launch_kv_prompt(const KvShape &s, AttendArgs a, hipStream_t st);
 
 }  // namespace eqat
