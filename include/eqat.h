@@ -402,7 +402,8 @@ eqat_status eqat_dx_route(const eqat_desc *d, int block_ap, int32_t *route);
  *   in binary32 (the quotients correctly rounded, round() half to even), f16 the nearest binary16 number.  A group with an element that is not finite, or beyond
  *   binary16 (65504), stands as NaN; one that spans less than about 2^-16 is held in steps of 2^-24.
  *
- *   Pool       eqat_kv_pool_bytes(desc) bytes of device memory, 256-byte aligned, owned by the caller; of any size (offsets are 64 bits), of any contents at first.
+ *   Pool       eqat_kv_pool_bytes(desc) bytes of device memory, 256-byte aligned, owned by the caller; of any size (offsets are 64 bits; fewer than 2^31 records of
+ *              32 tokens and a head), of any contents at first.
  *              It is a number of pages of `page_tokens` tokens; how a page is laid out is the library's own.  Bytes per token and head: head_dim + 8 head_dim / group.
  *   Sequences  An eqat_kv_batch says, in device arrays, where the sequences of a call stand: sequence b holds lens[b] tokens, its position p on page
  *              table[b * table_stride + p / page_tokens] (at p % page_tokens), and its newest starts[b+1] - starts[b] tokens are the rows starts[b] .. starts[b+1] - 1 of

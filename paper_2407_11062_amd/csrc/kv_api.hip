@@ -26,7 +26,7 @@ eqat_status check_desc(const eqat_kv_desc *d, KvShape *s)
     if ((g != 32 && g != 64 && g != 128 && g != 256) || g > d->head_dim) return EQAT_ERR_GROUP;
     if (d->heads < 1 || d->heads > 1 << 16 || d->page_tokens < 32 || d->page_tokens % 32 != 0 || d->pages < 1 || d->pages >= kMost) return EQAT_ERR_SHAPE;
     const int64_t per_page = eqat::kv_record_bytes(d->head_dim, d->head_dim / g) * d->heads * (d->page_tokens / 32);      // below 2^60
-    if (d->pages > ((int64_t)1 << 46) / per_page) return EQAT_ERR_SHAPE;
+    if (d->pages > ((int64_t)1 << 46) / per_page || d->pages * d->heads >= kMost / (d->page_tokens / 32)) return EQAT_ERR_SHAPE;         // records are numbered in 32 bits
     s->heads = d->heads; s->head_dim = d->head_dim; s->group = g; s->groups = d->head_dim / g;
     s->page_records = d->page_tokens / 32; s->pages = d->pages; s->act_bf16 = d->act_dtype == EQAT_BF16;
     return EQAT_OK;

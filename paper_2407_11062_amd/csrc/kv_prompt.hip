@@ -91,19 +91,15 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
     }
     const int tiles = max(0, (last - first + 1) >> 1);
     const int32_t *table = a.b.table + (int64_t)w.b * a.b.table_stride;
-    // the next record's place; nullptr where it is past the end or its page is not there.  Lane i has looked up where the i-th of 64 of them lies.
-    int ahead = 0, place_lo = -1, place_hi = -1;
-    auto next_record = [&]() __attribute__((always_inline)) -> const uint8_t * {
+    // the next record's number in the pool; -1 where it is past the end or its page is not there.  Lane i has looked up the i-th of 64 of them.
+    int ahead = 0, looked_up = -1;
+    auto next_record = [&]() __attribute__((always_inline)) {
         if ((ahead & 63) == 0) {
             const int rec = first + ahead + lane, of_seq = quotient(rec, a.page_records);
             const int page = rec < last ? table[of_seq] : -1;
-            const int64_t at = page >= 0 && page < a.pages ? (((int64_t)page * a.heads + head) * a.page_records + (rec - of_seq * a.page_records)) * R::kBytes : -1;
-            place_lo = (int)at; place_hi = (int)(at >> 32);
+            looked_up = page >= 0 && page < a.pages ? (page * a.heads + head) * a.page_records + (rec - of_seq * a.page_records) : -1;
         }
-        const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_readlane(place_lo, ahead & 63) | (int64_t)__builtin_amdgcn_readlane(place_hi, ahead & 63) << 32;
-        const bool is = first + ahead < last && at >= 0;
-        ++ahead;
-        return is ? a.pool + at : nullptr;
+        return __builtin_amdgcn_readlane(looked_up, ahead++ & 63);
     };
     // Chunks of a tile, kStaged a wave: of two records, keys' and values' chunks.  Keys are fetched for two tiles on, values for the next.  All waves issue the same loads,
     // whichever they have use for, from the pool's first record where there is none: loads under a branch would be waited for where it ends.
@@ -111,12 +107,12 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
     constexpr int kGroups = SG == 1 ? 2 : 1;                 // groups of a chunk of values
     uintx4 raw[kStaged], value_steps[kStaged][2 * kGroups];
     uint32_t key_steps[kStaged][4 / kShared];
-    const uint8_t *here0 = nullptr, *here1 = nullptr, *next0 = nullptr, *next1 = nullptr, *after0 = nullptr, *after1 = nullptr;      // the records of this tile, the next, the one after
+    int here0 = -1, here1 = -1, next0 = -1, next1 = -1, after0 = -1, after1 = -1;            // the records of this tile, the next, the one after
     auto turn = [&]() __attribute__((always_inline)) {
         here0 = next0; here1 = next1; next0 = after0; next1 = after1;
         after0 = next_record(); after1 = next_record();
     };
-    auto of = [](const uint8_t *a, const uint8_t *b, bool second) __attribute__((always_inline)) { return second ? b : a; };          // (by value: a choice of variables would put them in memory)
+    auto of = [](int a, int b, bool second) __attribute__((always_inline)) { return second ? b : a; };          // (by value: a choice of variables would put them in memory)
     // chunk k of this wave: waves that share a SIMD (w, w + 4) take one of keys and one of values where there are eight
     struct Chunk { bool is, key; int rec, i; };
     auto chunk = [&](int k) __attribute__((always_inline)) {
@@ -127,8 +123,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
 #pragma unroll
         for (int k = 0; k < kStaged; ++k) {
             const Chunk x = chunk(k);
-            const uint8_t *at = of(of(next0, next1, x.rec != 0), of(after0, after1, x.rec != 0), x.key);
-            if (at == nullptr) at = a.pool;
+            const uint8_t *at = a.pool + (int64_t)max(of(of(next0, next1, x.rec != 0), of(after0, after1, x.rec != 0), x.key), 0) * R::kBytes;
             raw[k] = *reinterpret_cast<const uintx4 *>(at + (x.key ? R::kKeys : R::kValues) + x.i * 1024 + lane * 16);
 #pragma unroll
             for (int e = 0; e < 4; e += kShared) {
@@ -150,7 +145,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
             const Chunk x = chunk(k);
             if (!x.is) continue;
             if (x.key) {
-                if (!do_keys || of(after0, after1, x.rec != 0) == nullptr) continue;          // (not there: masked, whatever stands in LDS)
+                if (!do_keys || of(after0, after1, x.rec != 0) < 0) continue;          // (not there: masked, whatever stands in LDS)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int word = x.i * 4 + e, sub = word / NS, j = word % NS;
@@ -163,7 +158,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
             } else if (do_values) {
                 // What no row sees must be a number: 0 p = 0.  A NaN that some row may see is put aside and dealt with apart.
                 const int token = (first + 2 * value_tile + x.rec) * kKvRecord;
-                const bool there = of(next0, next1, x.rec != 0) != nullptr;
+                const bool there = of(next0, next1, x.rec != 0) >= 0;
                 uint32_t most = 0;                            // of the steps in the low halves: NaN is above every number
 #pragma unroll
                 for (int g = 0; g < 2 * kGroups; ++g)
@@ -213,15 +208,15 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
         for (int n = 0; n < 2 * NS; ++n) o[t][n] = zero;
     }
     // the scores of 16 tokens, less top
-    auto scores = [&](int tile, int h) __attribute__((always_inline)) {
-        const uint8_t *keys = lds + (tile & 1) * kTileBytes;
-        uintx4 k[NS];
+    auto key_parts = [&](int tile, int h, uintx4 (&k)[NS]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < NS; ++j) k[j] = *reinterpret_cast<const uintx4 *>(keys + (h * NS + j) * 1024 + lane * 16);
+        for (int j = 0; j < NS; ++j) k[j] = *reinterpret_cast<const uintx4 *>(lds + (tile & 1) * kTileBytes + (h * NS + j) * 1024 + lane * 16);
+    };
+    auto scores = [&](int h, const uintx4 (&k)[NS]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < kColumns; ++t) s[h][t] = floatx4{-top[t], -top[t], -top[t], -top[t]};
+        for (int t = 0; t < kColumns; ++t) s[h][t] = mfma(k[0], q[t][0], floatx4{-top[t], -top[t], -top[t], -top[t]});
 #pragma unroll
-        for (int j = 0; j < NS; ++j)
+        for (int j = 1; j < NS; ++j)
 #pragma unroll
             for (int t = 0; t < kColumns; ++t) s[h][t] = mfma(k[j], q[t][j], s[h][t]);
     };
@@ -235,19 +230,15 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
     __syncthreads();
     if (tiles > 0)
 #pragma unroll
-        for (int h = 0; h < 4; ++h) scores(0, h);
+        for (int h = 0; h < 4; ++h) { uintx4 k[NS]; key_parts(0, h, k); scores(h, k); }
     for (int tile = 0; tile < tiles; ++tile) {
         fetch();                                              // keys of tile + 2, values of tile + 1
         const int token0 = (first + 2 * tile) * kKvRecord;
         const uint32_t odd = s_odd[tile & 3];
-        const bool absent0 = here0 == nullptr, absent1 = here1 == nullptr;
-        if (any_fits) {
-#pragma unroll
-            for (int h = 0; h < 4; ++h)
-#pragma unroll
-                for (int t = 0; t < kColumns; ++t) s[h][t] *= back[t];
-        }
-        if (token0 < most_from || token0 + kTile > least_to || absent0 || absent1) {
+        const bool absent0 = here0 < 0, absent1 = here1 < 0;
+        uintx4 k_now[NS], k_next[NS];
+        key_parts(tile + 1, 0, k_now);
+        if (any_fits || token0 < most_from || token0 + kTile > least_to || absent0 || absent1) {
 #pragma unroll
             for (int h = 0; h < 4; ++h)
 #pragma unroll
@@ -256,7 +247,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
                     for (int i = 0; i < 4; ++i) {
                         const int at = token0 + h * 16 + c * 4 + i;
                         const bool seen = at >= seen_from[t] && at < seen_to[t] && !(h < 2 ? absent0 : absent1);
-                        s[h][t][i] = seen ? s[h][t][i] : -__builtin_inff();
+                        s[h][t][i] = seen ? s[h][t][i] * back[t] : -__builtin_inff();
                     }
         }
         bool move = false;
@@ -292,9 +283,10 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
                     for (int i = 0; i < 4; ++i) s[h][t][i] -= by;
             }
         }
+        // Exponentials of 16 tokens beside the products for the 16 before them of the next tile (past the last tile: of whatever stands there, not looked at), each
+        // step's parts of keys, then of values, read a step ahead
         uint32_t p[kColumns][2][4];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
+        auto exponentials = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < kColumns; ++t) {
                 float e[4];
@@ -303,33 +295,60 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
                 p[t][h >> 1][(h & 1) * 2] = __builtin_bit_cast(uint32_t, half2v{(_Float16)e[0], (_Float16)e[1]});
                 p[t][h >> 1][(h & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, half2v{(_Float16)e[2], (_Float16)e[3]});
             }
-            scores(tile + 1, h);                              // (past the last tile: of whatever stands there, not looked at)
-        }
+        };
+        constexpr int kAhead = NS < 4 ? NS : 4;               // parts of values read ahead
         const uint8_t *values = lds + (2 + (tile & 1)) * kTileBytes;
+        uintx4 v_now[kAhead], v_next[kAhead];
+        auto value_parts = [&](int n, uintx4 (&v)[kAhead]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            half8 ph[kColumns];
+            for (int i = 0; i < kAhead; ++i) v[i] = *reinterpret_cast<const uintx4 *>(values + (n + i) * 1024 + lane * 16);
+        };
+        exponentials(0);
 #pragma unroll
-            for (int t = 0; t < kColumns; ++t) {
-                ph[t] = __builtin_bit_cast(half8, uintx4{p[t][h][0], p[t][h][1], p[t][h][2], p[t][h][3]});
-                sum[t] = mfma(ones, ph[t], sum[t]);
+        for (int h = 0; h < 4; ++h) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (h < 3) { key_parts(tile + 1, h + 1, k_next); exponentials(h + 1); }
+            else value_parts(0, v_now);
+            scores(h, k_now);
+#pragma unroll
+            for (int j = 0; j < NS; ++j) k_now[j] = k_next[j];
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < NS * kColumns; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 4 / NS > 0 ? 4 / NS : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+            }
+        }
+        half8 ph[kColumns][2];
+#pragma unroll
+        for (int t = 0; t < kColumns; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                ph[t][h] = __builtin_bit_cast(half8, uintx4{p[t][h][0], p[t][h][1], p[t][h][2], p[t][h][3]});
+                sum[t] = mfma(ones, ph[t][h], sum[t]);
             }
 #pragma unroll
-            for (int n = 0; n < 2 * NS; ++n) {
-                const uintx4 v = *reinterpret_cast<const uintx4 *>(values + (h * 2 * NS + n) * 1024 + lane * 16);
+        for (int n = 0; n < 4 * NS; n += kAhead) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (n + kAhead < 4 * NS) value_parts(n + kAhead, v_next);
 #pragma unroll
-                for (int t = 0; t < kColumns; ++t) o[t][n] = mfma(v, ph[t], o[t][n]);
-            }
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int t = 0; t < kColumns; ++t) o[t][(n + i) % (2 * NS)] = mfma(v_now[i], ph[t][(n + i) / (2 * NS)], o[t][(n + i) % (2 * NS)]);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) v_now[i] = v_next[i];
+            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
         }
         if (__builtin_amdgcn_readfirstlane(odd) != 0u) {
             // NaN among the values: it reaches the rows that see its token, in the elements of its group
             for (int t64 = 0; t64 < kTile; ++t64) {
                 const int at = token0 + t64;
-                const uint8_t *rec = of(here0, here1, t64 >= kKvRecord);
-                if (rec == nullptr || at >= w.s.len) continue;
+                const int rec = of(here0, here1, t64 >= kKvRecord);
+                if (rec < 0 || at >= w.s.len) continue;
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    const uint32_t step = *reinterpret_cast<const uint32_t *>(rec + R::kValueSteps + g * 128 + (t64 & 31) * 4);
+                    const uint32_t step = *reinterpret_cast<const uint32_t *>(a.pool + (int64_t)rec * R::kBytes + R::kValueSteps + g * 128 + (t64 & 31) * 4);
                     if ((step & 0x7C00u) != 0x7C00u) continue;
 #pragma unroll
                     for (int t = 0; t < kColumns; ++t)
