@@ -420,7 +420,7 @@ WsLayout ws_layout(const KvShape &s, const KvBatch &b, int q_heads)
     l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
     if (s.act_bf16 && (int64_t)b.max_new * (q_heads / s.heads) > kStreamedRows) {
         const PromptPlan p = prompt_plan(s, b, q_heads / s.heads);
-        l.prompts = scratch_of((l.streamed.end + 255) / 256 * 256, p.target, s.heads, p.rows, s.head_dim);
+        if (p.cut) l.prompts = scratch_of((l.streamed.end + 255) / 256 * 256, p.target, s.heads, p.rows, s.head_dim);
     }
     return l;
 }

@@ -26,7 +26,7 @@ __device__ __forceinline__ half2v halves_of(uint32_t w, int p)
     return __builtin_elementwise_fma(x, half2v{by, by}, half2v{off, off});
 }
 
-template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_kv_prompt(const AttendArgs a)
+template <int NS, int SG, int kPromptWaves, int kColumns, bool CUT> __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_kv_prompt(const AttendArgs a)
 {
     using R = KvRecord<NS, SG>;
     constexpr int kUnitRows = kPromptWaves * kColumns * 16;
@@ -35,7 +35,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
     __shared__ uint32_t s_odd[4];                                             // tile & 3: a value of a token that is there is NaN
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, c = lane >> 4;
     const int head = blockIdx.x % a.heads;
-    const Work w = work_of(a, blockIdx.x / a.heads);
+    const Work w = work_of<CUT, false>(a, blockIdx.x / a.heads);
     if (!w.any) return;
     const int unit = (w.s.n * a.ratio + kUnitRows - 1) / kUnitRows - 1 - w.unit;        // the last rows, which see most, first
     // ---- this lane's rows -------------------------------------------------------------------------
@@ -375,57 +375,24 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
 #pragma unroll
         for (int n = 0; n < 2 * NS; ++n) o[t][n] *= 2.0f;
     }
-    if (w.chunks > 1) {
-        // as in the streamed kernel: parts and counter at device scope, the last workgroup to arrive adds up all parts in their order
-        __shared__ uint32_t s_last;
-        constexpr uint32_t kPart = kUnitRows * D * 4, kStats = kUnitRows * 8;
-        uint8_t *base = reinterpret_cast<uint8_t *>(a.parts), *stats = base + 2 * (int64_t)a.target * a.heads * kPart;
-        {
+    if constexpr (CUT) {
+        if (w.chunks > 1) {                                  // the join is a launch of its own: its bytes (a part is 32 KB and more) are too many for one workgroup
+            constexpr uint32_t kPart = kUnitRows * D * 4, kStats = kUnitRows * 8;
             const int64_t mine = (int64_t)w.part * a.heads + head;
-            const __amdgpu_buffer_rsrc_t dst = make_rsrc(base + mine * kPart, kPart), st = make_rsrc(stats + mine * kStats, kStats);
+            uint8_t *base = reinterpret_cast<uint8_t *>(a.parts), *stats = base + 2 * (int64_t)a.target * a.heads * kPart + mine * kStats;
+            base += mine * kPart;
 #pragma unroll
             for (int t = 0; t < kColumns; ++t) {
                 const int row = (wave * kColumns + t) * 16 + r;
 #pragma unroll
-                for (int n = 0; n < 2 * NS; ++n) {
-                    intx4 v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = __float_as_int(o[t][n][i]);
-                    __builtin_amdgcn_raw_buffer_store_b128(v, dst, (row * D + n * 16 + c * 4) * 4, 0, kAuxDeviceScope);
+                for (int j = 0; j < NS; ++j) {
+                    float *to = reinterpret_cast<float *>(base) + row * D + 32 * j + 8 * c;
+                    *reinterpret_cast<floatx4 *>(to) = floatx4{o[t][2 * j][0], o[t][2 * j + 1][0], o[t][2 * j][1], o[t][2 * j + 1][1]};
+                    *reinterpret_cast<floatx4 *>(to + 4) = floatx4{o[t][2 * j][2], o[t][2 * j + 1][2], o[t][2 * j][3], o[t][2 * j + 1][3]};
                 }
-                const intx2 v = {__float_as_int(top[t]), __float_as_int(total[t])};
-                if (c == 0) __builtin_amdgcn_raw_buffer_store_b64(v, st, row * 8, 0, kAuxDeviceScope);
+                if (c == 0) *reinterpret_cast<floatx2 *>(stats + row * 8) = floatx2{top[t], total[t]};
             }
-        }
-        wait_all_and_barrier();
-        uint32_t *counter = a.counters + (int64_t)w.counter * a.heads + head;
-        if (tid == 0) {
-            const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = before == (uint32_t)(w.chunks - 1) ? 1u : 0u;
-            if (s_last != 0u) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (s_last == 0u) return;
-#pragma unroll
-        for (int t = 0; t < kColumns; ++t) {
-            const int row = (wave * kColumns + t) * 16 + r;
-            top[t] = -3.0e38f; total[t] = 0.0f;
-#pragma unroll
-            for (int n = 0; n < 2 * NS; ++n) o[t][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-            for (int k = 0; k < w.chunks; ++k) {
-                const int64_t from = (int64_t)(w.part - w.chunk + k) * a.heads + head;
-                const __amdgpu_buffer_rsrc_t src = make_rsrc(base + from * kPart, kPart), st = make_rsrc(stats + from * kStats, kStats);
-                const intx2 ml = __builtin_amdgcn_raw_buffer_load_b64(st, row * 8, 0, kAuxDeviceScope);
-                const float next = fmaxf(top[t], __int_as_float(ml[0])), f = exp2_of(top[t] - next), g = exp2_of(__int_as_float(ml[0]) - next);
-                top[t] = next;
-                total[t] = __builtin_fmaf(__int_as_float(ml[1]), g, total[t] * f);
-#pragma unroll
-                for (int n = 0; n < 2 * NS; ++n) {
-                    const intx4 v = __builtin_amdgcn_raw_buffer_load_b128(src, (row * D + n * 16 + c * 4) * 4, 0, kAuxDeviceScope);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[t][n][i] = __builtin_fmaf(__int_as_float(v[i]), g, o[t][n][i] * f);
-                }
-            }
+            return;
         }
     }
 #pragma unroll
@@ -446,47 +413,90 @@ template <int NS, int SG, int kPromptWaves, int kColumns> __global__ __launch_bo
     }
 }
 
-template <int NS, int SG, int W, int C> void launch_t(const AttendArgs &a, hipStream_t st)
+// Sixteen rows of a unit that was cut, from its parts.
+template <int D> __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a)
 {
-    constexpr int smem = 4 * kTile * 32 * NS * 2;
-    allow_lds(reinterpret_cast<const void *>(&k_kv_prompt<NS, SG, W, C>), smem);
-    k_kv_prompt<NS, SG, W, C><<<dim3((unsigned)a.slots * (unsigned)a.heads), W * 64, smem, st>>>(a);
-}
-template <int NS, int SG> void launch(const AttendArgs &a, bool large, hipStream_t st)
-{
-    if constexpr (NS == 8) launch_t<NS, SG, kLargeWaves, large_columns(32 * NS)>(a, st);
-    else if (large) launch_t<NS, SG, kLargeWaves, large_columns(32 * NS)>(a, st);
-    else launch_t<NS, SG, kSmallWaves, 1>(a, st);
+    constexpr int kOut = D / 16;                             // elements of a thread
+    const int groups = 1 << (a.unit_bits - 4), head = blockIdx.x % a.heads, group = blockIdx.x / a.heads % groups, rows = 1 << a.unit_bits;
+    const Work w = work_of<true, true>(a, blockIdx.x / (a.heads * groups));
+    if (!w.any || w.chunks < 2) return;
+    const int unit = ((w.s.n * a.ratio + rows - 1) >> a.unit_bits) - 1 - w.unit;        // as in the kernel above
+    const int row = group * 16 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * kOut;
+    const int row_all = unit * rows + row, query = quotient(row_all, a.ratio), oh = head * a.ratio + (row_all - query * a.ratio);
+    if (query >= w.s.n) return;
+    const float *parts = a.parts + row * D + d0, *stats = a.parts + 2 * (int64_t)a.target * a.heads * rows * D + row * 2;
+    float m = -3.0e38f, l = 0.0f, x[kOut] = {};
+#pragma unroll 4
+    for (int k = 0; k < w.chunks; ++k) {
+        const int64_t from = (int64_t)(w.part + k) * a.heads + head;
+        const floatx2 ml = *reinterpret_cast<const floatx2 *>(stats + from * rows * 2);
+        floatx4 v[kOut / 4];
+#pragma unroll
+        for (int e = 0; e < kOut / 4; ++e) v[e] = *reinterpret_cast<const floatx4 *>(parts + from * rows * D + 4 * e);
+        const float next = fmaxf(m, ml[0]), f = exp2_of(m - next), g = exp2_of(ml[0] - next);
+        m = next;
+        l = __builtin_fmaf(ml[1], g, l * f);
+#pragma unroll
+        for (int e = 0; e < kOut; ++e) x[e] = __builtin_fmaf(v[e / 4][e % 4], g, x[e] * f);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    bf16_t *out = static_cast<bf16_t *>(a.out.p) + (int64_t)(w.s.first + query) * a.out.token_stride + (int64_t)oh * a.out.head_stride + d0;
+#pragma unroll
+    for (int e = 0; e < kOut; e += 4) {
+        bf16x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(x[e + i] * inv);
+        *reinterpret_cast<bf16x4 *>(out + e) = v;
+    }
+    if (a.lse != nullptr && d0 == 0)
+        a.lse[(int64_t)(w.s.first + query) * ((int64_t)a.heads * a.ratio) + oh] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
-int large_rows(const KvShape &s) { return kLargeWaves * large_columns(s.head_dim) * 16; }
-constexpr int kSmallRows = kSmallWaves * 16;
+template <int NS, int SG, int W, int C, bool CUT> void launch_t(const AttendArgs &a, bool join, int units, hipStream_t st)
+{
+    constexpr int smem = 4 * kTile * 32 * NS * 2;
+    allow_lds(reinterpret_cast<const void *>(&k_kv_prompt<NS, SG, W, C, CUT>), smem);
+    k_kv_prompt<NS, SG, W, C, CUT><<<dim3((unsigned)a.slots * (unsigned)a.heads), W * 64, smem, st>>>(a);
+    if (join) k_kv_join<32 * NS><<<dim3((unsigned)units * (W * C) * (unsigned)a.heads), 256, 0, st>>>(a);
+}
+template <int NS, int SG> void launch(const AttendArgs &a, const PromptPlan &p, int units, hipStream_t st)
+{
+    constexpr int kColumns = large_columns(32 * NS);
+    if (!p.small) launch_t<NS, SG, kLargeWaves, kColumns, false>(a, false, units, st);
+    else launch_t<NS, SG, NS == 8 ? kLargeWaves : kSmallWaves, 1, true>(a, p.cut, units, st);
+}
 
 }  // namespace
 
+// Workgroups of 256 rows where there is one for every compute unit, else of 64, two to a compute unit.  Where even those do not take half the places, sequences of more than
+// kFewest records are cut, and joined in a launch of its own (3 us).
+constexpr int kFewest = 16;
 PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio)
 {
+    const int large = kLargeWaves * large_columns(s.head_dim) * 16;
     PromptPlan p;
-    p.large = s.head_dim > 128 || (int64_t)units_at_most(b, ratio, large_rows(s)) * s.heads >= 256;
-    p.rows = p.large ? large_rows(s) : kSmallRows;
-    p.target = (256 * (p.large ? 1 : 2) + s.heads - 1) / s.heads;          // a workgroup on every compute unit, or two small ones
+    p.small = (int64_t)units_at_most(b, ratio, large) * s.heads < 256;
+    p.rows = p.small && s.head_dim <= 128 ? kSmallWaves * 16 : large;
+    p.target = ((s.head_dim <= 128 ? 512 : 256) + s.heads - 1) / s.heads;
+    p.cut = p.small && units_at_most(b, ratio, p.rows) < p.target / 2 && b.max_len > kFewest * kKvRecord;
     return p;
 }
 
 void launch_kv_prompt(const KvShape &s, AttendArgs a, hipStream_t st)
 {
     const PromptPlan p = prompt_plan(s, a.b, a.ratio);
+    const int units = units_at_most(a.b, a.ratio, p.rows);
     a.unit_bits = __builtin_ctz(p.rows);
-    a.fewest = 8;
+    a.fewest = p.cut ? kFewest : 1 << 30;
     a.target = p.target;
-    a.slots = p.target + units_at_most(a.b, a.ratio, p.rows);
+    a.slots = (p.cut ? p.target : 0) + units;
     const int sg = s.group / 32;
     switch (s.head_dim) {
-    case 64: if (sg == 1) launch<2, 1>(a, p.large, st); else launch<2, 2>(a, p.large, st); break;
-    case 128: if (sg == 1) launch<4, 1>(a, p.large, st); else if (sg == 2) launch<4, 2>(a, p.large, st); else launch<4, 4>(a, p.large, st); break;
+    case 64: if (sg == 1) launch<2, 1>(a, p, units, st); else launch<2, 2>(a, p, units, st); break;
+    case 128: if (sg == 1) launch<4, 1>(a, p, units, st); else if (sg == 2) launch<4, 2>(a, p, units, st); else launch<4, 4>(a, p, units, st); break;
     default:
-        if (sg == 1) launch<8, 1>(a, p.large, st); else if (sg == 2) launch<8, 2>(a, p.large, st);
-        else if (sg == 4) launch<8, 4>(a, p.large, st); else launch<8, 8>(a, p.large, st);
+        if (sg == 1) launch<8, 1>(a, p, units, st); else if (sg == 2) launch<8, 2>(a, p, units, st);
+        else if (sg == 4) launch<8, 4>(a, p, units, st); else launch<8, 8>(a, p, units, st);
     }
 }
 

@@ -53,7 +53,7 @@ __device__ __forceinline__ floatx4 mfma(const uintx4 &a, const half8 &b, const f
 
 // How the work of a call is divided: a unit is up to 2^unit_bits rows of a sequence (times every head of the cache), its records are cut into chunks of C, and a workgroup
 // takes a chunk.  C follows from the lengths as they are on the device, so that the chunks of all sequences are about `target` in all, however their lengths differ.
-struct Work { int b, unit, chunk, chunks, first, last, part, counter; KvSeq s; bool any; };
+struct Work { int b, unit, chunk, chunks, first, last, part; KvSeq s; bool any; };
 
 struct Extent { int units, lo, hi; };
 __device__ __forceinline__ Extent extent_of(const AttendArgs &a, const KvSeq &s)
@@ -66,7 +66,8 @@ __device__ __forceinline__ Extent extent_of(const AttendArgs &a, const KvSeq &s)
     return e;
 }
 
-__device__ __forceinline__ Work work_of(const AttendArgs &a, int slot)
+// CUT: units may be cut.  UNITS: the unit with number `slot` as a whole; else the chunk
+template <bool CUT, bool UNITS> __device__ __forceinline__ Work work_of(const AttendArgs &a, int slot)
 {
     const int lane = threadIdx.x & 63, page_tokens = a.page_records * kKvRecord;
     KvSeq s{};
@@ -76,35 +77,39 @@ __device__ __forceinline__ Work work_of(const AttendArgs &a, int slot)
         s = KvSeq{}; e = Extent{};
         if (b < a.b.sequences) { s = kv_seq(a.b, page_tokens, b); e = extent_of(a, s); }
     };
-    float records = 0.0f;                                // in all, up to rounding: every workgroup adds them up in the same order
-    for (int base = 0; base < a.b.sequences; base += 64) { look(base); records += (float)e.units * (float)(e.hi - e.lo); }
-    records = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(records)), 63));
-    // at least records / target whatever the rounding: the room for parts depends on it
-    const int C = max((int)fminf(records / (float)a.target * 1.00001f, 1.0e9f) + 1, a.fewest);
+    int C = 1 << 30;
+    if constexpr (CUT) {
+        float records = 0.0f;                            // in all, up to rounding: every workgroup adds them up in the same order
+        int units = 0;
+        for (int base = 0; base < a.b.sequences; base += 64) { look(base); records += (float)e.units * (float)(e.hi - e.lo); units += e.units; }
+        records = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(records)), 63));
+        units = __builtin_amdgcn_readlane(lane_sums(units), 63);
+        // every unit has one chunk that may be a small one; at least records / target whatever the rounding: the room for parts depends on it
+        C = max((int)fminf(records / (float)max(a.target - units, a.target / 2) * 1.00001f, 1.0e9f) + 1, a.fewest);
+    }
     Work w{};
-    int before = 0, parts = 0, counters = 0;
+    int before = 0, parts = 0;
     for (int base = 0; base < a.b.sequences; base += 64) {
-        if (a.b.sequences > 64) look(base);
-        const int chunks = e.units > 0 ? max(1, (e.hi - e.lo + C - 1) / C) : 0, mine = e.units * chunks, cut = chunks > 1 ? e.units : 0;
-        const int x = lane_sums(mine), y = lane_sums(cut * chunks), z = lane_sums(cut);
+        if (!CUT || a.b.sequences > 64) look(base);
+        const int recs = e.hi - e.lo, chunks = !CUT ? min(e.units, 1) : e.units > 0 ? max(1, quotient(recs + C - 1, C)) : 0;
+        const int mine = UNITS ? e.units : e.units * chunks, x = lane_sums(mine), y = CUT ? lane_sums(chunks > 1 ? e.units * chunks : 0) : 0;
         const int at = slot - before - (x - mine);       // this slot within the sequence of the lane
         const uint64_t has = __ballot(at >= 0 && at < mine);
         if (has != 0) {
             const int src = __ffsll((unsigned long long)has) - 1;
             auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
-            const int i = of(at);
+            const int i = of(at), each = quotient(of(recs) + of(chunks) - 1, of(chunks));
             w.any = true;
             w.b = base + src;
             w.chunks = of(chunks);
-            w.unit = w.chunks == 1 ? i : i / w.chunks;
-            w.chunk = i - w.unit * w.chunks;
+            w.unit = UNITS || w.chunks == 1 ? i : quotient(i, w.chunks);
+            w.chunk = UNITS ? 0 : i - w.unit * w.chunks;
             w.s.first = of(s.first); w.s.n = of(s.n); w.s.len = of(s.len);
-            w.first = of(e.lo) + w.chunk * C;
-            w.last = min(of(e.hi), w.first + C);
-            w.part = parts + of(y - cut * chunks) + i;
-            w.counter = counters + of(z - cut) + w.unit;
+            w.first = of(e.lo) + w.chunk * each;
+            w.last = min(of(e.hi), w.first + each);
+            if constexpr (CUT) w.part = parts + of(y - (chunks > 1 ? mine * (UNITS ? chunks : 1) : 0)) + w.unit * w.chunks + w.chunk;
         }
-        before += __builtin_amdgcn_readlane(x, 63); parts += __builtin_amdgcn_readlane(y, 63); counters += __builtin_amdgcn_readlane(z, 63);
+        before += __builtin_amdgcn_readlane(x, 63); parts += __builtin_amdgcn_readlane(y, 63);
     }
     w.any = w.any && before <= a.slots;                  // more than the host was told of: nothing is computed
     return w;
@@ -223,7 +228,7 @@ void allow_lds(const void *kernel, int bytes)
 }  // namespace
 
 // ---- kv_prompt.hip ---------------------------------------------------------------------------
-struct PromptPlan { int rows, target; bool large; };         // rows of a unit; chunks aimed at for a head of the cache
+struct PromptPlan { int rows, target; bool small, cut; };    // rows of a unit; chunks aimed at for a head of the cache; workgroups of few rows; units may be cut
 PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio);
 void launch_kv_prompt(const KvShape &s, AttendArgs a, hipStream_t st);
 
