@@ -409,19 +409,25 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
 // shares of the work of a head of the cache
 int shares_of(const KvShape &s) { return (kResident + s.heads - 1) / s.heads; }
 
-// Sequences with more rows than this go to the kernel that rebuilds keys and values (bf16).
+// Sequences of more rows than this go to the kernel that rebuilds keys and values (bf16): for 64 rows this one takes 13.6 us and that one 22.6 (8000 tokens, 8 heads of
+// the cache), 9 and 17 us (500 tokens).
 constexpr int kStreamedRows = 64;
+// Where a call's units of 16 rows are no more than two for every compute unit, and its caches long, no sequence does: 256 rows of four sequences at 2000 tokens 31 us and 37,
+// 800 rows at 4000 44 and 49, but 2700 rows at 333 tokens 40 and 18.5.
+bool has_prompts(const KvShape &s, const KvBatch &b, int ratio)
+{
+    if (!s.act_bf16 || (int64_t)b.max_new * ratio <= kStreamedRows) return false;
+    return b.max_len < 2048 || (int64_t)units_at_most(b, ratio, kRowsOfUnit) * s.heads > 2 * kResident;
+}
 
+// The workspace does not depend on which kernels a batch takes: what serves a batch serves every smaller one.
 struct WsLayout { Scratch streamed, prompts; };
-WsLayout ws_layout(const KvShape &s, const KvBatch &b, int q_heads)
+WsLayout ws_layout(const KvShape &s, const KvBatch &b, int ratio)
 {
     WsLayout l;
     l.streamed = scratch_of(0, shares_of(s), s.heads, kRowsOfUnit, s.head_dim);
     l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
-    if (s.act_bf16 && (int64_t)b.max_new * (q_heads / s.heads) > kStreamedRows) {
-        const PromptPlan p = prompt_plan(s, b, q_heads / s.heads);
-        if (p.cut) l.prompts = scratch_of((l.streamed.end + 255) / 256 * 256, p.target, s.heads, p.rows, s.head_dim);
-    }
+    if (s.act_bf16 && (int64_t)b.max_new * ratio > kStreamedRows) l.prompts = prompt_scratch(s, (l.streamed.end + 255) / 256 * 256);
     return l;
 }
 
@@ -439,11 +445,11 @@ template <int NS, int SG> void launch(const KvShape &s, const AttendArgs &a, hip
 
 }  // namespace
 
-size_t kv_attend_ws_bytes(const KvShape &s, const KvBatch &b, int q_heads) { return ws_layout(s, b, q_heads).prompts.end; }
+size_t kv_attend_ws_bytes(const KvShape &s, const KvBatch &b, int q_heads) { return ws_layout(s, b, q_heads / s.heads).prompts.end; }
 
 void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &t, const void *pool, void *ws, hipStream_t st)
 {
-    const WsLayout l = ws_layout(s, b, t.q_heads);
+    const WsLayout l = ws_layout(s, b, t.q_heads / s.heads);
     AttendArgs a;
     a.b = b; a.q = t.q; a.out = t.out; a.lse = t.lse;
     a.pool = static_cast<const uint8_t *>(pool);
@@ -453,7 +459,7 @@ void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &t, con
         a.counters = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ws) + x.counters);
         a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + x.parts);
     };
-    const bool prompts = s.act_bf16 && (int64_t)b.max_new * a.ratio > kStreamedRows;
+    const bool prompts = has_prompts(s, b, a.ratio);
     if (prompts) {
         a.from_rows = kStreamedRows + 1; a.to_rows = INT32_MAX;
         scratch(l.prompts);

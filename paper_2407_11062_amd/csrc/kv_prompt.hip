@@ -452,6 +452,8 @@ template <int D> __global__ __launch_bounds__(256) void k_kv_join(const AttendAr
         a.lse[(int64_t)(w.s.first + query) * ((int64_t)a.heads * a.ratio) + oh] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
+struct PromptPlan { int rows, target; bool small, cut; };    // rows of a unit; chunks aimed at for a head of the cache; workgroups of few rows; units may be cut
+
 template <int NS, int SG, int W, int C, bool CUT> void launch_t(const AttendArgs &a, bool join, int units, hipStream_t st)
 {
     constexpr int smem = 4 * kTile * 32 * NS * 2;
@@ -466,8 +468,6 @@ template <int NS, int SG> void launch(const AttendArgs &a, const PromptPlan &p, 
     else launch_t<NS, SG, NS == 8 ? kLargeWaves : kSmallWaves, 1, true>(a, p.cut, units, st);
 }
 
-}  // namespace
-
 // Workgroups of 256 rows where there is one for every compute unit, else of 64, two to a compute unit.  Where even those do not take half the places, sequences of more than
 // kFewest records are cut, and joined in a launch of its own (3 us).
 constexpr int kFewest = 16;
@@ -480,6 +480,14 @@ PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio)
     p.target = ((s.head_dim <= 128 ? 512 : 256) + s.heads - 1) / s.heads;
     p.cut = p.small && units_at_most(b, ratio, p.rows) < p.target / 2 && b.max_len > kFewest * kKvRecord;
     return p;
+}
+}  // namespace
+
+Scratch prompt_scratch(const KvShape &s, size_t at)
+{
+    const KvBatch none{};                                     // no units: the plan of the most that is cut
+    const PromptPlan p = prompt_plan(s, none, 1);
+    return scratch_of(at, p.target, s.heads, p.rows, s.head_dim);
 }
 
 void launch_kv_prompt(const KvShape &s, AttendArgs a, hipStream_t st)

@@ -22,6 +22,18 @@ struct AttendArgs {
     float scale;                                   // times log2(e)
 };
 
+// Where a launch's counters and parts lie in the workspace.  There is at most one cut unit per chunk aimed at, and a cut unit has fewer than twice its share of them.
+struct Scratch { size_t counters, parts, end; };
+inline Scratch scratch_of(size_t at, int target, int heads, int unit_rows, int head_dim)
+{
+    const size_t chunks = (size_t)target * heads;
+    Scratch l;
+    l.counters = at;
+    l.parts = at + (chunks * 4 + 255) / 256 * 256;
+    l.end = l.parts + 2 * chunks * (size_t)unit_rows * (size_t)(head_dim * 4 + 8);
+    return l;
+}
+
 namespace {
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -199,18 +211,6 @@ int units_at_most(const KvBatch &b, int ratio, int unit_rows)
     return (int)(each < all ? each : all);
 }
 
-// Where a launch's counters and parts lie in the workspace.  There is at most one cut unit per chunk aimed at, and a cut unit has fewer than twice its share of them.
-struct Scratch { size_t counters, parts, end; };
-Scratch scratch_of(size_t at, int target, int heads, int unit_rows, int head_dim)
-{
-    const size_t chunks = (size_t)target * heads;
-    Scratch l;
-    l.counters = at;
-    l.parts = at + (chunks * 4 + 255) / 256 * 256;
-    l.end = l.parts + 2 * chunks * (size_t)unit_rows * (size_t)(head_dim * 4 + 8);
-    return l;
-}
-
 // more LDS than the default has to be asked for, once on every device
 void allow_lds(const void *kernel, int bytes)
 {
@@ -228,8 +228,7 @@ void allow_lds(const void *kernel, int bytes)
 }  // namespace
 
 // ---- kv_prompt.hip ---------------------------------------------------------------------------
-struct PromptPlan { int rows, target; bool small, cut; };    // rows of a unit; chunks aimed at for a head of the cache; workgroups of few rows; units may be cut
-PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio);
+Scratch prompt_scratch(const KvShape &s, size_t at);
 void launch_kv_prompt(const KvShape &s, AttendArgs a, hipStream_t st);
 
 }  // namespace eqat

@@ -27,7 +27,8 @@ def attention(q, k, v, g, scale=None, causal=True, window=0, gone=None):
     """One sequence: q [n, Hq, D] stand at its last n positions, k and v [L, H, D] as they were written; gone: positions that are not there.
     Returns out, lse, and bounds on their errors (apart from the rounding of out to its type): the scores are binary32 sums of |q| (|m| + s c) terms,
     and the weights of the sums over codes are rounded to 11 bits (bf16) or 22 (fp32).  A bf16 sequence of more than 64 rows (query, head that shares a head of the
-    cache) has its keys and values rebuilt as binary16: 2^-12 of every |q| |k^| in a score, 2^-12 of a value."""
+    cache) may have its keys and values rebuilt as binary16, its queries held so with the scale in them, and sums its rounded p: 2^-11 of every |q| |k^| in a score,
+    2^-12 of a value, and of the sum in lse."""
     n, Hq, D = q.shape
     L, H = k.shape[:2]
     R = Hq // H
@@ -65,8 +66,8 @@ def attention(q, k, v, g, scale=None, causal=True, window=0, gone=None):
             out[i, h] = p @ V[at]
             eps = 2.0 ** -21 * float((size[at, h // R] @ Q[i].abs()).max()) * scale       # of a score: 2^-22 for either of its two sums
             if rebuilt:
-                eps += 2.0 ** -12 * float((K[at].abs() @ Q[i].abs()).max()) * scale + 2.0 ** -24
+                eps += 2.0 ** -11 * float((K[at].abs() @ Q[i].abs()).max()) * scale + 2.0 ** -24
             weights = p @ span[at, h // R]
             tol_o[i, h] = weights * (r + 2 * eps + 2.0 ** -19)
-            tol_l[i, h] = eps + 2.0 ** -20 * (1 + lse[i, h].abs())
+            tol_l[i, h] = eps + 2.0 ** -20 * (1 + lse[i, h].abs()) + (2.0 ** -12 if rebuilt else 0.0)
     return out, lse, tol_o, tol_l

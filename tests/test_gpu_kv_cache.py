@@ -262,6 +262,75 @@ def test_prompts(D, g, T, ratio, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("seqs,H,ratio", [([(70, 2600)], 2, 4), ([(33, 2100), (3, 2500), (0, 9)], 1, 8), ([(100, 900), (90, 700)], 1, 3)])
+def test_prompts_behind_long_pasts(seqs, H, ratio, dtype):
+    """units cut over workgroups and joined, by the kernel that streams (from 2048 positions on) and by the one that rebuilds"""
+    check(Setup(seqs, H, 128, 64, dtype, page=64, seed=sum(map(sum, seqs))).fill(), ratio)
+
+
+def close_to_fp32(s, q, b, window, nan=False):
+    """A prompt in bf16 against the same values in fp32, whose kernel rebuilds nothing and is held to 64 bits above: the bounds of the rounding to binary16 and bf16."""
+    out = eq.eqat_kv_attention(s.cache, b, q, window=window)
+    twin = eq.KvCache(s.H, s.D, s.g, s.page, s.cache.desc.pages, dtype=torch.float32)
+    eq.eqat_kv_write(twin, s.batch(s.lens), torch.cat(s.k).float().cuda(), torch.cat(s.v).float().cuda())
+    exact = eq.eqat_kv_attention(twin, b, q.float(), window=window)
+    assert torch.equal(out.isnan(), exact.isnan())
+    held = ref.held(torch.cat(s.k), s.g).cuda().float().nan_to_num().abs().transpose(0, 1)                    # [H, L, D]
+    R = q.shape[1] // s.H
+    most = torch.stack([(q[:, h].float().abs() @ held[h // R].T.contiguous()).amax(-1) for h in range(q.shape[1])], 1) / math.sqrt(s.D)
+    vs, vm, vc = ref.steps(torch.cat(s.v), s.g)
+    span = (vm.abs().unsqueeze(-1) + vs.unsqueeze(-1) * vc).nan_to_num().max().item()
+    bound = span * (2.0 ** -11 + 2 * (2.0 ** -11 * most[..., None] + 2.0 ** -18)) + 2.0 ** -8 * exact.abs()       # a key and a query: 2^-12 each
+    assert ((out.float() - exact).abs().nan_to_num() <= bound.nan_to_num(nan=1.0)).all()
+    return out
+
+
+@pytest.mark.parametrize("D,g", GRID)
+@pytest.mark.parametrize("window", [0, 200])
+def test_large_prompts(D, g, window):
+    """workgroups of 256 rows (heads of 256: 128): a sequence whose last rows leave most of one empty, one shorter than a tile, one behind a past"""
+    seqs = [(1061, 1061), (40, 40), (300, 777)]
+    s = Setup(seqs, 8, D, g, torch.bfloat16, page=96, seed=D + g).fill()
+    q = rows(s.gen, sum(n for n, _ in seqs), 64, D, torch.bfloat16).cuda()
+    close_to_fp32(s, q, s.batch([n for n, _ in seqs]), window)
+
+
+def test_large_prompts_with_values_and_keys_that_are_not_finite():
+    def bad(xs):
+        xs[0][1030:, :, 3] = math.nan
+        xs[0][500, 2] = math.inf
+        xs[1][39, 0, 100] = math.nan
+    seqs = [(1061, 1061), (40, 40)]
+    for kw in (dict(value_edit=bad), dict(key_edit=bad)):
+        s = Setup(seqs, 8, 128, 64, torch.bfloat16, seed=3, **kw).fill()
+        q = rows(s.gen, 1101, 64, 128, torch.bfloat16).cuda()
+        for window in (0, 300):
+            out = close_to_fp32(s, q, s.batch([1061, 40]), window)
+            assert not out[:500].isnan().any() and out.isnan().any()
+
+
+def test_large_and_small_queries_in_prompts():
+    """rows whose scores would leave binary16, or lie below it, with the scale in them"""
+    s = Setup([(200, 200)], 2, 128, 64, torch.bfloat16).fill()
+    def sizes(q):
+        q[::3] *= 1e-5
+        q[1::7] *= 1e6
+        q[5] = 0
+    check(s, 2, q_edit=sizes)
+
+
+def test_a_workspace_serves_smaller_batches():
+    s = Setup([(3000, 3000), (200, 2100)], 2, 128, 64, torch.bfloat16).fill()
+    heads = 8
+    ws = eq.kv_workspace(s.cache, s.batch([3000, 200]), heads)
+    for counts, lens in (([3000, 200], [3000, 2100]), ([100, 30], [600, 2100]), ([1, 1], [3000, 2100]), ([17, 0], [40, 0]), ([300, 0], [700, 0])):
+        b = s.batch(counts, lens=lens)
+        q = rows(s.gen, sum(counts), heads, 128, torch.bfloat16).cuda()
+        assert len(eq.kv_workspace(s.cache, b, heads)) <= len(ws)
+        assert torch.equal(eq.eqat_kv_attention(s.cache, b, q, ws=ws), eq.eqat_kv_attention(s.cache, b, q))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n", [1, 6, 150])
 def test_what_a_query_does_not_see_does_not_reach_it(n, dtype):
     """NaN and infinities in later keys and values, and in those that a window leaves out"""
