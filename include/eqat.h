@@ -454,7 +454,8 @@ eqat_status eqat_kv_read(const eqat_kv_desc *d, const eqat_kv_batch *b, void *K,
  * Softmax attention of the newest tokens' queries over what their sequences hold (write first, then attend):
  *   out[t, h] = sum over j of softmax_j(scale q[t, h] . k^_j) v^_j,   lse[t, h] = ln(sum over j of exp(scale q . k^_j)),
  * j over the positions that the query, at position lens[b] - (new tokens) + (its place among them), sees.  A query that sees none gives zeros and lse -inf.
- * NaN or infinities at positions that a query does not see do not reach it.  Scores, softmax and sums are binary32.
+ * NaN or infinities at positions that a query does not see do not reach it.  Scores, softmax and sums are binary32.  With fp32 tensors the results are as near as
+ * binary32 arithmetic; with bf16 p is rounded to 11 bits, and in sequences of more than 64 rows (new tokens x q_heads / heads) so may be queries, keys and values.
  *   Q, out: [tokens, q_heads, head_dim];  lse: [tokens, q_heads] contiguous, or NULL.
  *   ws: eqat_kv_workspace_bytes bytes (independent of the batch but for max_new and max_len), 256-byte aligned, ZEROED ONCE by the caller before its first use.  Every call
  *   leaves the counters in it at zero; calls that share a workspace must not overlap in time.

@@ -36,7 +36,7 @@ eqat_status check_batch(const eqat_kv_batch *b, const KvShape &s, KvBatch *k)
 {
     if (b == nullptr) return EQAT_ERR_NULL;
     if (b->tokens < 0 || b->sequences < 0 || b->table_stride < 0 || b->max_new < 0 || b->max_len < 0) return EQAT_ERR_SHAPE;
-    if (b->tokens * s.heads >= kMost || b->max_len > INT32_MAX - 32) return EQAT_ERR_SHAPE;
+    if (b->tokens >= kMost || b->tokens * s.heads >= kMost / 4 || b->max_len > INT32_MAX - 32) return EQAT_ERR_SHAPE;
     if (b->tokens > 0 && b->sequences == 0) return EQAT_ERR_SHAPE;
     if (b->sequences > 0 && (b->lens == nullptr || b->starts == nullptr || (b->table == nullptr && b->table_stride > 0))) return EQAT_ERR_NULL;
     if (!aligned(b->table, 4) || !aligned(b->lens, 4) || !aligned(b->starts, 4)) return EQAT_ERR_ALIGN;
@@ -68,7 +68,7 @@ eqat_status check_heads(const KvShape &s, const KvBatch &b, int q_heads)
     // the streamed kernel counts the records of all units of 16 rows; a bf16 sequence of more than 64 rows is not its business
     const double units = s.act_bf16 ? 4.0 * b.sequences : (double)(b.tokens * ratio) / 16 + b.sequences;
     if (units * (b.max_len / 32 + 1.0) > 2.0e9) return EQAT_ERR_SHAPE;
-    if (b.tokens * q_heads >= kMost || (int64_t)b.max_new * ratio >= kMost || ((int64_t)b.sequences + b.tokens * ratio / 16 + 2048) * s.heads >= kMost) return EQAT_ERR_SHAPE;
+    if (b.tokens * q_heads >= kMost || (int64_t)b.max_new * ratio >= kMost / 2 || ((int64_t)b.sequences + b.tokens * ratio / 16 + 2048) * s.heads >= kMost) return EQAT_ERR_SHAPE;
     return EQAT_OK;
 }
 

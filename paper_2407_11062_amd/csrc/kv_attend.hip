@@ -434,7 +434,8 @@ WsLayout ws_layout(const KvShape &s, const KvBatch &b, int ratio)
 template <int NS, int SG, bool F32> void launch_t(const AttendArgs &a, hipStream_t st)
 {
     constexpr int D = 32 * NS, kWaves = waves_of(D), rings = kWaves * depth_of(D) * KvRecord<NS, SG>::kBytes, sums = kWaves * kRowsOfUnit * (D + 4) * 4, smem = rings > sums ? rings : sums;
-    allow_lds(reinterpret_cast<const void *>(&k_kv_attend<NS, SG, F32>), smem);
+    static std::atomic<uint64_t> asked{0};
+    allow_lds(asked, reinterpret_cast<const void *>(&k_kv_attend<NS, SG, F32>), smem);
     k_kv_attend<NS, SG, F32><<<dim3((unsigned)a.slots * (unsigned)a.heads), kWaves * 64, smem, st>>>(a);
 }
 template <int NS, int SG> void launch(const KvShape &s, const AttendArgs &a, hipStream_t st)

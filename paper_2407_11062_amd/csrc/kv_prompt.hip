@@ -457,7 +457,8 @@ struct PromptPlan { int rows, target; bool small, cut; };    // rows of a unit; 
 template <int NS, int SG, int W, int C, bool CUT> void launch_t(const AttendArgs &a, bool join, int units, hipStream_t st)
 {
     constexpr int smem = 4 * kTile * 32 * NS * 2;
-    allow_lds(reinterpret_cast<const void *>(&k_kv_prompt<NS, SG, W, C, CUT>), smem);
+    static std::atomic<uint64_t> asked{0};
+    allow_lds(asked, reinterpret_cast<const void *>(&k_kv_prompt<NS, SG, W, C, CUT>), smem);
     k_kv_prompt<NS, SG, W, C, CUT><<<dim3((unsigned)a.slots * (unsigned)a.heads), W * 64, smem, st>>>(a);
     if (join) k_kv_join<32 * NS><<<dim3((unsigned)units * (W * C) * (unsigned)a.heads), 256, 0, st>>>(a);
 }

@@ -3,8 +3,7 @@
 #include "gemm_tiles.h"
 #include "kv.h"
 
-#include <mutex>
-#include <vector>
+#include <atomic>
 
 namespace eqat {
 
@@ -211,18 +210,14 @@ int units_at_most(const KvBatch &b, int ratio, int unit_rows)
     return (int)(each < all ? each : all);
 }
 
-// more LDS than the default has to be asked for, once on every device
-void allow_lds(const void *kernel, int bytes)
+// more LDS than the default has to be asked for, once on every device; `asked`: a bit per device, of the kernel
+inline void allow_lds(std::atomic<uint64_t> &asked, const void *kernel, int bytes)
 {
-    struct Asked { const void *kernel; int dev; };
-    static std::mutex mutex;
-    static std::vector<Asked> asked;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return;
-    std::lock_guard<std::mutex> lock(mutex);
-    for (const Asked &x : asked)
-        if (x.kernel == kernel && x.dev == dev) return;
-    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) asked.push_back(Asked{kernel, dev});
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if ((asked.load(std::memory_order_relaxed) & bit) != 0) return;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) asked.fetch_or(bit, std::memory_order_relaxed);
 }
 
 }  // namespace

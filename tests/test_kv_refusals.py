@@ -117,3 +117,15 @@ def test_the_binding_refuses_other_tensors():
         eq.KvBatch(i32(2, 3), i32(2), i32(2), 4, 2, 100)
     with pytest.raises(ValueError):
         eq.KvBatch(i32(2, 3), i32(2), i32(3), 4, 2, 100)               # not on the device
+
+
+def test_what_is_numbered_in_32_bits():
+    """records, rows and workgroups: the first count that does not fit is refused, in the products too"""
+    assert eq.lib().eqat_kv_pool_bytes(ctypes.byref(desc(pages=(1 << 24) - 1, heads=64))) > 0                       # 2^31 - 128 records
+    assert eq.lib().eqat_kv_pool_bytes(ctypes.byref(desc(pages=1 << 24, heads=64))) == 0                            # 2^31
+    wide = desc(heads=1 << 16, head_dim=64, group=64)
+    assert write(wide, batch(tokens=1 << 13), ks=strides(), vs=strides()) == SHAPE and write(wide, batch(tokens=(1 << 13) - 1), ks=strides(), vs=strides(), pool=None) == NULL
+    assert write(desc(), batch(tokens=1 << 62), ks=strides(), vs=strides()) == SHAPE                                # times the heads: not an overflow
+    one = desc(heads=1)
+    assert attend(one, batch(sequences=1, max_new=1 << 20), q_heads=1 << 10, qs=strides(), os_=strides()) == SHAPE
+    assert attend(one, batch(sequences=1, max_new=(1 << 20) - 1), q_heads=1 << 10, qs=strides(), os_=strides(), pool=None) == NULL
