@@ -156,14 +156,23 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int slot, Lane l)
     about = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(about)), 63));
     if (records == 0 || about > 2.1e9f) return Share{0, 0, 1, true};          // (more than the host was told of: nothing is computed)
     const int size = max(quotient(records + a.slots - 1, a.slots), a.fewest);
-    for (int larger = size; larger <= size + kSpare; larger += max(1, larger >> 4)) {
+    auto shares_of_size = [&](int larger) {
         int shares = 0;
         for (int base = 0; base < a.b.sequences; base += 64) {
             if (a.b.sequences > 64) l = lane_of(a, base);
             shares += l.e.units * max(1, quotient(l.e.hi - l.e.lo + larger - 1, larger));
         }
-        shares = __builtin_amdgcn_readlane(lane_sums(shares), 63);
-        if (shares <= a.slots) return slot < shares ? Share{slot * larger, (slot + 1) * larger, larger, true} : Share{0, 0, 1, true};
+        return __builtin_amdgcn_readlane(lane_sums(shares), 63);
+    };
+    // the smallest such size, by halves: a larger size never has more shares
+    int low = size, high = size, shares = shares_of_size(size);
+    if (shares > a.slots) { high = size + kSpare; shares = shares_of_size(high); low = size + 1; }
+    if (shares <= a.slots) {
+        while (low < high) {
+            const int half = (low + high) >> 1, of_half = shares_of_size(half);
+            if (of_half <= a.slots) { high = half; shares = of_half; } else { low = half + 1; }
+        }
+        return slot < shares ? Share{slot * high, (slot + 1) * high, high, true} : Share{0, 0, 1, true};
     }
     return Share{(int)min((int64_t)slot * size, (int64_t)records), (int)min((int64_t)(slot + 1) * size, (int64_t)records), size, false};
 }
