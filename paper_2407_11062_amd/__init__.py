@@ -453,8 +453,8 @@ class KvCache:
         if n == 0:
             raise ValueError(f"eqat_kv_pool_bytes: no cache of {heads} heads of {head_dim}, groups of {group}, {pages} pages of {page_tokens} tokens")
         self.pool = torch.empty(n, dtype=torch.uint8, device=device) if pool is None else pool
-        if self.pool.numel() < n:
-            raise ValueError(f"the pool needs {n} bytes")
+        if self.pool.dtype != torch.uint8 or not self.pool.is_contiguous() or self.pool.numel() < n:
+            raise ValueError(f"the pool is a contiguous uint8 tensor of at least {n} bytes")
 
 
 class KvBatch:

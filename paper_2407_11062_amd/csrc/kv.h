@@ -23,6 +23,8 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 
 constexpr int kKvRecord = 32;        // tokens
+constexpr int kKvBeginning = 32;     // records' time that the beginning and end of a unit take (kv_work.h)
+constexpr double kKvMostPlaces = 2.0e9;   // records and beginnings of all units of a call, counted in 32 bits
 
 struct KvShape {
     int heads, head_dim, group, groups, page_records;

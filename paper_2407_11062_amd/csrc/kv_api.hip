@@ -65,9 +65,9 @@ eqat_status check_heads(const KvShape &s, const KvBatch &b, int q_heads)
 {
     if (q_heads < s.heads || q_heads % s.heads != 0 || q_heads > 1 << 20) return EQAT_ERR_SHAPE;
     const int64_t ratio = q_heads / s.heads;
-    // the streamed kernel counts the records of all units of 16 rows; a bf16 sequence of more than 64 rows is not its business
+    // the streamed kernel counts the places of all units of 16 rows; a bf16 sequence of more than 64 rows is its business only where they fit
     const double units = s.act_bf16 ? 4.0 * b.sequences : (double)(b.tokens * ratio) / 16 + b.sequences;
-    if (units * (b.max_len / 32 + 1.0) > 2.0e9) return EQAT_ERR_SHAPE;
+    if (units * (b.max_len / 32 + 1.0 + eqat::kKvBeginning) > eqat::kKvMostPlaces) return EQAT_ERR_SHAPE;
     if (b.tokens * q_heads >= kMost || (int64_t)b.max_new * ratio >= kMost / 2 || ((int64_t)b.sequences + b.tokens * ratio / 16 + 2048) * s.heads >= kMost) return EQAT_ERR_SHAPE;
     return EQAT_OK;
 }

@@ -63,6 +63,7 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
     for (int at = mine.first; at < mine.last; at = w.to) {
         w = segment_of(a, mine, at, sequences);
         if (!w.any) return;
+        if (w.to <= w.unit_from) continue;                        // the unit's records are the next workgroup's
         // ---- this lane's row of the queries -----------------------------------------------------------
         const int row = w.unit * kRowsOfUnit + r, query = quotient(row, a.ratio), of_group = row - query * a.ratio;
         const bool is_row = query < w.s.n;
@@ -417,7 +418,8 @@ constexpr int kStreamedRows = 64;
 bool has_prompts(const KvShape &s, const KvBatch &b, int ratio)
 {
     if (!s.act_bf16 || (int64_t)b.max_new * ratio <= kStreamedRows) return false;
-    return b.max_len < 2048 || (int64_t)units_at_most(b, ratio, kRowsOfUnit) * s.heads > 2 * kResident;
+    const int units = units_at_most(b, ratio, kRowsOfUnit);
+    return b.max_len < 2048 || (int64_t)units * s.heads > 2 * kResident || units * (b.max_len / 32 + 1.0 + kKvBeginning) > kKvMostPlaces;
 }
 
 // The workspace does not depend on which kernels a batch takes: what serves a batch serves every smaller one.

@@ -128,10 +128,12 @@ template <bool CUT, bool UNITS> __device__ __forceinline__ Work work_of(const At
 
 // The other division, for rows few enough that what counts is the bytes of the cache: the records of all units, one after the other, in equal shares, one for each of
 // the workgroups that are resident.  A share may end within a unit and begin in the next; each stretch of a unit costs a beginning and a join with the others.  Where
-// shares that end with the units (`whole`: units take a whole number of them) are not more than kSpare records larger, it is those.
+// shares that end with the units (`whole`: units take a whole number of them) are not more than kSpare records larger, it is those.  Else each unit's records follow
+// kKvBeginning places that are none, for the time that a stretch's beginning and end take (about 4 us): shares of short units are of as many units, not of as many records.
 constexpr int kSpare = 20;
 struct Share { int first, last, size; bool whole; };
-struct Segment { int b, unit, rec, rec_to, unit_from, unit_to, to; KvSeq s; bool any; };      // a stretch of one unit: records rec .. rec_to - 1; the unit's whole extent within the row of work
+// A stretch of one unit: records rec .. rec_to - 1 (none: rec_to < rec), the unit's records and the stretch's end within the row of work.
+struct Segment { int b, unit, rec, rec_to, unit_from, unit_to, to; KvSeq s; bool any; };
 struct Lane { KvSeq s; Extent e; };                          // the sequence of a lane
 
 __device__ __forceinline__ Lane lane_of(const AttendArgs &a, int base)
@@ -145,14 +147,16 @@ __device__ __forceinline__ Lane lane_of(const AttendArgs &a, int base)
 // l: the lane's sequence of the first 64
 __device__ __forceinline__ Share share_of(const AttendArgs &a, int slot, Lane l)
 {
-    int records = 0;
+    int records = 0, units = 0;
     float about = 0.0f;
     for (int base = 0; base < a.b.sequences; base += 64) {
         if (base > 0) l = lane_of(a, base);
         records += l.e.units * max(1, l.e.hi - l.e.lo);
-        about += (float)l.e.units * (float)max(1, l.e.hi - l.e.lo);
+        units += l.e.units;
+        about += (float)l.e.units * (float)(kKvBeginning + max(1, l.e.hi - l.e.lo));
     }
     records = __builtin_amdgcn_readlane(lane_sums(records), 63);
+    units = __builtin_amdgcn_readlane(lane_sums(units), 63);
     about = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(about)), 63));
     if (records == 0 || about > 2.1e9f) return Share{0, 0, 1, true};          // (more than the host was told of: nothing is computed)
     const int size = max(quotient(records + a.slots - 1, a.slots), a.fewest);
@@ -174,7 +178,8 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int slot, Lane l)
         }
         return slot < shares ? Share{slot * high, (slot + 1) * high, high, true} : Share{0, 0, 1, true};
     }
-    return Share{(int)min((int64_t)slot * size, (int64_t)records), (int)min((int64_t)(slot + 1) * size, (int64_t)records), size, false};
+    const int places = records + units * kKvBeginning, each = quotient(places + a.slots - 1, a.slots);
+    return Share{(int)min((int64_t)slot * each, (int64_t)places), (int)min((int64_t)(slot + 1) * each, (int64_t)places), each, false};
 }
 
 __device__ __forceinline__ Segment segment_of(const AttendArgs &a, const Share &share, int pos, Lane l)
@@ -183,7 +188,7 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs &a, const Share &
     int before = 0;
     for (int base = 0; base < a.b.sequences && !w.any; base += 64) {
         if (a.b.sequences > 64) l = lane_of(a, base);
-        const int recs = l.e.hi - l.e.lo, shares = share.whole ? max(1, quotient(recs + share.size - 1, share.size)) : 1, each = share.whole ? shares * share.size : max(1, recs);
+        const int recs = l.e.hi - l.e.lo, shares = share.whole ? max(1, quotient(recs + share.size - 1, share.size)) : 1, each = share.whole ? shares * share.size : kKvBeginning + max(1, recs);
         const int mine = l.e.units * each, x = lane_sums(mine), at = pos - before - (x - mine);
         const uint64_t has = __ballot(at >= 0 && at < mine);
         if (has != 0) {
@@ -194,16 +199,17 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs &a, const Share &
             w.b = base + src;
             w.unit = i < n ? 0 : quotient(i, n);
             w.s.first = of(l.s.first); w.s.n = of(l.s.n); w.s.len = of(l.s.len);
-            w.unit_from = pos - (i - w.unit * n);
-            w.unit_to = w.unit_from + n;
+            const int start = pos - (i - w.unit * n);
+            w.unit_from = share.whole ? start : start + kKvBeginning;
+            w.unit_to = start + n;
             w.to = min(share.last, w.unit_to);
             if (share.whole) {                               // a unit's shares are alike
                 const int parts = of(shares), k = quotient(i - w.unit * n, share.size), each_part = quotient(hi - lo + parts - 1, parts);
                 w.rec = lo + k * each_part;
                 w.rec_to = min(hi, w.rec + each_part);
             } else {
-                w.rec = lo + (i - w.unit * n);
-                w.rec_to = min(hi, w.rec + (w.to - pos));     // a sequence that holds nothing has one record to itself that is none
+                w.rec = lo + max(0, pos - w.unit_from);
+                w.rec_to = min(hi, lo + (w.to - w.unit_from));     // a sequence that holds nothing has one record to itself that is none
             }
         }
         before += __builtin_amdgcn_readlane(x, 63);

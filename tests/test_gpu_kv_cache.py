@@ -256,6 +256,16 @@ def test_long_sequences_are_cut_and_joined(B, H, L, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("D,g,H", [(128, 64, 8), (256, 128, 24), (64, 32, 1)])
+def test_more_short_units_than_workgroups(D, g, H, window, dtype):
+    """several units of a workgroup one after the other, some of them cut, beside sequences that are long or have no new token"""
+    lens = [3, 31, 32, 33, 90, 64, 5, 200, 3, 40] * (3 if H > 1 else 30) + [1500, 700]
+    s = Setup([((3, 2, 0)[i % 3], L) for i, L in enumerate(lens)], H, D, g, dtype, page=32).fill()
+    check(s, 16, window=window)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("D,g,T,ratio", [(128, 128, 333, 1), (128, 32, 130, 4), (64, 64, 257, 2), (256, 64, 96, 2), (128, 64, 700, 1)])
 def test_prompts(D, g, T, ratio, dtype):
     check(Setup([(T, T), (T // 2, T // 2 + 45), (1, 80), (0, 20)], 2, D, g, dtype, seed=T).fill(), ratio)

@@ -129,3 +129,10 @@ def test_what_is_numbered_in_32_bits():
     one = desc(heads=1)
     assert attend(one, batch(sequences=1, max_new=1 << 20), q_heads=1 << 10, qs=strides(), os_=strides()) == SHAPE
     assert attend(one, batch(sequences=1, max_new=(1 << 20) - 1), q_heads=1 << 10, qs=strides(), os_=strides(), pool=None) == NULL
+    assert attend(one, batch(sequences=1 << 24, max_new=1, max_len=4096), q_heads=1, qs=strides(), os_=strides()) == SHAPE          # 2^26 units of up to 128 records
+
+
+@pytest.mark.parametrize("pool", [torch.empty(1 << 10, dtype=torch.uint8), torch.empty(1 << 20, dtype=torch.int8), torch.empty(1 << 21, dtype=torch.uint8)[::2]])
+def test_pools_that_are_none(pool):
+    with pytest.raises(ValueError):
+        eq.KvCache(2, 128, 64, 64, 3, device="cpu", pool=pool)
