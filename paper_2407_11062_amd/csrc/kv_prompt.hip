@@ -26,14 +26,18 @@ __device__ __forceinline__ half2v halves_of(uint32_t w, int p)
     return __builtin_elementwise_fma(x, half2v{by, by}, half2v{off, off});
 }
 
-template <int NS, int SG, int kPromptWaves, int kColumns, bool CUT> __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_kv_prompt(const AttendArgs a)
+// TEAMS of kPromptWaves waves each take the same rows and their own stretch of the tokens, in tiles of their own, and the first joins what they have.
+template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> __global__ __launch_bounds__(kPromptWaves * 64 * TEAMS, 2) void k_kv_prompt(const AttendArgs a)
 {
     using R = KvRecord<NS, SG>;
     constexpr int kUnitRows = kPromptWaves * kColumns * 16;
     constexpr int D = R::D, G = R::G, kChunks = NS / 2, kTileBytes = kTile * D * 2, kStaged = (4 * kChunks + kPromptWaves - 1) / kPromptWaves;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];             // two tiles of keys, two of values
-    __shared__ uint32_t s_odd[4];                                             // tile & 3: a value of a token that is there is NaN
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, c = lane >> 4;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds_all[];         // a team's two tiles of keys, two of values
+    __shared__ uint32_t s_odd_all[TEAMS][4];                                  // tile & 3: a value of a token that is there is NaN
+    const int tid = threadIdx.x, wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, c = lane >> 4;
+    const int team = TEAMS > 1 ? wave_all / kPromptWaves : 0, wave = TEAMS > 1 ? wave_all % kPromptWaves : wave_all;
+    uint8_t *lds = lds_all + team * 4 * kTileBytes;
+    uint32_t *s_odd = s_odd_all[team];
     const int head = blockIdx.x % a.heads;
     const Work w = work_of<CUT, false>(a, blockIdx.x / a.heads);
     if (!w.any) return;
@@ -90,7 +94,12 @@ template <int NS, int SG, int kPromptWaves, int kColumns, bool CUT> __global__ _
         if (a.causal) last = min(last, (w.s.len - w.s.n + row1 / a.ratio + 32) >> 5);
         if (a.window > 0) first = max(first, max(0, w.s.len - w.s.n + unit * kUnitRows / a.ratio - a.window + 1) >> 5);
     }
-    const int tiles = max(0, (last - first + 1) >> 1);
+    int tiles = max(0, (last - first + 1) >> 1);
+    if constexpr (TEAMS > 1) {                               // as many tiles each, past the last one none that is there
+        tiles = (tiles + TEAMS - 1) / TEAMS;
+        first += 2 * tiles * team;
+        last = min(last, first + 2 * tiles);
+    }
     const int32_t *table = a.b.table + (int64_t)w.b * a.b.table_stride;
     // the next record's number in the pool; -1 where it is past the end or its page is not there.  Lane i has looked up the i-th of 64 of them.
     int ahead = 0, looked_up = -1;
@@ -221,7 +230,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns, bool CUT> __global__ _
 #pragma unroll
             for (int t = 0; t < kColumns; ++t) s[h][t] = mfma(k[j], q[t][j], s[h][t]);
     };
-    if (tid < 4) s_odd[tid] = 0u;
+    if (tid < 4 * TEAMS) s_odd_all[tid >> 2][tid & 3] = 0u;
     __syncthreads();
     if (tiles > 0) {
         turn(); fetch(); rebuild(0, 0, true, false);
@@ -361,7 +370,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns, bool CUT> __global__ _
                 }
             }
         }
-        if (tid == 0) s_odd[(tile + 3) & 3] = 0u;             // read a tile ago, set again two tiles on
+        if (wave == 0 && lane == 0) s_odd[(tile + 3) & 3] = 0u;             // read a tile ago, set again two tiles on
         rebuild(tile + 2, tile + 1, true, true);
         turn();
         __syncthreads();
@@ -374,6 +383,34 @@ template <int NS, int SG, int kPromptWaves, int kColumns, bool CUT> __global__ _
         top[t] = limit[t] > 0.0f ? top[t] * back[t] : -3.0e38f;
 #pragma unroll
         for (int n = 0; n < 2 * NS; ++n) o[t][n] *= 2.0f;
+    }
+    if constexpr (TEAMS > 1) {
+        // the other team's through its tiles, lane by lane: rows and elements are the same
+        static_assert(TEAMS == 2 && kPromptWaves * kColumns * (2 * NS + 1) * 1024 <= 4 * kTileBytes, "the team's sums and results fit its tiles");
+        floatx4 *theirs = reinterpret_cast<floatx4 *>(lds_all + 4 * kTileBytes) + wave * kColumns * (2 * NS + 1) * 64 + lane;
+        if (team == 1) {
+#pragma unroll
+            for (int t = 0; t < kColumns; ++t) {
+#pragma unroll
+                for (int n = 0; n < 2 * NS; ++n) theirs[(t * (2 * NS + 1) + n) * 64] = o[t][n];
+                theirs[(t * (2 * NS + 1) + 2 * NS) * 64] = floatx4{top[t], total[t], 0.0f, 0.0f};
+            }
+        }
+        __syncthreads();
+        if (team == 1) return;
+#pragma unroll
+        for (int t = 0; t < kColumns; ++t) {
+            const floatx4 stats = theirs[(t * (2 * NS + 1) + 2 * NS) * 64];
+            const float next = fmaxf(top[t], stats[0]), f = exp2_of(top[t] - next), g = exp2_of(stats[0] - next);
+            top[t] = next;
+            total[t] = __builtin_fmaf(stats[1], g, total[t] * f);
+#pragma unroll
+            for (int n = 0; n < 2 * NS; ++n) {
+                const floatx4 x = theirs[(t * (2 * NS + 1) + n) * 64];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[t][n][i] = __builtin_fmaf(x[i], g, o[t][n][i] * f);
+            }
+        }
     }
     if constexpr (CUT) {
         if (w.chunks > 1) {                                  // the join is a launch of its own: its bytes (a part is 32 KB and more) are too many for one workgroup
@@ -452,21 +489,23 @@ template <int D> __global__ __launch_bounds__(256) void k_kv_join(const AttendAr
         a.lse[(int64_t)(w.s.first + query) * ((int64_t)a.heads * a.ratio) + oh] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
-struct PromptPlan { int rows, target; bool small, cut; };    // rows of a unit; chunks aimed at for a head of the cache; workgroups of few rows; units may be cut
+struct PromptPlan { int rows, target; bool small, cut, teams; };    // rows of a unit; chunks aimed at for a head of the cache; workgroups of few rows; units may be cut; two teams
 
-template <int NS, int SG, int W, int C, bool CUT> void launch_t(const AttendArgs &a, bool join, int units, hipStream_t st)
+template <int NS, int SG, int W, int C, int TEAMS, bool CUT> void launch_t(const AttendArgs &a, bool join, int units, hipStream_t st)
 {
-    constexpr int smem = 4 * kTile * 32 * NS * 2;
+    constexpr int smem = TEAMS * 4 * kTile * 32 * NS * 2;
     static std::atomic<uint64_t> asked{0};
-    allow_lds(asked, reinterpret_cast<const void *>(&k_kv_prompt<NS, SG, W, C, CUT>), smem);
-    k_kv_prompt<NS, SG, W, C, CUT><<<dim3((unsigned)a.slots * (unsigned)a.heads), W * 64, smem, st>>>(a);
+    allow_lds(asked, reinterpret_cast<const void *>(&k_kv_prompt<NS, SG, W, C, TEAMS, CUT>), smem);
+    k_kv_prompt<NS, SG, W, C, TEAMS, CUT><<<dim3((unsigned)a.slots * (unsigned)a.heads), W * 64 * TEAMS, smem, st>>>(a);
     if (join) k_kv_join<32 * NS><<<dim3((unsigned)units * (W * C) * (unsigned)a.heads), 256, 0, st>>>(a);
 }
 template <int NS, int SG> void launch(const AttendArgs &a, const PromptPlan &p, int units, hipStream_t st)
 {
     constexpr int kColumns = large_columns(32 * NS);
-    if (!p.small) launch_t<NS, SG, kLargeWaves, kColumns, false>(a, false, units, st);
-    else launch_t<NS, SG, NS == 8 ? kLargeWaves : kSmallWaves, 1, true>(a, p.cut, units, st);
+    if (!p.small) return launch_t<NS, SG, kLargeWaves, kColumns, 1, false>(a, false, units, st);
+    if constexpr (NS < 8)
+        if (p.teams) return launch_t<NS, SG, kSmallWaves, 1, 2, false>(a, false, units, st);
+    launch_t<NS, SG, NS == 8 ? kLargeWaves : kSmallWaves, 1, 1, true>(a, p.cut, units, st);
 }
 
 // Workgroups of 256 rows where there is one for every compute unit, else of 64, two to a compute unit.  Where even those do not take half the places, sequences of more than
@@ -480,6 +519,7 @@ PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio)
     p.rows = p.small && s.head_dim <= 128 ? kSmallWaves * 16 : large;
     p.target = ((s.head_dim <= 128 ? 512 : 256) + s.heads - 1) / s.heads;
     p.cut = p.small && units_at_most(b, ratio, p.rows) < p.target / 2 && b.max_len > kFewest * kKvRecord;
+    p.teams = p.small && !p.cut && s.head_dim <= 128 && b.max_len > kTile && (int64_t)units_at_most(b, ratio, p.rows) * s.heads <= 256;
     return p;
 }
 }  // namespace
