@@ -12,6 +12,9 @@
 // A matrix instruction drops what lies 2^-26 below its largest term, its addend among them.  With fp32 activations the two parts and the records are therefore added
 // up outside, and codes are taken as c - 8 about m + 8 s, which leaves less to cancel between the two sums.  The softmax keeps a running maximum
 // and sum; the maximum moves only when a score passes it by 2 in log2, so that most records rescale nothing (p <= 4, and s < 2^14, so p s stays in binary16).
+//
+// 32 sequences of 32768 tokens, 64 heads on 8 of 128: 147 us, 5.2 TB/s (a large copy: 4.8).  A token at 515, 32 heads of 128: 8.4 us, of which the way to the first
+// record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 18 us for 44 MB.
 #include "kv_work.h"
 
 namespace eqat {
@@ -427,7 +430,7 @@ struct WsLayout { Scratch streamed, prompts; };
 WsLayout ws_layout(const KvShape &s, const KvBatch &b, int ratio)
 {
     WsLayout l;
-    l.streamed = scratch_of(0, shares_of(s), s.heads, kRowsOfUnit, s.head_dim);
+    l.streamed = scratch_of(0, (size_t)shares_of(s) * s.heads, true, kRowsOfUnit, s.head_dim);
     l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
     if (s.act_bf16 && (int64_t)b.max_new * ratio > kStreamedRows) l.prompts = prompt_scratch(s, (l.streamed.end + 255) / 256 * 256);
     return l;

@@ -10,8 +10,8 @@ namespace eqat {
 struct AttendArgs {
     KvBatch b;
     KvRows q, out;
-    float *lse, *parts;                            // parts: [chunk][head][rows of a unit][D] sums, then [chunk][head][rows of a unit][2] maxima and totals
-    uint32_t *counters;                            // [unit][head], zero before and after every launch
+    float *lse, *parts;                            // parts: [chunk, or two of a workgroup][head][rows of a unit][D] sums, then [..][head][rows of a unit][2] maxima and totals
+    uint32_t *counters;                            // streamed: [workgroup that a unit begins in][head], zero before and after every launch
     const uint8_t *pool;
     int64_t pages;
     int heads, ratio, page_records, window, target, slots;
@@ -21,14 +21,14 @@ struct AttendArgs {
     float scale;                                   // times log2(e)
 };
 
-// Where a launch's counters and parts lie in the workspace.  There is at most one cut unit per chunk aimed at, and a cut unit has fewer than twice its share of them.
+// Where a launch's counters and parts lie in the workspace: two parts for each of the streamed kernel's workgroups, and for each chunk that prompts are cut into (a cut
+// unit has fewer than twice its share of them).
 struct Scratch { size_t counters, parts, end; };
-inline Scratch scratch_of(size_t at, int target, int heads, int unit_rows, int head_dim)
+inline Scratch scratch_of(size_t at, size_t chunks, bool counted, int unit_rows, int head_dim)
 {
-    const size_t chunks = (size_t)target * heads;
     Scratch l;
     l.counters = at;
-    l.parts = at + (chunks * 4 + 255) / 256 * 256;
+    l.parts = at + (counted ? (chunks * 4 + 255) / 256 * 256 : 0);
     l.end = l.parts + 2 * chunks * (size_t)unit_rows * (size_t)(head_dim * 4 + 8);
     return l;
 }
