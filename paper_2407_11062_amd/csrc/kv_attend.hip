@@ -13,8 +13,8 @@
 // up outside, and codes are taken as c - 8 about m + 8 s, which leaves less to cancel between the two sums.  The softmax keeps a running maximum
 // and sum; the maximum moves only when a score passes it by 2 in log2, so that most records rescale nothing (p <= 4, and s < 2^14, so p s stays in binary16).
 //
-// 32 sequences of 32768 tokens, 64 heads on 8 of 128: 147 us, 5.2 TB/s (a large copy: 4.8).  A token at 515, 32 heads of 128: 8.4 us, of which the way to the first
-// record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 18 us for 44 MB.
+// 32 sequences of 32768 tokens, 64 heads on 8 of 128: 145 us, 5.3 TB/s (a large copy: 4.8).  A token at 515, 32 heads of 128: 8.1 us, of which the way to the first
+// record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 17.4 us for 44 MB.
 #include "kv_work.h"
 
 namespace eqat {
@@ -22,7 +22,7 @@ namespace {
 
 constexpr int waves_of(int head_dim) { return head_dim > 128 ? 4 : 8; }         // of a workgroup, one on each compute unit
 constexpr int kRowsOfUnit = 16;                    // rows (query, head of the group) of a unit
-constexpr int kFewestRecords = 32;                 // of a share: a join with another workgroup costs about as much (one token at 515: 32 8.3 us, 16 9.5, 8 9.3)
+constexpr int kFewestRecords = 32;                 // of a share: a join with another workgroup costs about as much (one token at 515: 32 8.1 us, 16 9.5, 8 9.3)
 constexpr int kFewParts = 4;                       // parts of a unit that are fetched together
 constexpr int kResident = 256;                     // workgroups
 constexpr int depth_of(int head_dim) { return head_dim > 128 ? 2 : 3; }          // records of a wave's ring
@@ -85,15 +85,11 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
         const int first_rec = w.rec + wave, records = max(0, (w.rec_to - first_rec + kWaves - 1) / kWaves);
         look_up(first_rec);
         T loaded[NS][8];
-        if (is_row) {
-            const T *q = static_cast<const T *>(a.q.p) + (int64_t)(w.s.first + query) * a.q.token_stride + (int64_t)(head * a.ratio + of_group) * a.q.head_stride;
+        {
+            // (a row that is none has one of the last query's)
+            const T *q = static_cast<const T *>(a.q.p) + (int64_t)(w.s.first + min(query, w.s.n - 1)) * a.q.token_stride + (int64_t)(head * a.ratio + of_group) * a.q.head_stride;
 #pragma unroll
             for (int j = 0; j < NS; ++j) __builtin_memcpy(loaded[j], __builtin_assume_aligned(q + 32 * j + 8 * c, 16), sizeof(loaded[j]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < NS; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) loaded[j][e] = (T)0.0f;
         }
         // The i-th record of this wave into the ring.  The loads are assembly, so nothing but the waits below counts them; a record that is not there is fetched from
         // the pool's first bytes and not looked at, so that every record counts as many.

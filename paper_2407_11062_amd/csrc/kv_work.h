@@ -160,24 +160,19 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int slot, Lane l)
     about = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(about)), 63));
     if (records == 0 || about > 2.1e9f) return Share{0, 0, 1, true};          // (more than the host was told of: nothing is computed)
     const int size = max(quotient(records + a.slots - 1, a.slots), a.fewest);
-    auto shares_of_size = [&](int larger) {
-        int shares = 0;
+    // the smallest such size: `size`, or by halves where size + kSpare is one (a larger size never has more shares).  One body: code that runs once comes from far.
+    int low = size, high = size + kSpare + 1, at = size, shares = 0;
+    while (low < high) {
+        int of_at = 0;
         for (int base = 0; base < a.b.sequences; base += 64) {
             if (a.b.sequences > 64) l = lane_of(a, base);
-            shares += l.e.units * max(1, quotient(l.e.hi - l.e.lo + larger - 1, larger));
+            of_at += l.e.units * max(1, quotient(l.e.hi - l.e.lo + at - 1, at));
         }
-        return __builtin_amdgcn_readlane(lane_sums(shares), 63);
-    };
-    // the smallest such size, by halves: a larger size never has more shares
-    int low = size, high = size, shares = shares_of_size(size);
-    if (shares > a.slots) { high = size + kSpare; shares = shares_of_size(high); low = size + 1; }
-    if (shares <= a.slots) {
-        while (low < high) {
-            const int half = (low + high) >> 1, of_half = shares_of_size(half);
-            if (of_half <= a.slots) { high = half; shares = of_half; } else { low = half + 1; }
-        }
-        return slot < shares ? Share{slot * high, (slot + 1) * high, high, true} : Share{0, 0, 1, true};
+        of_at = __builtin_amdgcn_readlane(lane_sums(of_at), 63);
+        if (of_at <= a.slots) { high = at; shares = of_at; } else { low = at + 1; }
+        at = shares == 0 ? size + kSpare : (low + high) >> 1;
     }
+    if (shares > 0) return slot < shares ? Share{slot * high, (slot + 1) * high, high, true} : Share{0, 0, 1, true};
     const int places = records + units * kKvBeginning, each = quotient(places + a.slots - 1, a.slots);
     return Share{(int)min((int64_t)slot * each, (int64_t)places), (int)min((int64_t)(slot + 1) * each, (int64_t)places), each, false};
 }
