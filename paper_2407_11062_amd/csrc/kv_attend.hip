@@ -17,6 +17,8 @@
 // record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 17.4 us for 44 MB.
 #include "kv_work.h"
 
+#include <algorithm>
+
 namespace eqat {
 namespace {
 
@@ -24,7 +26,8 @@ constexpr int waves_of(int head_dim) { return head_dim > 128 ? 4 : 8; }         
 constexpr int kRowsOfUnit = 16;                    // rows (query, head of the group) of a unit
 constexpr int kFewestRecords = 32;                 // of a share: a join with another workgroup costs about as much (one token at 515: 32 8.1 us, 16 9.5, 8 9.3)
 constexpr int kFewParts = 4;                       // parts of a unit that are fetched together
-constexpr int kResident = 256;                     // workgroups
+constexpr int kResident = 256;                     // compute units
+constexpr int workgroups_of(int head_dim, bool bf16) { return head_dim == 64 && bf16 ? 2 : 1; }          // that registers and LDS of a compute unit hold
 constexpr int depth_of(int head_dim) { return head_dim > 128 ? 2 : 3; }          // records of a wave's ring
 
 // f16(a * s.lo), f16(b * t.lo) in the halves of a register, s, t words whose low half is a binary16 number: the form that the compiler makes v_fma_mixlo_f16 and
@@ -47,7 +50,7 @@ template <bool CENTRED> __device__ __forceinline__ float middle(uint32_t step)  
 {
     return CENTRED ? __builtin_fmaf(8.0f, low_half(step), high_half(step)) : high_half(step);
 }
-template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * NS) * 64, waves_of(32 * NS) / 4) void k_kv_attend(const AttendArgs a)
+template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * NS) * 64, workgroups_of(32 * NS, !F32) * waves_of(32 * NS) / 4) void k_kv_attend(const AttendArgs a)
 {
     using R = KvRecord<NS, SG>;
     using T = typename std::conditional<F32, float, bf16_t>::type;
@@ -406,8 +409,16 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
     }
 }
 
-// shares of the work of a head of the cache
-int shares_of(const KvShape &s) { return (kResident + s.heads - 1) / s.heads; }
+// Shares of the work of a head of the cache: no more workgroups than are resident (a second round of a few took as long as the first: 40 heads, 16 sequences of 8000
+// 131 us, with 7 shares a head for 6 192), and two a compute unit only where that leaves shares of 64 records (heads of 64 on 40, 8 sequences of 8000 48 us one, 42 two;
+// on 8, where it leaves 31, 16.5 and 17.8).
+int most_shares_of(const KvShape &s, int workgroups) { return std::max(1, workgroups * kResident / s.heads); }
+int shares_of(const KvShape &s, const KvBatch &b, int ratio)
+{
+    const int workgroups = workgroups_of(s.head_dim, s.act_bf16);
+    const bool large = (double)units_at_most(b, ratio, kRowsOfUnit) * s.heads * (b.max_len / 32) >= 64.0 * workgroups * kResident;
+    return most_shares_of(s, large ? workgroups : 1);
+}
 
 // Sequences of more rows than this go to the kernel that rebuilds keys and values (bf16): for 64 rows this one takes 13.6 us and that one 22.6 (8000 tokens, 8 heads of
 // the cache), 9 and 17 us (500 tokens).
@@ -426,7 +437,7 @@ struct WsLayout { Scratch streamed, prompts; };
 WsLayout ws_layout(const KvShape &s, const KvBatch &b, int ratio)
 {
     WsLayout l;
-    l.streamed = scratch_of(0, (size_t)shares_of(s) * s.heads, true, kRowsOfUnit, s.head_dim);
+    l.streamed = scratch_of(0, (size_t)most_shares_of(s, workgroups_of(s.head_dim, s.act_bf16)) * s.heads, true, kRowsOfUnit, s.head_dim);
     l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
     if (s.act_bf16 && (int64_t)b.max_new * ratio > kStreamedRows) l.prompts = prompt_scratch(s, (l.streamed.end + 255) / 256 * 256);
     return l;
@@ -472,7 +483,7 @@ void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &t, con
     scratch(l.streamed);
     a.unit_bits = __builtin_ctz(kRowsOfUnit);
     a.fewest = kFewestRecords;
-    a.slots = shares_of(s);
+    a.slots = shares_of(s, b, a.ratio);
     const int sg = s.group / 32;
     switch (s.head_dim) {
     case 64: if (sg == 1) launch<2, 1>(s, a, st); else launch<2, 2>(s, a, st); break;

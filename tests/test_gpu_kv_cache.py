@@ -266,6 +266,15 @@ def test_more_short_units_than_workgroups(D, g, H, window, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("H,D,g", [(8, 64, 32), (40, 64, 64), (24, 128, 128), (300, 64, 64)])
+def test_shares_of_many_records(H, D, g, dtype):
+    """workgroups of two a compute unit, and of heads that do not divide them"""
+    s = Setup([(1, L) for L in [2000 if H < 100 else 300] * 2 + [3 + 7 * i % 50 for i in range(90 if H < 40 else 20)]], H, D, g, dtype, page=32).fill()
+    check(s, 1)
+    assert D != 64 or len(s.seqs) * H * (max(s.lens) // 32) >= 64 * 512
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("D,g,T,ratio", [(128, 128, 333, 1), (128, 32, 130, 4), (64, 64, 257, 2), (256, 64, 96, 2), (128, 64, 700, 1)])
 def test_prompts(D, g, T, ratio, dtype):
     check(Setup([(T, T), (T // 2, T // 2 + 45), (1, 80), (0, 20)], 2, D, g, dtype, seed=T).fill(), ratio)
