@@ -27,7 +27,7 @@ constexpr int kRowsOfUnit = 16;                    // rows (query, head of the g
 constexpr int kFewestRecords = 32;                 // of a share: a join with another workgroup costs about as much (one token at 515: 32 8.1 us, 16 9.5, 8 9.3)
 constexpr int kFewParts = 4;                       // parts of a unit that are fetched together
 constexpr int kResident = 256;                     // compute units
-constexpr int workgroups_of(int head_dim, bool bf16) { return head_dim == 64 && bf16 ? 2 : 1; }          // that registers and LDS of a compute unit hold
+constexpr int workgroups_of(int head_dim, int groups, bool bf16) { return head_dim == 64 && (bf16 || groups == 1) ? 2 : 1; }          // that registers and LDS of a compute unit hold
 constexpr int depth_of(int head_dim) { return head_dim > 128 ? 2 : 3; }          // records of a wave's ring
 
 // f16(a * s.lo), f16(b * t.lo) in the halves of a register, s, t words whose low half is a binary16 number: the form that the compiler makes v_fma_mixlo_f16 and
@@ -50,7 +50,7 @@ template <bool CENTRED> __device__ __forceinline__ float middle(uint32_t step)  
 {
     return CENTRED ? __builtin_fmaf(8.0f, low_half(step), high_half(step)) : high_half(step);
 }
-template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * NS) * 64, workgroups_of(32 * NS, !F32) * waves_of(32 * NS) / 4) void k_kv_attend(const AttendArgs a)
+template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * NS) * 64, workgroups_of(32 * NS, NS / SG, !F32) * waves_of(32 * NS) / 4) void k_kv_attend(const AttendArgs a)
 {
     using R = KvRecord<NS, SG>;
     using T = typename std::conditional<F32, float, bf16_t>::type;
@@ -415,7 +415,7 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
 int most_shares_of(const KvShape &s, int workgroups) { return std::max(1, workgroups * kResident / s.heads); }
 int shares_of(const KvShape &s, const KvBatch &b, int ratio)
 {
-    const int workgroups = workgroups_of(s.head_dim, s.act_bf16);
+    const int workgroups = workgroups_of(s.head_dim, s.groups, s.act_bf16);
     const bool large = (double)units_at_most(b, ratio, kRowsOfUnit) * s.heads * (b.max_len / 32) >= 64.0 * workgroups * kResident;
     return most_shares_of(s, large ? workgroups : 1);
 }
@@ -437,7 +437,7 @@ struct WsLayout { Scratch streamed, prompts; };
 WsLayout ws_layout(const KvShape &s, const KvBatch &b, int ratio)
 {
     WsLayout l;
-    l.streamed = scratch_of(0, (size_t)most_shares_of(s, workgroups_of(s.head_dim, s.act_bf16)) * s.heads, true, kRowsOfUnit, s.head_dim);
+    l.streamed = scratch_of(0, (size_t)most_shares_of(s, workgroups_of(s.head_dim, s.groups, s.act_bf16)) * s.heads, true, kRowsOfUnit, s.head_dim);
     l.prompts = Scratch{l.streamed.end, l.streamed.end, l.streamed.end};
     if (s.act_bf16 && (int64_t)b.max_new * ratio > kStreamedRows) l.prompts = prompt_scratch(s, (l.streamed.end + 255) / 256 * 256);
     return l;
