@@ -14,7 +14,7 @@
 // and sum; the maximum moves only when a score passes it by 2 in log2, so that most records rescale nothing (p <= 4, and s < 2^14, so p s stays in binary16).
 //
 // 32 sequences of 32768 tokens, 64 heads on 8 of 128: 145 us, 5.3 TB/s (a large copy: 4.8).  A token at 515, 32 heads of 128: 8.1 us, of which the way to the first
-// record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 17.4 us for 44 MB.
+// record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 17.5 us for 44 MB.
 #include "kv_work.h"
 
 #include <algorithm>

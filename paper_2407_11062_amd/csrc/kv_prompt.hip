@@ -7,7 +7,7 @@
 // Keys and values are halved on their way (m + s c may pass 65504 by a rounding), and held to 11 bits, as are queries with the scale of the scores in them, and p.  The
 // running maximum is the products' addend, so that a score is an exponent as it comes, and the sum of p is one product more, with ones.  Scores and sums are binary32.
 //
-// 8192 tokens, 64 heads on 8 of 128: 1145 us, 960 TFLOP/s where a product of 8192^3 reaches 1207.  333 tokens, 32 heads of 128: 15.7 us, of which the first tile of a
+// 8192 tokens, 64 heads on 8 of 128: 1140 to 1160 us, 950 TFLOP/s where a product of 8192^3 reaches 1207.  333 tokens, 32 heads of 128: 15.7 us, of which the first tile of a
 // workgroup takes 7 (launch, lengths, pages, records, each known only after the one before) and a tile 1.2.
 #include "kv_work.h"
 
