@@ -241,9 +241,13 @@ template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> _
         turn();                                              // this tile, the next, the one after
     }
     __syncthreads();
-    if (tiles > 0)
+    if (tiles > 0) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) { uintx4 k[NS]; key_parts(0, h, k); scores(h, k); }
+        __syncthreads();                                     // all waves have read the first tile's keys: the loop's first rebuild puts the third tile's there
+    }
+    // A tile's turn reads the keys of the next tile and its own values, and writes the keys of the one after into the place of its own, which nobody reads any more
+    // since the barrier before (here, or at the turn's end), and the next tile's values into that of the last tile's.
     for (int tile = 0; tile < tiles; ++tile) {
         fetch();                                              // keys of tile + 2, values of tile + 1
         const int token0 = (first + 2 * tile) * kKvRecord;
