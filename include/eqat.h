@@ -407,9 +407,12 @@ eqat_status eqat_dx_route(const eqat_desc *d, int block_ap, int32_t *route);
  *              It is a number of pages of `page_tokens` tokens; how a page is laid out is the library's own.  Bytes per token and head: head_dim + 8 head_dim / group.
  *   Sequences  An eqat_kv_batch says, in device arrays, where the sequences of a call stand: sequence b holds lens[b] tokens, its position p on page
  *              table[b * table_stride + p / page_tokens] (at p % page_tokens), and its newest starts[b+1] - starts[b] tokens are the rows starts[b] .. starts[b+1] - 1 of
- *              the call's tensors: lens counts them in.  Either number may be 0.  The host gives bounds only (tokens = starts[sequences], max_new, max_len), so that a
+ *              the call's tensors: lens counts them in.  Either number may be 0, and there may be more new tokens than held ones (the first of them, which stand
+ *              before the beginning, are not there).  The host gives bounds only (tokens = starts[sequences], max_new, max_len), so that a
  *              captured graph serves lengths and pages that change between its replays.  What lies beyond the bounds, or on a page outside the pool, is taken as not
- *              there: not written, read as zeros, not attended to; nothing outside the tensors and the pool is touched whatever stands in the arrays.
+ *              there: not written, read as zeros, not attended to; the tokens within keep their positions (a step replayed past the end writes nothing).  Of a sequence with
+ *              more new tokens than max_new the first max_new rows are taken and the others left as they are.  Nothing outside the tensors and the pool is touched
+ *              whatever stands in the arrays.
  *   Tensors    [tokens, heads, head_dim] with any strides (in elements, of a token and of a head; elements of a head are contiguous), such as slices of the rows of
  *              a stacked q|k|v projection.  Pointers and strides in bytes are multiples of 16.
  *   Types      desc.act_dtype (bf16 or fp32) for every tensor; lse is fp32.

@@ -63,18 +63,24 @@ size_t kv_attend_ws_bytes(const KvShape &s, const KvBatch &b, int q_heads);
 void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &a, const void *pool, void *ws, hipStream_t st);
 
 
-// Sequence `b` of a call: its new tokens are rows first .. first + n - 1 of the call's tensors and stand at positions len - n .. len - 1.
-struct KvSeq { int first, n, len; };
+// Sequence `b` of a call: rows first .. first + n - 1 of the call's tensors are tokens at positions pos .. pos + n - 1 of it, and positions 0 .. len - 1 may be there.
+// n and len are cut to what the host was told of, and rows to those of the tensors; pos is what the arrays say, so a position may be below 0, or be len and more: a token
+// that is not there.  No position passes 2^31 - 2 nor lies below 1 - 2^31.
+struct KvSeq { int first, n, len, pos; };
 __device__ __forceinline__ KvSeq kv_seq(const KvBatch &k, int page_tokens, int b)
 {
     const int total = (int)k.tokens;
     KvSeq s;
+    const int held = max(k.lens[b], 0), end = k.starts[b + 1];
     s.first = min(max(k.starts[b], 0), total);
-    s.n = min(max(min(k.starts[b + 1], total) - s.first, 0), k.max_new);
+    s.n = min(max(min(end, total) - s.first, 0), k.max_new);
+    s.pos = (int)((uint32_t)held - (uint32_t)end + (uint32_t)s.first);          // (without rows: any number)
     const int64_t most = min((int64_t)k.table_stride * page_tokens, (int64_t)k.max_len);
-    s.len = (int)min((int64_t)max(k.lens[b], 0), most);
+    s.len = (int)min((int64_t)held, most);
     return s;
 }
+// the first position that a query at `pos` sees through a window
+__device__ __forceinline__ int window_from(int pos, int window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
 
 // sums over the lanes up to and with this one (row shifts, then the rows' last lanes to the rows behind them)
 template <typename T> __device__ __forceinline__ T lane_sums(T x)

@@ -73,9 +73,9 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
         // ---- this lane's row of the queries -----------------------------------------------------------
         const int row = w.unit * kRowsOfUnit + r, query = quotient(row, a.ratio), of_group = row - query * a.ratio;
         const bool is_row = query < w.s.n;
-        const int pos = w.s.len - w.s.n + query;
+        const int pos = w.s.pos + query;
         const int seen_to = is_row && a.causal ? min(w.s.len, pos + 1) : w.s.len;             // positions seen_from .. seen_to - 1 (a row that is none restricts nothing)
-        const int seen_from = is_row && a.window > 0 ? max(0, pos - a.window + 1) : 0;
+        const int seen_from = is_row ? window_from(pos, a.window) : 0;
         // Records w.rec + wave, + kWaves, ...: lane i looks up where the i-th of 64 of them lies (-1: its page is not there).
         const int32_t *table = a.b.table + (int64_t)w.b * a.b.table_stride;
         int place_lo = -1, place_hi = -1;

@@ -95,8 +95,9 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float (
     }
 }
 
-// The record of a wave: the `index`-th of those that the newest tokens of the sequences touch, and one head.
-struct Place { bool any, there, full; int first, from, to; uint8_t *record; };         // row of position 0 (so row = first + position); positions from .. to - 1 of the record are the call's
+// The record of a wave: the `index`-th of those that the newest tokens of the sequences touch, and one head.  Positions from .. to - 1 of the record are the call's,
+// position from + i in row `row` + i; those from `held` on are not there, nor is any where the record is not.
+struct Place { bool any, there; int token0, row, from, to, held; uint8_t *record; };
 __device__ __forceinline__ Place place_of(const CacheArgs &a, int index, int head, int64_t record_bytes)
 {
     Place p{};
@@ -105,20 +106,23 @@ __device__ __forceinline__ Place place_of(const CacheArgs &a, int index, int hea
         const int b = base + (threadIdx.x & 63);
         KvSeq s{};
         if (b < a.b.sequences) s = kv_seq(a.b, a.page_records * kKvRecord, b);
-        const int rec0 = max(0, s.len - s.n) >> 5, mine = s.n > 0 && s.len > 0 ? ((s.len - 1) >> 5) - rec0 + 1 : 0, x = lane_sums(mine), at = index - before - (x - mine);
+        const int rec0 = s.pos >> 5, mine = s.n > 0 ? ((s.pos + s.n - 1) >> 5) - rec0 + 1 : 0, x = lane_sums(mine), at = index - before - (x - mine);
         const uint64_t has = __ballot(at >= 0 && at < mine);
         if (has != 0) {
             const int src = __ffsll((unsigned long long)has) - 1;
             auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
-            const int rec = of(rec0) + of(at), len = of(s.len), n = of(s.n), of_seq = quotient(rec, a.page_records);
-            const int page = __builtin_amdgcn_readfirstlane(a.b.table[(int64_t)(base + src) * a.b.table_stride + of_seq]);
+            const int rec = of(rec0) + of(at), pos = of(s.pos), end = pos + of(s.n) - 1;
             p.any = true;
-            p.first = of(s.first) - (len - n);
-            p.from = max(max(rec * kKvRecord, len - n), 0);
-            p.to = min(rec * kKvRecord + kKvRecord, len);
-            p.full = p.to - p.from == kKvRecord;
-            p.there = page >= 0 && page < a.pages;
-            p.record = a.pool + (((int64_t)(p.there ? page : 0) * a.heads + head) * a.page_records + (rec - of_seq * a.page_records)) * record_bytes;
+            p.token0 = rec * kKvRecord;
+            p.from = max(p.token0, pos);
+            p.to = min(p.token0 + kKvRecord - 1, end) + 1;
+            p.row = of(s.first) + (p.from - pos);
+            p.held = of(s.len);
+            if (rec >= 0 && p.token0 < p.held) {
+                const int of_seq = quotient(rec, a.page_records), page = __builtin_amdgcn_readfirstlane(a.b.table[(int64_t)(base + src) * a.b.table_stride + of_seq]);
+                p.there = page >= 0 && page < a.pages;
+                p.record = a.pool + (((int64_t)(p.there ? page : 0) * a.heads + head) * a.page_records + (rec - of_seq * a.page_records)) * record_bytes;
+            }
         }
         before += __builtin_amdgcn_readlane(x, 63);
     }
@@ -144,7 +148,7 @@ __device__ __forceinline__ void wave_meets() { __builtin_amdgcn_fence(__ATOMIC_A
 template <int NS, typename T> __device__ __forceinline__ void load_token(const KvRows &rows, const Place &at, int pos, int head, int c, float (&x)[NS][8])
 {
     if (pos >= at.from && pos < at.to) {
-        const T *p = static_cast<const T *>(rows.p) + (int64_t)(at.first + pos) * rows.token_stride + head * rows.head_stride + 8 * c;
+        const T *p = static_cast<const T *>(rows.p) + (int64_t)(at.row + (pos - at.from)) * rows.token_stride + head * rows.head_stride + 8 * c;
 #pragma unroll
         for (int j = 0; j < NS; ++j) load8(p + 32 * j, x[j]);
     } else {
@@ -163,13 +167,14 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
     const int head = blockIdx.y * (kCacheWaves / 2) + (wave >> 1);
     const bool values = (wave & 1) != 0;                      // this wave's part of the record
     if (head >= a.heads) return;
-    const Place at = place_of(a, blockIdx.x, head, R::kBytes);
+    Place at = place_of(a, blockIdx.x, head, R::kBytes);
     if (!at.any || !at.there) return;
+    at.to = min(at.to, at.held);
+    const bool full = at.to - at.from == kKvRecord;
     const KvRows rows = values ? a.v : a.k;
-    const int token0 = (at.to - 1) & ~(kKvRecord - 1);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int pos = token0 + h * 16 + t;
+        const int pos = at.token0 + h * 16 + t;
         const bool is = pos >= at.from && pos < at.to;
         if (!__any(is)) continue;
         float x[NS][8];
@@ -200,7 +205,7 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
             uint32_t pairs[NS];                               // byte i: the elements 2 i and 2 i + 1
 #pragma unroll
             for (int j = 0; j < NS; ++j) pairs[j] = codes_of(x[j], steps[j / SG], [](int e) { return 4 * e; });
-            uint8_t *to = at.full ? lds[wave >> 1] : at.record + R::kValues;
+            uint8_t *to = full ? lds[wave >> 1] : at.record + R::kValues;
 #pragma unroll
             for (int n = 0; n < NS / 2; ++n)
 #pragma unroll
@@ -210,7 +215,7 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
                 }
         }
     }
-    if (values && at.full) {
+    if (values && full) {
         wave_meets();
 #pragma unroll
         for (int n = 0; n < NS / 2; ++n)
@@ -235,7 +240,6 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
     if (head >= a.heads || rows.p == nullptr) return;
     const Place at = place_of(a, blockIdx.x, head, R::kBytes);
     if (!at.any) return;
-    const int token0 = (at.to - 1) & ~(kKvRecord - 1);
     uint32_t steps[2][R::G], words[2][NS];                    // of a key
     if (at.there) {
 #pragma unroll
@@ -266,16 +270,17 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int pos = token0 + h * 16 + t;
+        const int pos = at.token0 + h * 16 + t;
         if (pos < at.from || pos >= at.to) continue;
-        T *to = static_cast<T *>(rows.p) + (int64_t)(at.first + pos) * rows.token_stride + head * rows.head_stride + 8 * c;
+        const bool there = at.there && pos < at.held;
+        T *to = static_cast<T *>(rows.p) + (int64_t)(at.row + (pos - at.from)) * rows.token_stride + head * rows.head_stride + 8 * c;
         float x[NS][8] = {};
-        if (at.there && !values) {
+        if (there && !values) {
 #pragma unroll
             for (int j = 0; j < NS; ++j)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[j][e] = stands_for((words[h][j] >> (16 * (e & 1) + 4 * (e >> 1))) & 15u, steps[h][j / SG]);
-        } else if (at.there) {
+        } else if (there) {
 #pragma unroll
             for (int n = 0; n < NS / 2; ++n)
 #pragma unroll

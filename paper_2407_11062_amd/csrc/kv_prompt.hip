@@ -56,9 +56,9 @@ template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> _
         const int row = unit * kUnitRows + (wave * kColumns + t) * 16 + r;
         query[t] = quotient(row, a.ratio); of_group[t] = row - query[t] * a.ratio;
         const bool is_row = query[t] < w.s.n;
-        const int pos = w.s.len - w.s.n + query[t];
+        const int pos = w.s.pos + query[t];
         seen_to[t] = !is_row ? 0 : a.causal ? min(w.s.len, pos + 1) : w.s.len;
-        seen_from[t] = is_row && a.window > 0 ? max(0, pos - a.window + 1) : 0;
+        seen_from[t] = is_row ? window_from(pos, a.window) : 0;
         if (is_row) { least_to = min(least_to, seen_to[t]); most_from = max(most_from, seen_from[t]); }
         const bf16_t *src = static_cast<const bf16_t *>(a.q.p) + (int64_t)(w.s.first + query[t]) * a.q.token_stride + (int64_t)(head * a.ratio + of_group[t]) * a.q.head_stride;
         float top = 0.0f;
@@ -94,8 +94,8 @@ template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> _
     int first = w.first, last = w.last;
     {
         const int row1 = min((unit + 1) * kUnitRows, w.s.n * a.ratio) - 1;
-        if (a.causal) last = min(last, (w.s.len - w.s.n + row1 / a.ratio + 32) >> 5);
-        if (a.window > 0) first = max(first, max(0, w.s.len - w.s.n + unit * kUnitRows / a.ratio - a.window + 1) >> 5);
+        if (a.causal) last = min(last, ((w.s.pos + row1 / a.ratio) >> 5) + 1);
+        first = max(first, window_from(w.s.pos + unit * kUnitRows / a.ratio, a.window) >> 5);
     }
     int tiles = max(0, (last - first + 1) >> 1);
     if constexpr (TEAMS > 1) {                               // as many tiles each, past the last one none that is there

@@ -72,8 +72,8 @@ __device__ __forceinline__ Extent extent_of(const AttendArgs &a, const KvSeq &s)
     Extent e;
     const int rows = s.n * a.ratio;
     e.units = rows >= a.from_rows && rows < a.to_rows ? (rows + (1 << a.unit_bits) - 1) >> a.unit_bits : 0;
-    e.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) >> 5 : 0;
     e.hi = (s.len + 31) >> 5;
+    e.lo = a.window > 0 ? min(window_from(s.pos, a.window) >> 5, e.hi) : 0;
     return e;
 }
 
@@ -115,7 +115,7 @@ template <bool CUT, bool UNITS> __device__ __forceinline__ Work work_of(const At
             w.chunks = of(chunks);
             w.unit = UNITS || w.chunks == 1 ? i : quotient(i, w.chunks);
             w.chunk = UNITS ? 0 : i - w.unit * w.chunks;
-            w.s.first = of(s.first); w.s.n = of(s.n); w.s.len = of(s.len);
+            w.s.first = of(s.first); w.s.n = of(s.n); w.s.len = of(s.len); w.s.pos = of(s.pos);
             w.first = of(e.lo) + w.chunk * each;
             w.last = min(of(e.hi), w.first + each);
             if constexpr (CUT) w.part = parts + of(y - (chunks > 1 ? mine * (UNITS ? chunks : 1) : 0)) + w.unit * w.chunks + w.chunk;
@@ -193,7 +193,7 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs &a, const Share &
             w.any = true;
             w.b = base + src;
             w.unit = i < n ? 0 : quotient(i, n);
-            w.s.first = of(l.s.first); w.s.n = of(l.s.n); w.s.len = of(l.s.len);
+            w.s.first = of(l.s.first); w.s.n = of(l.s.n); w.s.len = of(l.s.len); w.s.pos = of(l.s.pos);
             const int start = pos - (i - w.unit * n);
             w.unit_from = share.whole ? start : start + kKvBeginning;
             w.unit_to = start + n;

@@ -1,0 +1,185 @@
+"""The 4-bit cache where bounds are passed, rows fall short of what the host was told, softmaxes are steep and numbers extreme: against the 64-bit reference."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_11062_amd as eq
+import kv_reference as ref
+from test_gpu_kv_cache import DTYPES, Setup, as_type, check, rows, same
+
+pytestmark = pytest.mark.gpu
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def batch(s, counts, lens=None, max_len=None, max_new=None, table=None):
+    starts = [sum(counts[:i]) for i in range(len(counts) + 1)]
+    lens = s.lens if lens is None else lens
+    return eq.KvBatch((s.table if table is None else table).contiguous().cuda(), i32(lens), i32(starts), tokens=starts[-1],
+                      max_new=max(counts) if max_new is None else max_new, max_len=max(lens) if max_len is None else max_len)
+
+
+def held_to(got, lse, want, dtype, what, rows_of=slice(None)):
+    """results of one sequence's rows against (out, lse, bounds) of the reference"""
+    o, l, to, tl = (x[rows_of] for x in want)
+    got, lse = got.cpu(), lse.cpu().double()
+    assert torch.equal(got.isnan(), o.isnan()) and torch.equal(lse == -math.inf, l == -math.inf), what
+    over = (got.double() - o).abs() - to - (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -23) * o.abs()
+    assert over.nan_to_num().max() <= 0, f"{what}: {over.nan_to_num().max()} beyond the bound"
+    fine = l.isfinite()
+    over = ((lse - l).abs() - tl)[fine]
+    assert over.numel() == 0 or over.nan_to_num().max() <= 0, f"{what}: lse {over.max()} beyond the bound"
+
+
+# ---- bounds that are passed --------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("by_table", [False, True])
+@pytest.mark.parametrize("reach", [64, 96])
+def test_tokens_beyond_a_bound_are_not_written_and_read_as_zeros(reach, by_table, dtype):
+    """ten tokens at 90 .. 99 where the call was told of `reach` positions, by the host's number or by the table's width; a whole sequence beside it"""
+    s = Setup([(10, 100), (4, 50)], 2, 128, 64, dtype, page=32).fill()
+    everything = s.batch(s.lens)
+    k0, v0 = eq.eqat_kv_read(s.cache, everything)
+    b = batch(s, [10, 4], max_len=100 if by_table else reach, table=s.table[:, :reach // 32] if by_table else None)
+    k, v = (rows(s.gen, 14, 2, 128, dtype) for _ in "kv")
+    eq.eqat_kv_write(s.cache, b, k.cuda(), v.cuda())
+    k1, v1 = eq.eqat_kv_read(s.cache, everything)
+    inside = max(0, reach - 90)
+    for before, now, new in ((k0, k1, k), (v0, v1, v)):
+        want = before.clone().cpu()
+        want[90:90 + inside] = as_type(ref.held(new[:inside], 64), dtype)
+        want[146:] = as_type(ref.held(new[10:], 64), dtype)
+        assert same(now.cpu(), want)
+    for got, new in zip(eq.eqat_kv_read(s.cache, b, k=torch.full_like(k, 7.0).cuda(), v=torch.full_like(v, 7.0).cuda()), (k, v)):
+        want = as_type(ref.held(new, 64), dtype)
+        want[inside:10] = 0
+        assert same(got.cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,ratio", [(3, 2), (90, 2), (300, 8)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 40), (False, 25)])
+def test_queries_beyond_a_bound_stand_where_they_stand(n, ratio, causal, window, dtype):
+    """attention of the newest tokens of 400 where the call was told of 350 positions: those from 350 on are not there, the queries at their own positions"""
+    s = Setup([(n, 400), (2, 30)], 2, 128, 64, dtype, page=32, seed=n + window).fill()
+    b = batch(s, [n, 2], max_len=350)
+    q = rows(s.gen, n + 2, 2 * ratio, 128, dtype)
+    lse = torch.empty((n + 2, 2 * ratio), dtype=torch.float32, device="cuda")
+    out = eq.eqat_kv_attention(s.cache, b, q.cuda(), causal=causal, window=window, lse=lse)
+    some = slice(0, n, max(1, n // 40))
+    want = ref.attention(q[:n], s.k[0], s.v[0], 64, causal=causal, window=window, gone=torch.arange(400) >= 350)
+    held_to(out[:n][some], lse[:n][some], want, dtype, "beyond", some)
+    held_to(out[n:], lse[n:], ref.attention(q[n:], s.k[1], s.v[1], 64, causal=causal, window=window), dtype, "beside")
+    if window == 25 and not causal:
+        assert bool((out[n - 1] == 0).all())                       # the last query sees from 375 on: nothing that is there
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,most,ratio", [(9, 5, 2), (150, 100, 2)])
+def test_more_new_tokens_than_the_bound(n, most, ratio, dtype):
+    """the first `most` of a sequence's new tokens, at their own positions; the rows of the others stay as they are"""
+    s = Setup([(n, 200), (2, 30)], 2, 128, 64, dtype, page=32).fill()
+    everything = s.batch(s.lens)
+    before = eq.eqat_kv_read(s.cache, everything)
+    b = batch(s, [n, 2], max_new=most)
+    new = [rows(s.gen, n + 2, 2, 128, dtype) for _ in "kv"]
+    eq.eqat_kv_write(s.cache, b, *(x.cuda() for x in new))
+    first = 200 - n
+    for was, now, x, xs in zip(before, eq.eqat_kv_read(s.cache, everything), new, (s.k, s.v)):
+        want = was.clone().cpu()
+        want[first:first + most] = as_type(ref.held(x[:most], 64), dtype)
+        want[228:] = as_type(ref.held(x[n:], 64), dtype)
+        assert same(now.cpu(), want)
+        xs[0][first:first + most], xs[1][28:] = x[:most], x[n:]
+    for got, x in zip(eq.eqat_kv_read(s.cache, b, *(torch.full((n + 2, 2, 128), 7.0, dtype=dtype, device="cuda") for _ in "kv")), new):
+        want = as_type(ref.held(x, 64), dtype)
+        want[most:n] = 7.0
+        assert same(got.cpu(), want)
+    q = rows(s.gen, n + 2, 2 * ratio, 128, dtype)
+    out = torch.full(q.shape, 7.0, dtype=dtype, device="cuda")
+    lse = torch.full(q.shape[:2], 7.0, dtype=torch.float32, device="cuda")
+    eq.eqat_kv_attention(s.cache, b, q.cuda(), out=out, lse=lse)
+    held_to(out[:most], lse[:most], ref.attention(q[:n], s.k[0], s.v[0], 64), dtype, "first", slice(0, most))
+    held_to(out[n:], lse[n:], ref.attention(q[n:], s.k[1], s.v[1], 64), dtype, "beside")
+    assert bool((out[most:n] == 7).all()) and bool((lse[most:n] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,window", [(7, 0), (7, 2), (7, 2 ** 31 - 1), (90, 0), (90, 2 ** 31 - 1)])
+def test_more_new_tokens_than_are_held(n, window, dtype):
+    """five tokens held, `n` of them new: the first rows stand before the beginning, are not written, read as zeros, see nothing"""
+    s = Setup([(5, 5), (0, 0), (2, 40)], 2, 128, 64, dtype, page=32).fill()
+    before = s.cache.pool.clone()
+    b = batch(s, [n, 3, 2])
+    new = [torch.cat([rows(s.gen, n - 5, 2, 128, dtype), x[0], rows(s.gen, 3, 2, 128, dtype), x[2][38:]]) for x in (s.k, s.v)]
+    eq.eqat_kv_write(s.cache, b, *(x.cuda() for x in new))
+    assert torch.equal(before, s.cache.pool)
+    for got, x in zip(eq.eqat_kv_read(s.cache, b, *(torch.full((n + 5, 2, 128), 7.0, dtype=dtype, device="cuda") for _ in "kv")), new):
+        want = as_type(ref.held(x, 64), dtype)
+        want[:n - 5], want[n:n + 3] = 0, 0
+        assert same(got.cpu(), want)
+    q = rows(s.gen, n + 5, 4, 128, dtype)
+    lse = torch.empty((n + 5, 4), dtype=torch.float32, device="cuda")
+    out = eq.eqat_kv_attention(s.cache, b, q.cuda(), window=window, lse=lse)
+    assert bool((out[:n - 5] == 0).all()) and bool((out[n:n + 3] == 0).all()) and bool((lse[:n - 5] == -math.inf).all()) and bool((lse[n:n + 3] == -math.inf).all())
+    many = 2 * n > 64                                             # (the reference's bounds of a sequence of many rows)
+    padded = torch.cat([rows(s.gen, 40, 4, 128, dtype), q[n - 5:n]]) if many else q[n - 5:n]
+    held_to(out[n - 5:n], lse[n - 5:n], ref.attention(padded, s.k[0], s.v[0], 64, window=window), dtype, "held", slice(-5, None))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [2, 80])
+def test_lengths_of_any_size(n, dtype):
+    """a length at the end of 32 bits, one that is negative: nothing is written or read beyond the table, queries see what a window leaves of what is there"""
+    s = Setup([(0, 96), (0, 64), (1, 33)], 2, 128, 64, dtype, page=32).fill()
+    before = s.cache.pool.clone()
+    b = batch(s, [n, n, 1], lens=[2 ** 31 - 1, -7, 33], max_len=96, table=s.table[:, :3])
+    k, v = (torch.cat([rows(s.gen, 2 * n, 2, 128, dtype), x[2][32:]]).cuda() for x in (s.k, s.v))
+    eq.eqat_kv_write(s.cache, b, k, v)
+    assert torch.equal(before, s.cache.pool)
+    kr, _ = eq.eqat_kv_read(s.cache, b)
+    assert bool((kr[:2 * n] == 0).all()) and same(kr[2 * n:].cpu(), as_type(ref.held(s.k[2][32:], 64), dtype))
+    q = rows(s.gen, 2 * n + 1, 2, 128, dtype)
+    for causal, window in ((True, 0), (True, 500), (False, 500), (True, 2 ** 31 - 1)):
+        lse = torch.empty((2 * n + 1, 2), dtype=torch.float32, device="cuda")
+        out = eq.eqat_kv_attention(s.cache, b, q.cuda(), causal=causal, window=window, lse=lse)
+        assert bool((out[n:2 * n] == 0).all())
+        if window == 500:
+            assert bool((out[:n] == 0).all())
+        elif window == 0:
+            held_to(out[:n], lse[:n], ref.attention(q[:n], s.k[0], s.v[0], 64, causal=False), dtype, "all")
+
+
+def test_a_captured_step_replayed_past_the_end():
+    """the replays whose token no longer fits leave the cache as it is"""
+    s = Setup([(0, 62), (0, 20)], 2, 128, 64, torch.bfloat16, page=32).fill()
+    table, lens = s.table[:, :2].contiguous().cuda(), i32([62, 20])
+    b = eq.KvBatch(table, lens, i32([0, 1, 2]), tokens=2, max_new=1, max_len=64)
+    k, v = (torch.zeros(2, 2, 128, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    def step():
+        lens.add_(1)
+        eq.eqat_kv_write(s.cache, b, k, v)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    lens.copy_(i32([62, 20]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    tokens = [[], []]
+    for t in range(5):
+        new = [rows(s.gen, 2, 2, 128, torch.bfloat16) for _ in "kv"]
+        k.copy_(new[0]); v.copy_(new[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        tokens[0].append(new[0]); tokens[1].append(new[1])
+    assert lens.tolist() == [67, 25]
+    now = eq.eqat_kv_read(s.cache, eq.KvBatch(table, i32([64, 25]), i32([0, 64, 89]), tokens=89, max_new=64, max_len=64))
+    for got, xs, new in zip(now, (s.k, s.v), tokens):
+        want = torch.cat([xs[0]] + [x[:1] for x in new[:2]] + [xs[1]] + [x[1:] for x in new])
+        assert same(got.cpu(), as_type(ref.held(want, 64), torch.bfloat16))
