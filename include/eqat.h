@@ -408,11 +408,11 @@ eqat_status eqat_dx_route(const eqat_desc *d, int block_ap, int32_t *route);
  *   Sequences  An eqat_kv_batch says, in device arrays, where the sequences of a call stand: sequence b holds lens[b] tokens, its position p on page
  *              table[b * table_stride + p / page_tokens] (at p % page_tokens), and its newest starts[b+1] - starts[b] tokens are the rows starts[b] .. starts[b+1] - 1 of
  *              the call's tensors: lens counts them in.  Either number may be 0, and there may be more new tokens than held ones (the first of them, which stand
- *              before the beginning, are not there).  The host gives bounds only (tokens = starts[sequences], max_new, max_len), so that a
- *              captured graph serves lengths and pages that change between its replays.  What lies beyond the bounds, or on a page outside the pool, is taken as not
- *              there: not written, read as zeros, not attended to; the tokens within keep their positions (a step replayed past the end writes nothing).  Of a sequence with
- *              more new tokens than max_new the first max_new rows are taken and the others left as they are.  Nothing outside the tensors and the pool is touched
- *              whatever stands in the arrays.
+ *              before the beginning, are not there).  The host gives bounds only (tokens, max_new, max_len), so that a captured graph serves lengths, pages and
+ *              numbers of new tokens that change between its replays.  What lies beyond the bounds, or on a page outside the pool, is taken as not there: not
+ *              written, read as zeros, not attended to; the tokens within keep their positions (a step replayed past the end writes nothing).  Of a sequence with
+ *              more new tokens than max_new the first max_new rows are taken; the others, and rows from starts[sequences] on, are left as they are.  Nothing
+ *              outside the tensors and the pool is touched whatever stands in the arrays.
  *   Tensors    [tokens, heads, head_dim] with any strides (in elements, of a token and of a head; elements of a head are contiguous), such as slices of the rows of
  *              a stacked q|k|v projection.  Pointers and strides in bytes are multiples of 16.
  *   Types      desc.act_dtype (bf16 or fp32) for every tensor; lse is fp32.
@@ -430,7 +430,7 @@ typedef struct eqat_kv_batch {
     const int32_t *table;   /* [sequences, table_stride] pages, device                          */
     const int32_t *lens;    /* [sequences] tokens held, the newest included, device             */
     const int32_t *starts;  /* [sequences + 1] first rows, not decreasing, starts[0] = 0, device */
-    int64_t tokens;         /* rows of the call's tensors                                       */
+    int64_t tokens;         /* rows of the call's tensors: starts[sequences] or more            */
     int32_t sequences, table_stride;
     int32_t max_new;        /* no sequence has more newest tokens                               */
     int32_t max_len;        /* none holds more tokens                                           */
@@ -458,7 +458,7 @@ eqat_status eqat_kv_read(const eqat_kv_desc *d, const eqat_kv_batch *b, void *K,
  *   out[t, h] = sum over j of softmax_j(scale q[t, h] . k^_j) v^_j,   lse[t, h] = ln(sum over j of exp(scale q . k^_j)),
  * j over the positions that the query, at position lens[b] - (new tokens) + (its place among them), sees.  A query that sees none gives zeros and lse -inf.
  * NaN or infinities at positions that a query does not see do not reach it.  Scores, softmax and sums are binary32.  With fp32 tensors the results are as near as
- * binary32 arithmetic; with bf16 p is rounded to 11 bits, and in sequences of more than 64 rows (new tokens x q_heads / heads) so may be queries, keys and values.
+ * binary32 arithmetic; with bf16 p is rounded to 11 bits, and where max_new x q_heads / heads is more than 64 so may be queries, keys and values.
  *   Q, out: [tokens, q_heads, head_dim];  lse: [tokens, q_heads] contiguous, or NULL.
  *   ws: eqat_kv_workspace_bytes bytes (independent of the batch but for max_new and max_len), 256-byte aligned, ZEROED ONCE by the caller before its first use.  Every call
  *   leaves the counters in it at zero; calls that share a workspace must not overlap in time.

@@ -474,10 +474,12 @@ void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &t, con
     };
     const bool prompts = has_prompts(s, b, a.ratio);
     if (prompts) {
-        a.from_rows = kStreamedRows + 1; a.to_rows = INT32_MAX;
+        // Where all sequences have as many new tokens as any may, one launch takes them all, and so it does where the arrays have changed since and some have fewer.
+        const bool all = b.tokens == (int64_t)b.sequences * b.max_new;
+        a.from_rows = all ? 1 : kStreamedRows + 1; a.to_rows = INT32_MAX;
         scratch(l.prompts);
         launch_kv_prompt(s, a, st);
-        if (b.tokens == (int64_t)b.sequences * b.max_new) return;        // all sequences have as many new tokens
+        if (all) return;
     }
     a.from_rows = 1; a.to_rows = prompts ? kStreamedRows + 1 : INT32_MAX;
     scratch(l.streamed);

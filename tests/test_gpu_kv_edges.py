@@ -183,3 +183,38 @@ def test_a_captured_step_replayed_past_the_end():
     for got, xs, new in zip(now, (s.k, s.v), tokens):
         want = torch.cat([xs[0]] + [x[:1] for x in new[:2]] + [xs[1]] + [x[1:] for x in new])
         assert same(got.cpu(), as_type(ref.held(want, 64), torch.bfloat16))
+
+
+# ---- rows that change between replays ----------------------------------------------------------------------------------------
+def test_replays_in_which_a_sequence_falls_short():
+    """captured with four sequences of 128 new tokens; replayed with starts that leave one of them a single token, or none"""
+    H, R, D, g = 2, 2, 128, 64
+    s = Setup([(128, 300)] * 4, H, D, g, torch.bfloat16, page=32).fill()
+    lens, starts = i32([300] * 4), i32([0, 128, 256, 384, 512])
+    b = eq.KvBatch(s.table.cuda(), lens, starts, tokens=512, max_new=128, max_len=300)
+    q, out = torch.zeros(512, H * R, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(512, H * R, D, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(512, H * R, device="cuda")
+    ws = eq.kv_workspace(s.cache, b, H * R)
+    def step():
+        eq.eqat_kv_attention(s.cache, b, q, out=out, lse=lse, ws=ws)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for counts in ([128, 128, 128, 1], [128, 20, 0, 128], [1, 1, 1, 1], [128, 128, 128, 128]):
+        starts.copy_(i32([sum(counts[:i]) for i in range(5)]))
+        qh = rows(s.gen, 512, H * R, D, torch.bfloat16)
+        q.copy_(qh)
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        at = 0
+        for i, n in enumerate(counts):
+            if n:
+                some = slice(at, at + n, max(1, n // 10))
+                padded = torch.cat([rows(s.gen, 40, H * R, D, torch.bfloat16), qh[at:at + n]])                # (the bounds of a sequence of many rows: one kernel takes all of this call)
+                held_to(out[some], lse[some], ref.attention(padded, s.k[i], s.v[i], g), torch.bfloat16, f"{counts} {i}", slice(40, 40 + n, max(1, n // 10)))
+            at += n
+        assert bool((out[at:] == 7).all()) and bool((lse[at:] == 7).all())
