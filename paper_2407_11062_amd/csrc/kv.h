@@ -90,6 +90,14 @@ template <typename T> __device__ __forceinline__ T lane_sums(T x)
     x += from(x, IC<0x142>{}, IC<0xA>{}); x += from(x, IC<0x143>{}, IC<0xC>{});
     return x;
 }
+// the greatest of the wave, the same way
+__device__ __forceinline__ uint32_t lanes_greatest(uint32_t x)
+{
+    auto from = [](uint32_t v, auto ctrl, auto rows) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, true); };
+    x = max(x, from(x, IC<0x111>{}, IC<0xF>{})); x = max(x, from(x, IC<0x112>{}, IC<0xF>{})); x = max(x, from(x, IC<0x114>{}, IC<0xF>{})); x = max(x, from(x, IC<0x118>{}, IC<0xF>{}));
+    x = max(x, from(x, IC<0x142>{}, IC<0xA>{})); x = max(x, from(x, IC<0x143>{}, IC<0xC>{}));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
 
 // x / d for 0 <= x, 0 < d: twice by a reciprocal, the second time of what the first left (its error is below 2^10), and put right by one.  The compiler's own is four
 // times as long, and these stand in a row before anything is fetched.

@@ -8,10 +8,11 @@
 //   q . k^_t   = sum over groups g of  s_tg (q_g . c_tg) + m_tg sum(q_g)
 //   sum_t p_t v^_td = sum_t (p_t s_tg) c_td  +  sum_t p_t m_tg
 // The products with codes run on the matrix cores, everything else in binary32; no key or value is ever rebuilt.  q and p s are binary16 there: q of bf16 exactly
-// (scaled by a power of two per row), p s to 11 bits, and with fp32 activations both as the sum of two such numbers (22 bits).
+// (scaled by a power of two per row; elements 2^26 below its largest to what that leaves), p s to 11 bits, and with fp32 activations both as the sum of two such numbers
+// (22 bits).  The values' steps say by what power of two p is held, so that p s keeps its bits far below the largest p and however small the values are.
 // A matrix instruction drops what lies 2^-26 below its largest term, its addend among them.  With fp32 activations the two parts and the records are therefore added
 // up outside, and codes are taken as c - 8 about m + 8 s, which leaves less to cancel between the two sums.  The softmax keeps a running maximum
-// and sum; the maximum moves only when a score passes it by 2 in log2, so that most records rescale nothing (p <= 4, and s < 2^14, so p s stays in binary16).
+// and sum; the maximum moves only when a score passes it by 2 in log2, so that most records rescale nothing (p <= 4).
 //
 // 32 sequences of 32768 tokens, 64 heads on 8 of 128: 145 us, 5.3 TB/s (a large copy: 4.8).  A token at 515, 32 heads of 128: 8.1 us, of which the way to the first
 // record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 17.5 us for 44 MB.
@@ -54,7 +55,7 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
 {
     using R = KvRecord<NS, SG>;
     using T = typename std::conditional<F32, float, bf16_t>::type;
-    constexpr int D = R::D, G = R::G, kChunks = NS / 2, kPad = D + 4, kWaves = waves_of(D), kDepth = depth_of(D), kStepLoads = (G + 3) / 4, kLoads = 2 * kChunks + kStepLoads;
+    constexpr int D = R::D, G = R::G, kChunks = NS / 2, kPad = D + 4, kWaves = waves_of(D), kDepth = depth_of(D), kStepLoads = (G + 3) / 4, kLoads = 2 * kChunks + kStepLoads, kStepWords = (G + 1) / 2;
     constexpr float kUnit = F32 ? 1.0f : 0x1p24f;          // what a code's binary16 form is divided by
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];              // the waves' rings; then the waves' sums [wave][row][kPad]
     __shared__ float s_ml[kWaves][kRowsOfUnit][2];
@@ -76,14 +77,15 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
         const int pos = w.s.pos + query;
         const int seen_to = is_row && a.causal ? min(w.s.len, pos + 1) : w.s.len;             // positions seen_from .. seen_to - 1 (a row that is none restricts nothing)
         const int seen_from = is_row ? window_from(pos, a.window) : 0;
-        // Records w.rec + wave, + kWaves, ...: lane i looks up where the i-th of 64 of them lies (-1: its page is not there).
-        const int32_t *table = a.b.table + (int64_t)w.b * a.b.table_stride;
-        int place_lo = -1, place_hi = -1;
+        // Records w.rec + wave, + kWaves, ...: lane i looks up the number in the pool of the i-th of 64 of them (-1: its page is not there).  Without a branch: lanes past the
+        // last record read beyond the table's buffer.
+        const __amdgpu_buffer_rsrc_t table = make_rsrc(a.b.table + (int64_t)w.b * a.b.table_stride, (uint32_t)min(a.b.table_stride, 1 << 28) * 4u);
+        int numbers = -1;
         auto look_up = [&](int from) {
             const int rec = from + lane * kWaves, of_seq = quotient(rec, a.page_records);
-            const int page = rec < w.rec_to ? table[of_seq] : -1;
-            const int64_t at = page >= 0 && page < a.pages ? (((int64_t)page * a.heads + head) * a.page_records + (rec - of_seq * a.page_records)) * R::kBytes : -1;
-            place_lo = (int)at; place_hi = (int)(at >> 32);
+            const bool is = rec < w.rec_to;
+            const int page = __builtin_amdgcn_raw_buffer_load_b32(table, is ? of_seq * 4 : (int)kOobOffset, 0, 0);
+            numbers = (is & (page >= 0) & (page < (int)a.pages)) ? (page * a.heads + head) * a.page_records + (rec - of_seq * a.page_records) : -1;
         };
         const int first_rec = w.rec + wave, records = max(0, (w.rec_to - first_rec + kWaves - 1) / kWaves);
         look_up(first_rec);
@@ -99,9 +101,9 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
         uint64_t gone = 0;                                     // bit i & 63: the i-th record is not there
         auto fetch = [&](int i) {
             if (i > 0 && (i & 63) == 0) look_up(first_rec + i * kWaves);
-            const int64_t place = (int64_t)(uint32_t)__builtin_amdgcn_readlane(place_lo, i & 63) | (int64_t)__builtin_amdgcn_readlane(place_hi, i & 63) << 32;
-            gone = place < 0 ? gone | (uint64_t)1 << (i & 63) : gone & ~((uint64_t)1 << (i & 63));
-            const RawRsrc src = make_raw_rsrc(a.pool + (place < 0 ? 0 : place), R::kBytes);
+            const int number = __builtin_amdgcn_readlane(numbers, i & 63);
+            gone = number < 0 ? gone | (uint64_t)1 << (i & 63) : gone & ~((uint64_t)1 << (i & 63));
+            const RawRsrc src = make_raw_rsrc(a.pool + (int64_t)max(number, 0) * R::kBytes, R::kBytes);
             const uint32_t to = ring_at + (uint32_t)(i % kDepth) * R::kBytes;
 #pragma unroll
             for (int k = 0; k < 2 * kChunks; ++k) load_to_lds16_at(src, to + k * 1024, (uint32_t)(k * 1024 + lane * 16));
@@ -147,17 +149,32 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
         }
         // ---- the records of this wave -----------------------------------------------------------------
         floatx4 o[2 * NS];
-        float top = -3.0e38f, total = 0.0f, even[G];            // running maximum, sum of p, sum of p m
-        float v_scale = 1.0f;                                   // fp32: what the accumulators are scaled by
+        // Running maximum (rounded up to a whole number, so that powers of two are exact), what scores have taken off them, sum of p, sum of p m.  p is held times 2^bias, and so
+        // are the sums: the largest value step so far is below 2^(13 - bias), so p s (p at most 4) stays in binary16, and one that lies 2^25 below the largest is normal there.
+        float top = -3.0e38f, off = top, total = 0.0f, even[G];
+        int bias = 0;
+        uint32_t steps_to = 0;                                  // the last binary16 number, as bits, that `bias` was made for
 #pragma unroll
         for (int n = 0; n < 2 * NS; ++n) o[n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int g = 0; g < G; ++g) even[g] = 0.0f;
+        // a maximum of 2^22 and more has no room for a bias in binary32: p s stays in binary16 without
+        auto settle = [&](float next) {
+            const float next_off = fabsf(next) < 4194304.0f ? next - (float)bias : next, down = exp2_of(off - next_off);
+            top = next; off = next_off;
+            total *= down;
+#pragma unroll
+            for (int g = 0; g < G; ++g) even[g] *= down;
+#pragma unroll
+            for (int n = 0; n < 2 * NS; ++n) o[n] *= down;
+        };
         // records that every row of the unit sees in full need no mask
         int all_from = seen_from, all_to = seen_to;
 #pragma unroll
         for (int d = 8; d >= 1; d >>= 1) { all_from = max(all_from, __shfl_xor(all_from, d)); all_to = min(all_to, __shfl_xor(all_to, d)); }
         all_from = __builtin_amdgcn_readfirstlane(all_from); all_to = __builtin_amdgcn_readfirstlane(all_to);
+        // what some row sees: from the first row's beginning to the last one's end
+        const int any_from = __builtin_amdgcn_readfirstlane(seen_from), any_to = __builtin_amdgcn_readlane(seen_to, min(kRowsOfUnit, w.s.n * a.ratio - w.unit * kRowsOfUnit) - 1);
 
         for (int i = 0; i < records; ++i) {
             const int rec = first_rec + i * kWaves;
@@ -171,6 +188,12 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
             asm volatile("" ::: "memory");
             if (gone >> (i & 63) & 1) continue;
             const uint8_t *at = ring + (i % kDepth) * R::kBytes;
+            const bool edge = rec * kKvRecord < all_from || (rec + 1) * kKvRecord > all_to;
+            // the values' steps, each in one lane (NaN is above every number)
+            auto step = [&](int k) { return (uint32_t)*reinterpret_cast<const uint16_t *>(at + R::kValueSteps + k * 256 + (lane & (G > 1 ? 63 : 31)) * 4); };
+            uint32_t steps = 0;
+#pragma unroll
+            for (int k = 0; k < kStepWords; ++k) steps = max(steps, step(k));
             uintx4 kc[kChunks], vc[kChunks], ks[G][2], vs[G][2];
 #pragma unroll
             for (int k = 0; k < kChunks; ++k) {
@@ -184,7 +207,19 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
                     ks[g][h] = *reinterpret_cast<const uintx4 *>(at + R::kKeySteps + g * 128 + h * 64 + c * 16);
                     vs[g][h] = *reinterpret_cast<const uintx4 *>(at + R::kValueSteps + g * 128 + h * 64 + c * 16);
                 }
-            const bool edge = rec * kKvRecord < all_from || (rec + 1) * kKvRecord > all_to;
+            if (__any(steps > steps_to)) {
+                // of those that are numbers and that some row sees
+                const int t = rec * kKvRecord + (lane & 31);
+                uint32_t big = 0;
+#pragma unroll
+                for (int k = 0; k < kStepWords; ++k) { const uint32_t u = step(k); big = max(big, u < 0x7C00u ? u : 0u); }
+                big = lanes_greatest(t >= any_from && t < any_to ? big : 0u);
+                if (big > steps_to) {
+                    steps_to = big < 0x400u ? 0xFFFFFFFFu >> __builtin_clz(big) : big | 0x3FFu;
+                    bias = 139 - (int)(__float_as_uint(low_half(big)) >> 23);
+                    settle(top);
+                }
+            }
             float s[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -222,44 +257,15 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
             }
             float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
             most = chunks_max(most) * k_scale;
-            if (__any(most > top + 2.0f)) {
-                const float next = fmaxf(top, most), down = exp2_of(top - next);
-                top = next;
-                total *= down;
-#pragma unroll
-                for (int g = 0; g < G; ++g) even[g] *= down;
-#pragma unroll
-                for (int n = 0; n < 2 * NS; ++n) o[n] *= down;
-            }
+            if (__any(most > top + 2.0f)) settle(fmaxf(top, __builtin_ceilf(most)));
             float p[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[h][i] = exp2_of(__builtin_fmaf(s[h][i], k_scale, -top));
+                    p[h][i] = exp2_of(__builtin_fmaf(s[h][i], k_scale, -off));
                     total += p[h][i];
                 }
-            if constexpr (F32) {
-                // two binary16 numbers hold 22 bits of p s only where its low part does not run into denormals: values' steps are brought to about 2^11 by a power of two
-                uint32_t big = 0;
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { const float v = low_half(vs[g][h][i]); big = max(big, v < 65536.0f ? __float_as_uint(v) : 0u); }
-                if (edge) {                      // rows see different tokens
-#pragma unroll
-                    for (int d = 8; d >= 1; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
-                }
-                const float most_step = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(chunks_max(__uint_as_float(big)))));
-                if (most_step * v_scale >= 4096.0f || (v_scale == 1.0f && most_step > 0.0f)) {
-                    const float next = __uint_as_float((uint32_t)(127 + 138 - (int)(__float_as_uint(most_step) >> 23)) << 23);
-#pragma unroll
-                    for (int n = 0; n < 2 * NS; ++n) o[n] *= next / v_scale;
-                    v_scale = next;
-                }
-            }
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 uintx4 ph, pl;
@@ -270,9 +276,9 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
 #pragma unroll
                     for (int i = 0; i < 4; i += 2) {
                         if constexpr (F32) {
-                            float x = p[h][i] * v_scale * low_half(vs[g][h][i]), y = p[h][i + 1] * v_scale * low_half(vs[g][h][i + 1]);
+                            float x = p[h][i] * low_half(vs[g][h][i]), y = p[h][i + 1] * low_half(vs[g][h][i + 1]);
                             asm("" : "+v"(x), "+v"(y));          // both uses below round the binary32 product (a mixed-precision product rounds once, and not to the same number)
-                            const half2v hi = {(_Float16)x, (_Float16)y}, lo = {(_Float16)(x - (float)hi[0]), (_Float16)(y - (float)hi[1])};
+                            const half2v hi = {(_Float16)x, (_Float16)y}, lo = {(_Float16)((x - (float)hi[0]) * 0x1p11f), (_Float16)((y - (float)hi[1]) * 0x1p11f)};
                             ph[h * 2 + i / 2] = __builtin_bit_cast(uint32_t, hi);
                             pl[h * 2 + i / 2] = __builtin_bit_cast(uint32_t, lo);
                         } else {
@@ -287,7 +293,8 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
                     for (int q = 0; q < 4; ++q) codes[q] = pick<F32>(vc[n >> 2][q], n & 3);
                     if constexpr (F32) {
                         const floatx4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                        o[n] += mfma(codes, __builtin_bit_cast(half8, ph), zero) + mfma(codes, __builtin_bit_cast(half8, pl), zero);
+                        const floatx4 low = mfma(codes, __builtin_bit_cast(half8, pl), zero), down = {0x1p-11f, 0x1p-11f, 0x1p-11f, 0x1p-11f};
+                        o[n] += __builtin_elementwise_fma(low, down, mfma(codes, __builtin_bit_cast(half8, ph), zero));
                     } else {
                         o[n] = mfma(codes, __builtin_bit_cast(half8, ph), o[n]);
                     }
@@ -298,9 +305,10 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
         // ---- the waves' sums joined ---------------------------------------------------------------------
         float (*s_o)[kRowsOfUnit][kPad] = reinterpret_cast<float (*)[kRowsOfUnit][kPad]>(lds);
         __syncthreads();                                          // the rings have been read
-        total = chunks_sum(total);
+        const float unit = exp2_of(off - top);                    // 2^-bias
+        total = chunks_sum(total) * unit;
 #pragma unroll
-        for (int g = 0; g < G; ++g) even[g] = chunks_sum(even[g]);
+        for (int g = 0; g < G; ++g) even[g] = chunks_sum(even[g]) * unit;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
             // products 2 j and 2 j + 1: elements 32 j + 8 c + 0 .. 7
@@ -308,7 +316,7 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int n = 2 * j + (i & 1);
-                x[i] = __builtin_fmaf(o[n][i >> 1], (n & 1 ? kUnit / 16.0f : kUnit) / v_scale, even[j / SG]);
+                x[i] = __builtin_fmaf(o[n][i >> 1], (n & 1 ? kUnit / 16.0f : kUnit) * unit, even[j / SG]);
             }
             *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c]) = floatx4{x[0], x[1], x[2], x[3]};
             *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c + 4]) = floatx4{x[4], x[5], x[6], x[7]};

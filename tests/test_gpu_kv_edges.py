@@ -218,3 +218,43 @@ def test_replays_in_which_a_sequence_falls_short():
                 held_to(out[some], lse[some], ref.attention(padded, s.k[i], s.v[i], g), torch.bfloat16, f"{counts} {i}", slice(40, 40 + n, max(1, n // 10)))
             at += n
         assert bool((out[at:] == 7).all()) and bool((lse[at:] == 7).all())
+
+
+# ---- steep softmaxes, small values, extreme queries and scales ---------------------------------------------------------------
+def steep(seqs, gap, dtype, H=2, D=128, g=64, every=32):
+    """Every `every` positions a key that stands 2^gap above the others, its value zero: results are made of small probabilities alone."""
+    direction = torch.randn(D, generator=torch.Generator().manual_seed(int(gap)))
+    up = gap * math.log(2.0) * math.sqrt(D) / direction.square().sum() * direction
+    def keys(xs):
+        for x in xs:
+            x.mul_(0.05)
+            x[::every] = up.to(dtype)
+    def values(xs):
+        for x in xs:
+            x[::every] = 0
+    def queries(q):
+        q[:] = direction.to(dtype)
+    return Setup(seqs, H, D, g, dtype, key_edit=keys, value_edit=values).fill(), queries
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("gap", [12, 20, 26])
+@pytest.mark.parametrize("D,g", [(64, 32), (128, 64), (256, 256)])
+def test_steep_softmaxes_of_few_rows(D, g, gap, dtype):
+    """(in fp32 too: what lies 2^26 below the greatest is held to the same share of itself)"""
+    s, queries = steep([(1, 33), (3, 300), (1, 1700)], gap, dtype, D=D, g=g)
+    check(s, 4, q_edit=queries)
+
+
+@pytest.mark.parametrize("size", [1e-6, 1e-5, 1e-4])
+def test_small_values(size):
+    """a few steps of the cache's smallest: what they stand for is summed as well as larger values are"""
+    def small(xs):
+        for x in xs:
+            x.mul_(size)
+    check(Setup([(1, 33), (3, 300), (1, 1700)], 2, 128, 64, torch.bfloat16, value_edit=small).fill(), 4)
+    def mixed(xs):
+        for x in xs:
+            x[:len(x) // 2].mul_(size)
+            x[len(x) // 2:].mul_(3e3)
+    check(Setup([(1, 33), (3, 300), (1, 1700)], 2, 128, 64, torch.bfloat16, value_edit=mixed).fill(), 4)
