@@ -458,8 +458,9 @@ eqat_status eqat_kv_read(const eqat_kv_desc *d, const eqat_kv_batch *b, void *K,
  *   out[t, h] = sum over j of softmax_j(scale q[t, h] . k^_j) v^_j,   lse[t, h] = ln(sum over j of exp(scale q . k^_j)),
  * j over the positions that the query, at position lens[b] - (new tokens) + (its place among them), sees.  A query that sees none gives zeros and lse -inf.
  * NaN or infinities at positions that a query does not see do not reach it.  Scores, softmax and sums are binary32.  With fp32 tensors the results are as near as
- * binary32 arithmetic; with bf16 the products of p and a value's step are rounded to 11 bits (or to 2^-36 of their largest, where that is more), and where max_new x q_heads / heads
- * is more than 64 p, queries, keys and values may be rounded to 11 bits instead.
+ * binary32 arithmetic; with bf16 the products of p and a value's step are rounded to 11 bits (or to 2^-36 of their largest, where that is more).  Where max_new x q_heads / heads
+ * is more than 64, it may be p (or to 2^-36 of the largest), queries with the scale, keys and values that are rounded to 11 bits instead, keys and values to 2^-24 where
+ * that is more (below 2^-13; the cache has no finer steps).
  *   Q, out: [tokens, q_heads, head_dim];  lse: [tokens, q_heads] contiguous, or NULL.
  *   ws: eqat_kv_workspace_bytes bytes (independent of the batch but for max_new and max_len), 256-byte aligned, ZEROED ONCE by the caller before its first use.  Every call
  *   leaves the counters in it at zero; calls that share a workspace must not overlap in time.

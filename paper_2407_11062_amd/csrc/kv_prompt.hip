@@ -4,8 +4,8 @@
 // Bound by the matrix cores, by the exponentials and by the reads of LDS, about evenly, so a key or value is rebuilt once for the rows of the workgroup, and the products
 // for the scores of one tile stand between the exponentials of the one before it.  It lies in LDS in the order in which the matrix instructions' lanes take it (kv.h), which
 // is the order of the cache: writes and reads are 1 KB of neighbouring bytes.
-// Keys and values are halved on their way (m + s c may pass 65504 by a rounding), and held to 11 bits, as are queries with the scale of the scores in them, and p.  The
-// running maximum is the products' addend, so that a score is an exponent as it comes, and the sum of p is one product more, with ones.  Scores and sums are binary32.
+// Keys and values are halved on their way (m + s c may pass 65504 by a rounding), and held to 11 bits (2^-24 below 2^-13: of the cache's smallest steps that is one), as are
+// queries with the scale of the scores in them, and p.  The running maximum is the products' addend, so that a score is an exponent as it comes, and the sum of p is one product more, with ones.  Scores and sums are binary32.
 //
 // 8192 tokens, 64 heads on 8 of 128: 1140 to 1160 us, 950 TFLOP/s where a product of 8192^3 reaches 1207.  333 tokens, 32 heads of 128: 15.7 us, of which the first tile of a
 // workgroup takes 7 (launch, lengths, pages, records, each known only after the one before) and a tile 1.2.
@@ -15,6 +15,8 @@ namespace eqat {
 namespace {
 
 constexpr int kTile = 64;                          // tokens in LDS at a time, two records; two tiles of keys and two of values
+// p is held times 2^kRaised: up to four times the maximum stays in binary16, and what lies 2^27 below it is still rounded to all of its bits.
+constexpr float kRaised = 13.0f;
 // Rows of a workgroup: 256, or 64 where that leaves compute units without one; for heads of 256 it is 128 (two groups of rows a wave do not fit the registers, nor do four
 // waves' shares of a tile on its way).
 constexpr int kLargeWaves = 8, kSmallWaves = 4;
@@ -211,7 +213,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> _
     };
     floatx4 o[kColumns][2 * NS], sum[kColumns], s[4][kColumns];
     float top[kColumns];                                     // what a score has had taken off it, in its own fitted units
-    float limit[kColumns];                                   // above which a score moves it: 2, or anything before the row has seen something
+    float limit[kColumns];                                   // above which a score moves it: kRaised + 2, or anything before the row has seen something
     const floatx4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     const uintx4 ones = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
@@ -278,7 +280,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> _
             move |= most > limit[t];
         }
         if (__any(move)) {
-            // the maximum moves: always to the first tile's, later where a score passes it by 2 (p is at most 4)
+            // the maximum moves: always to the first tile's, later where a score passes it by 2.  (Scores of 2^22 and more have no room for kRaised in binary32.)
 #pragma unroll
             for (int t = 0; t < kColumns; ++t) {
                 float most = s[0][t][0];
@@ -288,9 +290,9 @@ template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> _
                     for (int i = 0; i < 4; ++i) most = fmaxf(most, s[h][t][i]);
                 most = chunks_max(most);
                 const bool moves = most > limit[t];
-                const float by = moves ? most : 0.0f, down = limit[t] > 0.0f ? exp2_of(-by) : 0.0f;
+                const float by = moves ? fabsf(most) < 4194304.0f ? most - kRaised : most : 0.0f, down = limit[t] > 0.0f ? exp2_of(-by) : 0.0f;
                 top[t] += by / back[t];
-                limit[t] = moves ? 2.0f : limit[t];
+                limit[t] = moves ? kRaised + 2.0f : limit[t];
                 sum[t] *= down;
 #pragma unroll
                 for (int n = 0; n < 2 * NS; ++n) o[t][n] *= down;

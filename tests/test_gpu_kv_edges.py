@@ -246,6 +246,22 @@ def test_steep_softmaxes_of_few_rows(D, g, gap, dtype):
     check(s, 4, q_edit=queries)
 
 
+@pytest.mark.parametrize("gap", [12, 20, 26])
+@pytest.mark.parametrize("D,g,H,n,past,ratio", [(64, 32, 2, 150, 0, 2), (128, 64, 2, 150, 0, 2), (256, 128, 2, 150, 0, 2), (128, 128, 8, 1100, 0, 8), (128, 64, 1, 80, 1420, 2)])
+def test_steep_softmaxes_of_prompts(D, g, H, n, past, ratio, gap):
+    """workgroups of few and of many rows, teams, units that are cut"""
+    s, queries = steep([(n, past + n)], gap, torch.bfloat16, H=H, D=D, g=g, every=64)
+    q = torch.empty(n, H * ratio, D, dtype=torch.bfloat16)
+    queries(q)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
+    out = eq.eqat_kv_attention(s.cache, s.batch([n]), q.cuda(), lse=lse)
+    some = slice(1, n, n // 12)
+    for head in (0, H * ratio - 1):
+        one = slice(head // ratio, head // ratio + 1)
+        want = ref.attention(q[:, head:head + 1], s.k[0][:, one], s.v[0][:, one], g)
+        held_to(out[some, head:head + 1], lse[some, head:head + 1], want, torch.bfloat16, "steep", some)
+
+
 @pytest.mark.parametrize("size", [1e-6, 1e-5, 1e-4])
 def test_small_values(size):
     """a few steps of the cache's smallest: what they stand for is summed as well as larger values are"""
