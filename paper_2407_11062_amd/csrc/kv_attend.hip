@@ -255,15 +255,20 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
                         for (int g = 0; g < G; ++g) vs[g][h][i] = seen ? vs[g][h][i] : 0u;
                     }
             }
+            // (rounded before the maximum is taken off: what one rounding of both would leave of large scores is no small number)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[h][i] *= k_scale;
             float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            most = chunks_max(most) * k_scale;
+            most = chunks_max(most);
             if (__any(most > top + 2.0f)) settle(fmaxf(top, __builtin_ceilf(most)));
             float p[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[h][i] = exp2_of(__builtin_fmaf(s[h][i], k_scale, -off));
+                    p[h][i] = exp2_of(s[h][i] - off);
                     total += p[h][i];
                 }
 #pragma unroll

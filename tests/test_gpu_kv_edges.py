@@ -274,3 +274,16 @@ def test_small_values(size):
             x[:len(x) // 2].mul_(size)
             x[len(x) // 2:].mul_(3e3)
     check(Setup([(1, 33), (3, 300), (1, 1700)], 2, 128, 64, torch.bfloat16, value_edit=mixed).fill(), 4)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [4, 90])
+@pytest.mark.parametrize("scale", [1e8, 1e10, 2.0 ** 100])
+def test_large_scales(scale, n, dtype):
+    """scores that are far apart: one key a row, whatever the roundings"""
+    s = Setup([(n, 300)], 2, 128, 64, dtype).fill()
+    def sizes(q):
+        q[1::2] *= 1e-3
+        q[0] *= 2.0 ** -100
+        q[2] = 0
+    check(s, 2, scale=scale, q_edit=sizes)
