@@ -440,7 +440,7 @@ typedef struct eqat_kv_attn {
     int32_t q_heads;        /* a multiple of desc.heads: query head h reads head h / (q_heads / heads) */
     int32_t causal;         /* 0: every query sees all of its sequence; else positions up to its own   */
     int32_t window;         /* > 0: only the last `window` of the positions up to its own; 0: no limit */
-    float scale;            /* of the scores; 0: 1 / sqrt(head_dim)                                    */
+    float scale;            /* of the scores, up to 2^100; 0: 1 / sqrt(head_dim)                       */
 } eqat_kv_attn;
 
 size_t eqat_kv_pool_bytes(const eqat_kv_desc *d);                       /* 0 for a bad descriptor */
@@ -464,7 +464,8 @@ eqat_status eqat_kv_read(const eqat_kv_desc *d, const eqat_kv_batch *b, void *K,
  *   Q, out: [tokens, q_heads, head_dim];  lse: [tokens, q_heads] contiguous, or NULL.
  *   ws: eqat_kv_workspace_bytes bytes (independent of the batch but for max_new and max_len), 256-byte aligned, ZEROED ONCE by the caller before its first use.  Every call
  *   leaves the counters in it at zero; calls that share a workspace must not overlap in time.
- * EQAT_ERR_HYPER for a scale that is negative, infinite or NaN, or a negative window.
+ * EQAT_ERR_HYPER for a scale that is negative, NaN or more than 2^100, or a negative window.  Queries of any size serve, as long as scale q and the scores are binary32
+ * numbers.
  */
 size_t eqat_kv_workspace_bytes(const eqat_kv_desc *d, const eqat_kv_batch *b, int q_heads);
 eqat_status eqat_kv_attention(const eqat_kv_desc *d, const eqat_kv_batch *b, const eqat_kv_attn *a, const void *Q, const int64_t *q_strides,

@@ -194,7 +194,7 @@ const char *eqat_status_string(int status)
     case EQAT_ERR_ALIGN: return "pointer not 16-byte aligned (workspace: 256-byte)";
     case EQAT_ERR_WORKSPACE: return "workspace missing or too small";
     case EQAT_ERR_DEVICE: return "HIP launch failed";
-    case EQAT_ERR_HYPER: return "constants out of range (optimizer: 0 <= beta < 1, eps >= 0, step >= 1; attention: scale >= 0 and finite, window >= 0)";
+    case EQAT_ERR_HYPER: return "constants out of range (optimizer: 0 <= beta < 1, eps >= 0, step >= 1; attention: 0 <= scale <= 2^100, window >= 0)";
     default: return "unknown status";
     }
 }

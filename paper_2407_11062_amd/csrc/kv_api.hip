@@ -132,7 +132,7 @@ eqat_status eqat_kv_attention(const eqat_kv_desc *d, const eqat_kv_batch *b, con
     KV_TRY(check_batch(b, s, &k));
     if (a == nullptr) return EQAT_ERR_NULL;
     KV_TRY(check_heads(s, k, a->q_heads));
-    if (!(a->scale >= 0.0f && a->scale <= 3.4e38f) || a->window < 0) return EQAT_ERR_HYPER;
+    if (!(a->scale >= 0.0f && a->scale <= 0x1p100f) || a->window < 0) return EQAT_ERR_HYPER;
     if (k.tokens == 0) return EQAT_OK;
     KV_TRY(check_rows(Q, q_strides, s, &t.q));
     KV_TRY(check_rows(out, out_strides, s, &t.out));

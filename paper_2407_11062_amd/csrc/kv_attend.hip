@@ -19,6 +19,7 @@
 #include "kv_work.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace eqat {
 namespace {
@@ -125,8 +126,12 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
                 for (int e = 0; e < 8; ++e) { x[j][e] = (float)loaded[j][e]; top = fmaxf(top, fabsf(x[j][e])); }
             // the row scaled by a power of two to a largest element in [2^13, 2^14): code products are sums of q c 2^-24 or, for the pairs in bits 4 - 7, of (q 2^-4) c 2^-20
             top = chunks_max(top);
-            const int up = min(max(140 - (int)(__float_as_uint(top) >> 23), -100), 100);
+            const int up = min(140 - (int)(__float_as_uint(top) >> 23), 126);
             const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
+#pragma unroll
+            for (int j = 0; j < NS; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] *= scale;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float s = 0.0f;
@@ -134,18 +139,22 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
                 for (int j = 0; j < SG; ++j)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s += x[g * SG + j][e];
-                sums[g] = chunks_sum(s) * scale * (1.0f / kUnit);
+                sums[g] = chunks_sum(s) * (1.0f / kUnit);
             }
 #pragma unroll
             for (int j = 0; j < NS; ++j)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float y = x[j][e] * scale, f = (e >> 1) & 1 ? 0x1p-4f : 1.0f;
+                    const float y = x[j][e], f = (e >> 1) & 1 ? 0x1p-4f : 1.0f;
                     const _Float16 h = (_Float16)(y * f);
                     qh[j][e] = h;
                     if constexpr (F32) ql[j][e] = (_Float16)(y * f - (float)h);
                 }
-            k_scale = a.scale * __uint_as_float((uint32_t)(127 - up) << 23) * kUnit;
+            // The scale of the scores, all powers of two taken back, as a normal binary32 number.  Beyond 2^126 a row has one key, or some that are alike, whatever the power:
+            // what is left off here comes back with the maximum.  Below 2^-126 all scores are nothing, but a hidden one has to stay -inf.
+            const int back = (F32 ? 0 : 24) - up, lowered = max(a.scale_exponent + back - 126, 0);
+            k_scale = fmaxf(__builtin_amdgcn_ldexpf(a.scale, back - lowered), 0x1p-126f);
+            s_ml[wave][r][0] = __builtin_amdgcn_ldexpf(1.0f, lowered);
         }
         // ---- the records of this wave -----------------------------------------------------------------
         floatx4 o[2 * NS];
@@ -326,7 +335,7 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
             *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c]) = floatx4{x[0], x[1], x[2], x[3]};
             *reinterpret_cast<floatx4 *>(&s_o[wave][r][32 * j + 8 * c + 4]) = floatx4{x[4], x[5], x[6], x[7]};
         }
-        if (c == 0) { s_ml[wave][r][0] = top; s_ml[wave][r][1] = total; }
+        if (c == 0) { s_ml[wave][r][0] = fmaxf(top * s_ml[wave][r][0], -3.0e38f); s_ml[wave][r][1] = total; }
         __syncthreads();
         constexpr int kOut = kWaves == 8 && D == 128 ? 4 : D / 16, kOfRow = D / kOut;      // elements of a row that a thread takes, threads of a row
         const bool joins = tid < kRowsOfUnit * kOfRow;
@@ -481,6 +490,7 @@ void launch_kv_attend(const KvShape &s, const KvBatch &b, const KvAttend &t, con
     a.pool = static_cast<const uint8_t *>(pool);
     a.pages = s.pages; a.heads = s.heads; a.ratio = t.q_heads / s.heads; a.page_records = s.page_records; a.window = t.window; a.causal = t.causal;
     a.scale = t.scale * 1.4426950408889634f;
+    a.scale_exponent = std::ilogb(a.scale);
     auto scratch = [&](const Scratch &x) {
         a.counters = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ws) + x.counters);
         a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + x.parts);

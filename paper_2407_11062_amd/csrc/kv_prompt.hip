@@ -75,7 +75,7 @@ template <int NS, int SG, int kPromptWaves, int kColumns, int TEAMS, bool CUT> _
         // The row with the scale of the scores in it, 2 for the halved keys and log2(e); a power of two more, taken back from the scores, where binary16 would not hold
         // it well: in rows far larger or smaller than those of a model.
         const float scale = a.scale * 2.0f, most = chunks_max(top) * scale;
-        const int fit = most > 32768.0f || (most > 0.0f && most < 0x1p-8f) ? min(max(127 - (int)(__float_as_uint(most) >> 23), -100), 100) : 0;
+        const int fit = most > 32768.0f || (most > 0.0f && most < 0x1p-8f) ? min(max(127 - (int)(__float_as_uint(most) >> 23), -126), 100) : 0;
         const float fitted = __uint_as_float((uint32_t)(127 + fit) << 23);
         back[t] = __uint_as_float((uint32_t)(127 - fit) << 23);
         fits |= fit != 0;

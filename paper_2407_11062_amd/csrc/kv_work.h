@@ -19,6 +19,7 @@ struct AttendArgs {
     int from_rows, to_rows;                        // the launch takes the sequences with from_rows <= rows < to_rows
     bool causal;
     float scale;                                   // times log2(e)
+    int scale_exponent;                            // 2^scale_exponent <= scale < 2^(scale_exponent + 1)
 };
 
 // Where a launch's counters and parts lie in the workspace: two parts for each of the streamed kernel's workgroups, and for each chunk that prompts are cut into (a cut

@@ -287,3 +287,27 @@ def test_large_scales(scale, n, dtype):
         q[0] *= 2.0 ** -100
         q[2] = 0
     check(s, 2, scale=scale, q_edit=sizes)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [4, 90])
+@pytest.mark.parametrize("size", [2.0 ** 112, 2.0 ** 117, 2.0 ** 121, 2.0 ** -110, 2.0 ** -124])
+def test_queries_of_extreme_sizes(size, n, dtype):
+    s = Setup([(n, 300)], 2, 128, 64, dtype).fill()
+    def sizes(q):
+        q[1::2] *= size
+        q[2] = 0
+    check(s, 2, q_edit=sizes)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [4, 90])
+@pytest.mark.parametrize("scale", [1e-12, 1e-24, 1e-38])
+def test_small_scales(scale, n, dtype):
+    """all that a row sees counts alike, what it does not see stays hidden"""
+    s = Setup([(n, 300)], 2, 128, 64, dtype).fill()
+    def sizes(q):
+        q[1::2] *= 1e-3
+        q[0] *= 2.0 ** -100
+        q[2] = 0
+    check(s, 2, scale=scale, q_edit=sizes)
