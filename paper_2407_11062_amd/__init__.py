@@ -505,7 +505,7 @@ _NO_STRIDES = (None, None)
 def eqat_kv_write(cache: KvCache, batch: KvBatch, k, v):
     """The newest tokens' keys and values [tokens, heads, head_dim] (any token and head strides) into the cache."""
     (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
-    _check("eqat_kv_write", lib().eqat_kv_write(cache.ref, batch.ref, kp, ks[0], vp, vs[0], cache.pool.data_ptr(), _stream()))
+    _check("eqat_kv_write", lib().eqat_kv_write(cache.ref, batch.ref, kp, ks[0], vp, vs[0], _p(cache.pool), _stream()))
 
 
 def eqat_kv_read(cache: KvCache, batch: KvBatch, k=None, v=None, want=("k", "v")):
@@ -513,7 +513,7 @@ def eqat_kv_read(cache: KvCache, batch: KvBatch, k=None, v=None, want=("k", "v")
     if k is None and v is None:
         k, v = (torch.empty((batch.tokens, cache.heads, cache.head_dim), dtype=cache.dtype, device=cache.pool.device) if name in want else None for name in ("k", "v"))
     (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
-    _check("eqat_kv_read", lib().eqat_kv_read(cache.ref, batch.ref, kp, ks[0], vp, vs[0], cache.pool.data_ptr(), _stream()))
+    _check("eqat_kv_read", lib().eqat_kv_read(cache.ref, batch.ref, kp, ks[0], vp, vs[0], _p(cache.pool), _stream()))
     return k, v
 
 
@@ -532,7 +532,7 @@ def eqat_kv_attention(cache: KvCache, batch: KvBatch, q, scale=0.0, causal=True,
         raise ValueError("lse is fp32 [tokens, q_heads]")
     ws = kv_workspace(cache, batch, q_heads) if ws is None else ws
     a = _kv_attn_ref(q_heads, 1 if causal else 0, int(window), float(scale))
-    _check("eqat_kv_attention", lib().eqat_kv_attention(cache.ref, batch.ref, a, qp, qs[0], op, os_[0], _p(lse), cache.pool.data_ptr(),
+    _check("eqat_kv_attention", lib().eqat_kv_attention(cache.ref, batch.ref, a, qp, qs[0], op, os_[0], _p(lse), _p(cache.pool),
                                                         _p(ws), ws.numel(), _stream()))
     return out
 
