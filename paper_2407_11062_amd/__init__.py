@@ -440,12 +440,20 @@ def eqat_block_ap_update(hyper: AdamW, bits, group, W=None, dW=None, mW=None, vW
         _p(mz), _p(vz), _stream()))
 
 
+def _i32(name, value):
+    """A number that travels in 32 bits: ctypes would cut it without a word."""
+    value = int(value)
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{name} does not fit 32 bits: {value}")
+    return value
+
+
 class KvCache:
     """A pool of pages for keys and values in 4 bits, and its descriptor.  `pool`: the caller's own uint8 device tensor, 256-byte aligned."""
 
     def __init__(self, heads, head_dim, group, page_tokens, pages, dtype=torch.bfloat16, device="cuda", pool=None):
-        self.heads, self.head_dim, self.dtype = int(heads), int(head_dim), dtype
-        self.desc = KvDesc(int(pages), self.heads, self.head_dim, int(group), int(page_tokens), F32 if dtype == torch.float32 else BF16)
+        self.heads, self.head_dim, self.dtype = _i32("heads", heads), _i32("head_dim", head_dim), dtype
+        self.desc = KvDesc(_i32("pages", pages), self.heads, self.head_dim, _i32("group", group), _i32("page_tokens", page_tokens), F32 if dtype == torch.float32 else BF16)
         self.ref = ctypes.byref(self.desc)
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError(f"unsupported dtype {dtype}")
@@ -470,7 +478,7 @@ class KvBatch:
             raise ValueError("table is [sequences, pages], lens [sequences], starts [sequences + 1]")
         self.keep = (table, lens, starts)            # they must outlive the pointers
         self.tokens = int(tokens)
-        self.desc = KvBatchDesc(_p(table), _p(lens), _p(starts), self.tokens, B, table.shape[1], int(max_new), int(max_len))
+        self.desc = KvBatchDesc(_p(table), _p(lens), _p(starts), self.tokens, B, _i32("pages of a sequence", table.shape[1]), _i32("max_new", max_new), _i32("max_len", max_len))
         self.ref = ctypes.byref(self.desc)
 
 
@@ -487,7 +495,7 @@ def _kv_strides(shape, stride, tokens, heads, head_dim):
 
 @functools.lru_cache(maxsize=1024)
 def _kv_attn_ref(q_heads, causal, window, scale):
-    return ctypes.byref(KvAttn(q_heads, causal, window, scale))
+    return ctypes.byref(KvAttn(_i32("q_heads", q_heads), causal, _i32("window", window), scale))
 
 
 def _kv_rows(cache, batch, t, heads):
@@ -519,7 +527,7 @@ def eqat_kv_read(cache: KvCache, batch: KvBatch, k=None, v=None, want=("k", "v")
 
 def kv_workspace(cache: KvCache, batch: KvBatch, q_heads) -> torch.Tensor:
     """The workspace of eqat_kv_attention, zeroed as its first use wants it.  It serves every later call with bounds no larger than this batch's."""
-    n = lib().eqat_kv_workspace_bytes(cache.ref, batch.ref, int(q_heads))
+    n = lib().eqat_kv_workspace_bytes(cache.ref, batch.ref, _i32("q_heads", q_heads))
     return torch.zeros(max(n, 256), dtype=torch.uint8, device=cache.pool.device)
 
 

@@ -43,3 +43,29 @@ def test_pools_in_host_memory():
                  lambda: eq.eqat_kv_attention(cache, none, q, out=q, ws=OnTheDevice(1, 1, 1))):
         with pytest.raises(ValueError, match="device"):
             call()
+
+
+def test_numbers_beyond_32_bits():
+    """none of them is cut to its low half"""
+    big = 2 ** 32
+    for numbers in ((big + 2, 128, 64, 64, 3), (2, big + 128, 64, 64, 3), (2, 128, big + 64, 64, 3), (2, 128, 64, big + 64, 3), (2, 128, 64, 64, big + 3)):
+        with pytest.raises(ValueError, match="32 bits"):
+            eq.KvCache(*numbers, device="cpu")
+    class Counts(OnTheDevice):
+        def numel(self):
+            return self.shape[0]
+
+        def dim(self):
+            return len(self.shape)
+    lens, starts, table = Counts(2, dtype=torch.int32), Counts(3, dtype=torch.int32), Counts(2, 5, dtype=torch.int32)
+    assert eq.KvBatch(table, lens, starts, 4, 2, 100).desc.max_len == 100
+    for numbers in ((4, big + 2, 100), (4, 2, big + 100)):
+        with pytest.raises(ValueError, match="32 bits"):
+            eq.KvBatch(table, lens, starts, *numbers)
+    cache = eq.KvCache(2, 128, 64, 64, 3, device="cpu")
+    none = types.SimpleNamespace(ref=ctypes.byref(eq.KvBatchDesc(P, P, P, 0, 1, 1, 0, 0)), tokens=0)
+    q = OnTheDevice(0, 4, 128)
+    with pytest.raises(ValueError, match="32 bits"):
+        eq.eqat_kv_attention(cache, none, q, out=q, ws=OnTheDevice(1, 1, 1), window=big + 16)
+    with pytest.raises(ValueError, match="32 bits"):
+        eq.kv_workspace(cache, none, big + 4)
