@@ -311,3 +311,29 @@ def test_small_scales(scale, n, dtype):
         q[0] *= 2.0 ** -100
         q[2] = 0
     check(s, 2, scale=scale, q_edit=sizes)
+
+
+# ---- one workspace for several caches ----------------------------------------------------------------------------------------
+def test_a_workspace_serves_caches_of_other_shapes():
+    """layers whose heads differ in size and number share a workspace, zeroed once, large enough for each of them"""
+    def setup(seqs, H, D, g, ratio, dtype=torch.bfloat16):
+        s = Setup(seqs, H, D, g, dtype).fill()
+        b = s.batch([n for n, _ in s.seqs])
+        q = rows(s.gen, b.tokens, H * ratio, D, dtype).cuda()
+        return s, b, q, H * ratio
+    shapes = [setup([(1, 3000 + i) for i in range(5)], 8, 128, 128, 4), setup([(1, 4300 - 70 * i) for i in range(32)], 8, 64, 64, 1), setup([(1, 5000), (100, 700)], 300, 64, 64, 1),
+              setup([(90, 900), (2, 40)], 2, 128, 32, 2), setup([(2, 3000)], 3, 256, 64, 4, torch.float32)]
+    alone = [eq.eqat_kv_attention(s.cache, b, q) for s, b, q, _ in shapes]
+    ws = torch.zeros(max(len(eq.kv_workspace(s.cache, b, heads)) for s, b, _, heads in shapes), dtype=torch.uint8, device="cuda")
+    for turn in range(2):
+        for (s, b, q, _), want in zip(shapes, alone):
+            out = torch.full_like(q, 7.0)
+            eq.eqat_kv_attention(s.cache, b, q, out=out, ws=ws)
+            assert torch.equal(out, want), (turn, s.H, s.D)
+
+
+@pytest.mark.parametrize("n,L,B", [(70, 100, 80), (33, 700, 130), (200, 200, 66)])
+def test_prompts_of_more_sequences_than_lanes(n, L, B):
+    """some of them without new tokens, some with few"""
+    seqs = [((n, 2, 0)[i % 3], max(n, L - 3 * i)) for i in range(B)]
+    check(Setup(seqs, 2, 128, 64, torch.bfloat16, page=32).fill(), 2)
