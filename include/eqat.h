@@ -438,8 +438,8 @@ typedef struct eqat_kv_batch {
 
 typedef struct eqat_kv_attn {
     int32_t q_heads;        /* a multiple of desc.heads: query head h reads head h / (q_heads / heads) */
-    int32_t causal;         /* 0: every query sees all of its sequence; else positions up to its own   */
-    int32_t window;         /* > 0: only the last `window` of the positions up to its own; 0: no limit */
+    int32_t causal;         /* not 0: a query sees no position after its own; 0: those after it too    */
+    int32_t window;         /* > 0: of the positions up to its own it sees only the last `window`      */
     float scale;            /* of the scores, up to 2^100; 0: 1 / sqrt(head_dim)                       */
 } eqat_kv_attn;
 

@@ -14,8 +14,8 @@
 // up outside, and codes are taken as c - 8 about m + 8 s, which leaves less to cancel between the two sums.  The softmax keeps a running maximum
 // and sum; the maximum moves only when a score passes it by 2 in log2, so that most records rescale nothing (p <= 4).
 //
-// 32 sequences of 32768 tokens, 64 heads on 8 of 128: 145 us, 5.3 TB/s (a large copy: 4.8).  A token at 515, 32 heads of 128: 8.1 us, of which the way to the first
-// record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 17.5 us for 44 MB.
+// 32 sequences of 32768 tokens, 64 heads on 8 of 128: 145 us, 5.3 TB/s (a large copy: 4.8).  A token at 515, 32 heads of 128: 8.4 us, of which the way to the first
+// record (lengths, pages and queries, the record itself) takes 3 and the launch as much.  16 sequences of up to 4096, 64 heads on 8: 17.7 us for 44 MB.
 #include "kv_work.h"
 
 #include <algorithm>
@@ -24,13 +24,14 @@
 namespace eqat {
 namespace {
 
-constexpr int waves_of(int head_dim) { return head_dim > 128 ? 4 : 8; }         // of a workgroup, one on each compute unit
+constexpr int waves_of(int head_dim) { return head_dim > 128 ? 4 : 8; }         // of a workgroup, one on each compute unit (heads of 256 take 250 to 490 registers: one wave a SIMD)
 constexpr int kRowsOfUnit = 16;                    // rows (query, head of the group) of a unit
-constexpr int kFewestRecords = 32;                 // of a share: a join with another workgroup costs about as much (one token at 515: 32 8.1 us, 16 9.5, 8 9.3)
+constexpr int kFewestRecords = 32;                 // of a share: a join with another workgroup costs about as much (one token at 515: 32 8.4 us, 16 9.7, 8 9.5)
 constexpr int kFewParts = 4;                       // parts of a unit that are fetched together
 constexpr int kResident = 256;                     // compute units
 constexpr int workgroups_of(int head_dim, int groups, bool bf16) { return head_dim == 64 && (bf16 || groups == 1) ? 2 : 1; }          // that registers and LDS of a compute unit hold
-constexpr int depth_of(int head_dim) { return head_dim > 128 ? 2 : 3; }          // records of a wave's ring
+// Records of a wave's ring.  Heads of 256: 2 and 3 are alike (32 sequences of 16000, 8 heads, one group 189 and 191 us, groups of 32 271 and 267; one of 515 13.6 and 13.8).
+constexpr int depth_of(int head_dim) { return head_dim > 128 ? 2 : 3; }
 
 // f16(a * s.lo), f16(b * t.lo) in the halves of a register, s, t words whose low half is a binary16 number: the form that the compiler makes v_fma_mixlo_f16 and
 // v_fma_mixhi_f16 of, with the wait states that those owe
@@ -432,8 +433,8 @@ template <int NS, int SG, bool F32> __global__ __launch_bounds__(waves_of(32 * N
 }
 
 // Shares of the work of a head of the cache: no more workgroups than are resident (a second round of a few took as long as the first: 40 heads, 16 sequences of 8000
-// 131 us, with 7 shares a head for 6 192), and two a compute unit only where that leaves shares of 64 records (heads of 64 on 40, 8 sequences of 8000 48 us one, 42 two;
-// on 8, where it leaves 31, 16.5 and 17.8).
+// 126 us, with 7 shares a head for 6 198), and two a compute unit only where that leaves shares of 64 records (heads of 64 on 40, 8 sequences of 8000 46 us one, 42 two;
+// 32 in fp32, 32 sequences of 2000 60 and 51; on 8, where it leaves 31, 15.3 and 17.2).
 int most_shares_of(const KvShape &s, int workgroups) { return std::max(1, workgroups * kResident / s.heads); }
 int shares_of(const KvShape &s, const KvBatch &b, int ratio)
 {
@@ -442,11 +443,11 @@ int shares_of(const KvShape &s, const KvBatch &b, int ratio)
     return most_shares_of(s, large ? workgroups : 1);
 }
 
-// Sequences of more rows than this go to the kernel that rebuilds keys and values (bf16): for 64 rows this one takes 13.6 us and that one 22.6 (8000 tokens, 8 heads of
-// the cache), 9 and 17 us (500 tokens).
+// Sequences of more rows than this go to the kernel that rebuilds keys and values (bf16): for 64 rows this one takes 14.6 us and that one 26 (8000 tokens, 8 heads of
+// the cache), 8.7 and 16.8 us (500 tokens).
 constexpr int kStreamedRows = 64;
-// Where a call's units of 16 rows are no more than two for every compute unit, and its caches long, no sequence does: 256 rows of four sequences at 2000 tokens 31 us and 37,
-// 800 rows at 4000 44 and 49, but 2700 rows at 333 tokens 40 and 18.5.
+// Where a call's units of 16 rows are no more than two for every compute unit, and its caches long, no sequence does: 256 rows of four sequences at 2100 tokens 28 us and 38,
+// 800 rows at 4000 42 and 48, but 2700 rows at 333 tokens 37 and 18.5.
 bool has_prompts(const KvShape &s, const KvBatch &b, int ratio)
 {
     if (!s.act_bf16 || (int64_t)b.max_new * ratio <= kStreamedRows) return false;

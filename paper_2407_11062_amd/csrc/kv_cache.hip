@@ -5,8 +5,8 @@
 // a value eight half words (kv.h says where they stand).  A lane then stores a key's words of four j as they lie, 16 neighbouring bytes, and a group's least and
 // greatest element are found in a lane and two exchanges.  Half words of values go through LDS into the order of the record where all of it is written, and singly where not.
 //
-// 8192 tokens of 32 heads of 128, one group, bf16: a write takes 39 us for its 152 MB (3.9 TB/s), bound by arithmetic (18 instructions an element, 33 us of a SIMD's
-// issue), a read 28 us (5.4 TB/s; a large copy 4.8).  A token of 32 heads: 4.3 and 3.8 us, the launch.  Half words in banks of their own, stored by LDS instructions
+// 8192 tokens of 32 heads of 128, one group, bf16: a write takes 40 us for its 170 MB (4.2 TB/s), bound by arithmetic (18 instructions an element, 33 us of a SIMD's
+// issue), a read 28 us (6.1 TB/s; a large copy 4.8).  A token of 32 heads: 4.3 and 3.6 us, the launch.  Half words in banks of their own, stored by LDS instructions
 // rather than by flat ones: 42 and 29.
 #include "kv.h"
 

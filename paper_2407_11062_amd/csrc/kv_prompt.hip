@@ -5,9 +5,10 @@
 // for the scores of one tile stand between the exponentials of the one before it.  It lies in LDS in the order in which the matrix instructions' lanes take it (kv.h), which
 // is the order of the cache: writes and reads are 1 KB of neighbouring bytes.
 // Keys and values are halved on their way (m + s c may pass 65504 by a rounding), and held to 11 bits (2^-24 below 2^-13: of the cache's smallest steps that is one), as are
-// queries with the scale of the scores in them, and p.  The running maximum is the products' addend, so that a score is an exponent as it comes, and the sum of p is one product more, with ones.  Scores and sums are binary32.
+// queries with the scale of the scores in them, and p.  The running maximum is the products' addend, so that a score is an exponent as it comes, and the sum of p is one
+// product more, with ones.  Scores and sums are binary32.
 //
-// 8192 tokens, 64 heads on 8 of 128: 1140 to 1160 us, 950 TFLOP/s where a product of 8192^3 reaches 1207.  333 tokens, 32 heads of 128: 15.7 us, of which the first tile of a
+// 8192 tokens, 64 heads on 8 of 128: 1150 to 1160 us, 950 TFLOP/s where a product of 8192^3 reaches 1207.  333 tokens, 32 heads of 128: 15.9 us, of which the first tile of a
 // workgroup takes 7 (launch, lengths, pages, records, each known only after the one before) and a tile 1.2.
 #include "kv_work.h"
 
@@ -519,7 +520,7 @@ template <int NS, int SG> void launch(const AttendArgs &a, const PromptPlan &p, 
 
 // Workgroups of 256 rows where there is one for every compute unit, else of 64, two to a compute unit.  Where even those do not take half the places, sequences of more than
 // kFewest records are cut, and joined in a launch of its own (3 us).  Where caches are shorter and there is no more than one workgroup for a compute unit, it is two teams
-// (333 tokens, 32 heads 15.7 us for 16.5, 100 rows behind 411 tokens 17.0 for 20.2; one tile, 11.0 for 10.6, is one team's).  Heads of 256: two teams' tiles do not fit LDS.
+// (333 tokens, 32 heads 16.1 us for 16.8, 100 rows behind 411 tokens 17.2 for 20.4; one tile, 11.0 for 9.2, is one team's).  Heads of 256: two teams' tiles do not fit LDS.
 constexpr int kFewest = 16;
 PromptPlan prompt_plan(const KvShape &s, const KvBatch &b, int ratio)
 {
