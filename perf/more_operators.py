@@ -249,7 +249,7 @@ def prepare(case, seed):
         st["kind"] = {"silu": eq.GATE_SILU, "gelu": eq.GATE_GELU}[case["kind"]]
         if case["layer"] == "prepared":
             st["prepared"] = eq.eqat_qlinear_prepare(st["codes"], st["zero"], I, case["bits"], case["group"], act_dtype=eq.BF16 if dt == torch.bfloat16 else eq.F32)
-        st["ws"] = eq.gated_workspace(T, I, F, case["bits"], case["group"], dt, prepared=case["layer"] == "prepared", backward=op == "gated_back")
+        st["ws"] = eq.gated_workspace(T, I, F, case["bits"], case["group"], dt, prepared=case["layer"] == "prepared")
         st["out"] = {"H": new(T, F)}
         if op == "gated_back":
             st["out"]["dY"] = new(T, 2 * F)
