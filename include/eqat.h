@@ -68,7 +68,7 @@ typedef enum {
     EQAT_ERR_ALIGN = 6,     /* pointer not 16-byte (workspace: 256-byte) aligned */
     EQAT_ERR_WORKSPACE = 7, /* workspace missing or too small                    */
     EQAT_ERR_DEVICE = 8,    /* the HIP runtime refused a launch                  */
-    EQAT_ERR_HYPER = 9      /* optimizer or attention constants out of range     */
+    EQAT_ERR_HYPER = 9      /* optimizer, attention, norm, rotary, gate constants  */
 } eqat_status;
 
 typedef enum { EQAT_F32 = 0, EQAT_BF16 = 1 } eqat_dtype;
@@ -470,6 +470,100 @@ eqat_status eqat_kv_read(const eqat_kv_desc *d, const eqat_kv_batch *b, void *K,
 size_t eqat_kv_workspace_bytes(const eqat_kv_desc *d, const eqat_kv_batch *b, int q_heads);
 eqat_status eqat_kv_attention(const eqat_kv_desc *d, const eqat_kv_batch *b, const eqat_kv_attn *a, const void *Q, const int64_t *q_strides,
                               void *out, const int64_t *out_strides, float *lse, const void *pool, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * What a decoder layer computes around its quantized linears: the norm in front of them, the rotary positions of queries and keys, the gate of the feed-forward.  (Not part of the
+ * paper's method: what stands between the linears of the blocks that it trains and serves.)
+ *
+ * Root-mean-square norm with the residual's addition.
+ *   S = X + R, rounded to the activations' type (R NULL: S = X);   Y = w S / sqrt(mean S^2 + eps), the mean over the row's `width` elements of S as it stands (w NULL: ones)
+ *   codes, scales   Y in 8 bits instead of, or beside, Y: of `group` neighbouring elements scale = max(max |Y| / 448, 2^-126), codes = e4m3(Y / scale) (the finite-only 8-bit
+ *                   float with 4 exponent bits, largest 448), from Y before it is rounded; to nearest, ties to even.
+ *   Backward, of S (what the forward left in S, or its X without R), the gradients dY of Y and dS of S (along the residual; NULL: none):
+ *                   dX = dS + rstd (w dY - S rstd^2 mean(w dY S)),  which is the gradient of X and of R;   dw = sum over the rows of dY S rstd,   rstd = 1 / sqrt(mean S^2 + eps).
+ *   All tensors are contiguous: X, R, S, Y, dY, dS, dX [tokens, width] in act_dtype, w [width] in w_dtype, codes [tokens, width] bytes, scales [tokens, width / group] and dw [width]
+ *   fp32.  S may be X or R itself, Y may be any of the three, dX may be dY, dS or S (a row is read before it is written); no other overlap.
+ *   Sums, means and products are binary32: a row whose squares pass binary32 gives zeros, a NaN or infinity stays in its row (and in dw).
+ *   width: a multiple of 8, up to 32768 (a multiple of `group` where codes are asked for); group 32, 64, 128, 256 or 512, or -1: one scale a row.
+ *   tokens >= 0 of any number below 2^31; none leaves dw at zero.  eps >= 0, finite (EQAT_ERR_HYPER otherwise).
+ *   ws: eqat_norm_workspace_bytes(d) bytes, 256-byte aligned, wanted for dw only; contents undefined before and after.
+ * S, Y, (codes and scales together), dX and dw may each be NULL (skipped).  Same inputs give bitwise the same outputs.
+ */
+typedef struct eqat_norm_desc {
+    int64_t tokens;
+    int32_t width;
+    int32_t group;          /* of a scale; ignored without codes                                */
+    int32_t act_dtype;      /* eqat_dtype                                                       */
+    int32_t w_dtype;        /* eqat_dtype of w                                                  */
+    float eps;
+} eqat_norm_desc;
+
+eqat_status eqat_norm_fwd(const eqat_norm_desc *d, const void *X, const void *R, const void *w, void *S, void *Y, uint8_t *codes, float *scales, void *stream);
+size_t eqat_norm_workspace_bytes(const eqat_norm_desc *d);                /* 0 for a bad descriptor or no tokens */
+eqat_status eqat_norm_bwd(const eqat_norm_desc *d, const void *S, const void *w, const void *dY, const void *dS, void *dX, float *dw, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Rotary positions.  The first `part` elements of every head are part / 2 pairs, (i, i + part / 2) or, interleaved, (2 i, 2 i + 1); pair i of a token at position p becomes
+ *   (a, b) -> amplitude (a cos t - b sin t, b cos t + a sin t),   t = p frequencies[i],
+ * the other elements stay.  The frequencies are the caller's (device, fp32, part / 2 of them): base^(-2 i / part), or any scaling of them for long contexts.  The angle is held in
+ * binary64, so that far positions keep it; cosine and sine are good to binary32.  `inverse` turns back by the same angles with the same amplitude: the transpose, which is
+ * the backward pass (gradients of the turned tensors in, of the tensors out).
+ *   positions   int32 [tokens], device, any values.
+ *   Q, K        [tokens, heads, head_dim] in act_dtype, strides { token, head } in elements; pointers and strides in bytes are multiples of 16, elements of a head contiguous.
+ *               Either may be NULL (with its output).  An output may be its input (same pointer and strides); no other overlap.
+ *   head_dim    a multiple of 8 up to 1024; part even, 2 .. head_dim.  tokens x heads below 2^31.
+ * EQAT_ERR_HYPER for an amplitude that is not finite.
+ */
+typedef struct eqat_rotary_desc {
+    const float *frequencies;   /* [part / 2], device                                            */
+    int32_t head_dim, part;
+    int32_t interleaved;        /* not 0: pairs are neighbours                                   */
+    int32_t act_dtype;          /* eqat_dtype                                                    */
+    float amplitude;
+} eqat_rotary_desc;
+
+eqat_status eqat_rotary(const eqat_rotary_desc *d, int64_t tokens, const int32_t *positions, const void *Q, const int64_t *q_strides, int q_heads, void *q_out,
+                        const int64_t *q_out_strides, const void *K, const int64_t *k_strides, int k_heads, void *k_out, const int64_t *k_out_strides, int inverse, void *stream);
+
+/*
+ * A served model's step into the 4-bit cache, in one launch: the queries of the newest tokens turned into q_out, their keys turned and, rounded to act_dtype, written into the cache
+ * with the values; the positions are those that `b` gives.  Bitwise what eqat_rotary (with those positions) and eqat_kv_write do one after the other.  K and V are only read.  Rows
+ * of q_out behind the last sequence, and those of a sequence beyond b->max_new, are left as they are; queries of tokens that are not there (beyond the bounds, on no page) are
+ * turned by their position all the same.  head_dim and act_dtype of both descriptors have to agree (EQAT_ERR_SHAPE, EQAT_ERR_DTYPE).  q_out may be Q itself, with its strides.
+ */
+eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, const eqat_rotary_desc *r, const void *Q, const int64_t *q_strides, int q_heads, void *q_out,
+                                 const int64_t *q_out_strides, const void *K, const int64_t *k_strides, const void *V, const int64_t *v_strides, void *pool, void *stream);
+
+/*
+ * Gated feed-forward:  H = act(G) U,  G = X Wg^T and U = X Wu^T two projections stacked in one layer of 2 F output rows, the F rows of Wg first.
+ *   kind   EQAT_GATE_SILU  act(x) = x / (1 + exp(-x));   EQAT_GATE_GELU  act(x) = x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2
+ *
+ * eqat_gate_fwd / _bwd: element by element, for projections of any kind (Y = [G | U] as eqat_fq_linear_fwd leaves it on stacked weights).
+ *   Y, dY [tokens, 2 F], H, dH [tokens, F] in `dtype`, contiguous; F a multiple of 8.  dY = [dH U act'(G) | dH act(G)].  In the backward pass H, or dY, may be NULL (skipped); dY
+ *   may be Y itself, H may be dH itself; no other overlap.
+ *
+ * eqat_gated_fwd / _bwd: both projections from the packed layer, the activation and the product in one kernel where activations are bf16 (G and U are not rounded and not stored):
+ *   d          the stacked layer: out_features = 2 F, F a multiple of 8; tokens, in_features, bits, group, act_dtype as for eqat_qlinear_fwd (w_dtype is ignored).
+ *   forward    X -> H [tokens, F].
+ *   backward   X, dH -> dY = [dH U act'(G) | dH act(G)] [tokens, 2 F], and H again (either may be NULL): both projections are made anew, so that a training step keeps X
+ *              alone between its passes; dY is what eqat_qlinear_bwd of the layer takes (dX, ds), H the input of the next linear in its own backward pass.
+ *   _prepared  the same on a layer prepared by eqat_qlinear_prepare, s the current step sizes, the zero points those that it was prepared with.  Like the calls of eqat_qlinear_fwd_prepared,
+ *              calls on one prepared layer must not overlap in time.
+ *   ws         eqat_gated_workspace_bytes(d, prepared) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
+ * With fp32 activations the projections are those of eqat_qlinear_fwd, in the workspace, and the gate a launch of its own.
+ * EQAT_ERR_HYPER for an unknown kind.
+ */
+typedef enum { EQAT_GATE_SILU = 0, EQAT_GATE_GELU = 1 } eqat_gate_kind;
+
+eqat_status eqat_gate_fwd(int64_t tokens, int64_t F, int32_t dtype, int kind, const void *Y, void *H, void *stream);
+eqat_status eqat_gate_bwd(int64_t tokens, int64_t F, int32_t dtype, int kind, const void *Y, const void *dH, void *dY, void *H, void *stream);
+size_t eqat_gated_workspace_bytes(const eqat_desc *d, int prepared);                 /* 0 for a bad descriptor */
+eqat_status eqat_gated_fwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, void *H, void *ws, size_t ws_bytes, void *stream);
+eqat_status eqat_gated_bwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, const void *dH, void *dY, void *H,
+                           void *ws, size_t ws_bytes, void *stream);
+eqat_status eqat_gated_fwd_prepared(const eqat_desc *d, int kind, const void *X, const void *prepared, const float *s, void *H, void *ws, size_t ws_bytes, void *stream);
+eqat_status eqat_gated_bwd_prepared(const eqat_desc *d, int kind, const void *X, const void *prepared, const float *s, const void *dH, void *dY, void *H,
+                                    void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Optional per-kernel timing (measurement aid, not part of the paper's method).

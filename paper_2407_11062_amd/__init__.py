@@ -20,6 +20,7 @@ LIB_PATH = os.environ.get("EQAT_LIB", os.path.join(_HERE, "libeqat.so"))   # EQA
 F32, BF16 = 0, 1
 OP_FQ_FWD, OP_FQ_BWD, OP_Q_FWD, OP_Q_BWD, OP_QP_FWD, OP_QP_BWD = 0, 1, 2, 3, 4, 5
 STATE_FQ_KEPT, STATE_Q_KEPT, STATE_PREPARED = 0, 1, 2
+GATE_SILU, GATE_GELU = 0, 1
 
 STATUS_NAMES = ["EQAT_OK", "EQAT_ERR_NULL", "EQAT_ERR_SHAPE", "EQAT_ERR_BITS", "EQAT_ERR_GROUP", "EQAT_ERR_DTYPE",
                 "EQAT_ERR_ALIGN", "EQAT_ERR_WORKSPACE", "EQAT_ERR_DEVICE", "EQAT_ERR_HYPER"]
@@ -34,6 +35,8 @@ EXPORTS = ["eqat_status_string", "eqat_validate_desc", "eqat_packed_w_bytes", "e
            "eqat_qlinear_bwd_prepared_kept", "eqat_unpack_state", "eqat_plan_item", "eqat_shared_item", "eqat_plan_scratch", "eqat_fwd_route", "eqat_dx_route",
            "eqat_recon_loss_workspace_bytes", "eqat_recon_loss", "eqat_recon_loss_static", "eqat_block_ap_update",
            "eqat_kv_pool_bytes", "eqat_kv_write", "eqat_kv_read", "eqat_kv_workspace_bytes", "eqat_kv_attention",
+           "eqat_norm_fwd", "eqat_norm_workspace_bytes", "eqat_norm_bwd", "eqat_rotary", "eqat_kv_rotary_write", "eqat_gate_fwd", "eqat_gate_bwd",
+           "eqat_gated_workspace_bytes", "eqat_gated_fwd", "eqat_gated_bwd", "eqat_gated_fwd_prepared", "eqat_gated_bwd_prepared",
            "eqat_profile_kernels", "eqat_profile_kernel_name",
            "eqat_profile_start", "eqat_profile_stop"]
 
@@ -62,6 +65,16 @@ class KvBatchDesc(ctypes.Structure):
 
 class KvAttn(ctypes.Structure):
     _fields_ = [("q_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("width", ctypes.c_int32), ("group", ctypes.c_int32), ("act_dtype", ctypes.c_int32), ("w_dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("frequencies", ctypes.c_void_p), ("head_dim", ctypes.c_int32), ("part", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("act_dtype", ctypes.c_int32),
+                ("amplitude", ctypes.c_float)]
 
 
 class EqatError(RuntimeError):
@@ -128,6 +141,19 @@ def lib():
         L.eqat_kv_read.argtypes = L.eqat_kv_write.argtypes
         L.eqat_kv_workspace_bytes.restype, L.eqat_kv_workspace_bytes.argtypes = sz, [kd, kb, ctypes.c_int]
         L.eqat_kv_attention.argtypes = [kd, kb, ctypes.POINTER(KvAttn), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        kn, kr, i64, i32 = ctypes.POINTER(NormDesc), ctypes.POINTER(RotaryDesc), ctypes.c_int64, ctypes.c_int
+        L.eqat_norm_fwd.argtypes = [kn, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.eqat_norm_workspace_bytes.restype, L.eqat_norm_workspace_bytes.argtypes = sz, [kn]
+        L.eqat_norm_bwd.argtypes = [kn, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.eqat_rotary.argtypes = [kr, i64, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, i32, vp]
+        L.eqat_kv_rotary_write.argtypes = [kd, kb, kr, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.eqat_gate_fwd.argtypes = [i64, i64, ctypes.c_int32, i32, vp, vp, vp]
+        L.eqat_gate_bwd.argtypes = [i64, i64, ctypes.c_int32, i32, vp, vp, vp, vp, vp]
+        L.eqat_gated_workspace_bytes.restype, L.eqat_gated_workspace_bytes.argtypes = sz, [dp, i32]
+        L.eqat_gated_fwd.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.eqat_gated_bwd.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.eqat_gated_fwd_prepared.argtypes = [dp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.eqat_gated_bwd_prepared.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.eqat_profile_kernel_name.restype = ctypes.c_char_p
         L.eqat_profile_kernel_name.argtypes = [ctypes.c_int]
         L.eqat_profile_stop.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64), ctypes.c_int]
@@ -543,6 +569,202 @@ def eqat_kv_attention(cache: KvCache, batch: KvBatch, q, scale=0.0, causal=True,
     _check("eqat_kv_attention", lib().eqat_kv_attention(cache.ref, batch.ref, a, qp, qs[0], op, os_[0], _p(lse), _p(cache.pool),
                                                         _p(ws), ws.numel(), _stream()))
     return out
+
+
+# ---- norm, rotary positions, gated feed-forward ---------------------------------------------------------------------------------------------------------
+@functools.lru_cache(maxsize=1024)
+def _norm_ref(tokens, width, group, act_dtype, w_dtype, eps):
+    return ctypes.byref(NormDesc(tokens, _i32("width", width), _i32("group", group), act_dtype, w_dtype, eps))
+
+
+def _like(name, t, shape, dtype):
+    """The pointer of a tensor whose shape and type the call goes by; None stays None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    return _p(t)
+
+
+def _codes_ptr(codes, T, n):
+    if codes is None:
+        return None
+    if codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or tuple(codes.shape) != (T, n):
+        raise ValueError(f"codes: expected float8_e4m3fn or uint8 [{T}, {n}], got {codes.dtype} {list(codes.shape)}")
+    return _p(codes)
+
+
+def eqat_norm_fwd(X, W, eps, R=None, group=0, want=None, out=None):
+    """Root-mean-square norm of S = X + R (R None: of X) over the rows of [tokens, width]; W [width] or None.  `want`: which of "S", "Y", "codes" (float8_e4m3fn, with "scales", one
+    for `group` neighbouring elements, -1: a row) to make, by default Y, or the codes where a group is given, and S where R is; tensors in `out` are filled."""
+    T, n = X.shape
+    group = _i32("group", group)
+    if want is None:
+        want = (("S",) if R is not None else ()) + (("codes",) if group else ("Y",))
+    out = {} if out is None else out
+    per = 1 if group == -1 else n // group if group > 0 else 0
+    for name in ("S", "Y"):
+        if name in want and name not in out: out[name] = torch.empty_like(X)
+    codes = "codes" in want or "scales" in want
+    if codes:
+        if per == 0:
+            raise ValueError("codes need a group (-1: one scale a row)")
+        if "codes" not in out: out["codes"] = torch.empty((T, n), dtype=torch.float8_e4m3fn, device=X.device)
+        if "scales" not in out: out["scales"] = torch.empty((T, per), dtype=torch.float32, device=X.device)
+    get = lambda name: out.get(name) if name in want else None
+    d = _norm_ref(T, n, group if codes else -1, _dt(X), _dt(X) if W is None else _dt(W), float(eps))
+    _check("eqat_norm_fwd", lib().eqat_norm_fwd(
+        d, _p(X), _like("R", R, X.shape, X.dtype), _like("W", W, (n,), W.dtype) if W is not None else None, _like("S", get("S"), X.shape, X.dtype),
+        _like("Y", get("Y"), X.shape, X.dtype), _codes_ptr(out["codes"], T, n) if codes else None, _like("scales", out["scales"], (T, per), torch.float32) if codes else None, _stream()))
+    return out
+
+
+def norm_workspace(tokens, width, dtype=torch.bfloat16, device="cuda") -> torch.Tensor:
+    """The workspace of eqat_norm_bwd."""
+    n = lib().eqat_norm_workspace_bytes(_norm_ref(int(tokens), int(width), -1, BF16 if dtype == torch.bfloat16 else F32, F32, 0.0))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def eqat_norm_bwd(S, W, eps, dY, dS=None, want=("dX", "dW"), out=None, ws=None):
+    """Gradients of eqat_norm_fwd from S (what it left, or its X): dX (also that of R) in S's type, dW fp32 [width].  dS: the gradient that reaches S along the residual."""
+    T, n = S.shape
+    out = {} if out is None else out
+    if "dX" in want and "dX" not in out: out["dX"] = torch.empty_like(S)
+    if "dW" in want and "dW" not in out: out["dW"] = torch.empty(n, dtype=torch.float32, device=S.device)
+    if ws is None and "dW" in want:
+        ws = norm_workspace(T, n, S.dtype, S.device)
+    get = lambda name: out.get(name) if name in want else None
+    d = _norm_ref(T, n, -1, _dt(S), _dt(S) if W is None else _dt(W), float(eps))
+    _check("eqat_norm_bwd", lib().eqat_norm_bwd(
+        d, _p(S), _like("W", W, (n,), W.dtype) if W is not None else None, _like("dY", dY, S.shape, S.dtype), _like("dS", dS, S.shape, S.dtype),
+        _like("dX", get("dX"), S.shape, S.dtype), _like("dW", get("dW"), (n,), torch.float32), _p(ws), 0 if ws is None else ws.numel(), _stream()))
+    return out
+
+
+def rotary_frequencies(part, base=10000.0, stretch=1.0, short=256.0, long=2048.0):
+    """fp32 frequencies base^(-2 i / part) of `part` / 2 pairs (on the host).  stretch > 1, for contexts that many times longer: wave lengths of `long` tokens and more are stretched by it,
+    those below `short` tokens are kept, between the two in proportion to their logarithm."""
+    i = torch.arange(int(part) // 2, dtype=torch.float64)
+    f = float(base) ** (-2.0 * i / int(part))
+    if stretch > 1.0:
+        slow = ((2.0 * torch.pi / f / short).log() / torch.tensor(long / short, dtype=torch.float64).log()).clamp(0.0, 1.0)
+        f = f * (1.0 - slow) + f / stretch * slow
+    return f.float()
+
+
+class Rotary:
+    """How positions turn queries and keys: fp32 device frequencies of the pairs of a head's first 2 * len(frequencies) elements, (i, i + that half), or neighbours where
+    `interleaved`; `amplitude` times.  Build once, call often."""
+
+    def __init__(self, frequencies, head_dim, interleaved=False, amplitude=1.0):
+        if frequencies.dtype != torch.float32 or frequencies.dim() != 1:
+            raise TypeError("frequencies are fp32 [pairs]")
+        self.frequencies, self.head_dim = frequencies, _i32("head_dim", head_dim)          # the tensor must outlive the pointer
+        at, part = _p(frequencies), 2 * frequencies.numel()
+        self.descs = {dt: RotaryDesc(at, self.head_dim, part, 1 if interleaved else 0, code, float(amplitude)) for dt, code in ((torch.float32, F32), (torch.bfloat16, BF16))}
+        self.refs = {dt: ctypes.byref(d) for dt, d in self.descs.items()}
+
+
+def _turned(rot, t, out, tokens, dtype):
+    """(pointer, strides, heads, pointer, strides) of what is turned and of where it goes"""
+    if t is None:
+        if out is not None:
+            raise ValueError("an output without its input")
+        return None, None, 0, None, None
+    for x in (t, out):
+        if x.dtype != dtype or not x.is_cuda:
+            raise ValueError(f"expected a {dtype} device tensor, got {x.dtype} on {x.device}")
+        if x.dim() != 3:
+            raise ValueError("expected [tokens, heads, head_dim]")
+    heads = t.shape[1]
+    return (t.data_ptr(), _kv_strides(t.shape, t.stride(), tokens, heads, rot.head_dim)[0], heads, out.data_ptr(),
+            _kv_strides(out.shape, out.stride(), tokens, heads, rot.head_dim)[0])
+
+
+def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, inverse=False):
+    """(q, k) [tokens, heads, head_dim] (any token and head strides) turned by their tokens' positions (int32 [tokens]); into q_out, k_out (which may be q and k themselves)."""
+    if positions.dtype != torch.int32 or positions.dim() != 1:
+        raise TypeError("positions are int32 [tokens]")
+    T, like = positions.numel(), q if q is not None else k
+    if like is None:
+        return None, None
+    if q is not None and q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None: k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    if like.dtype not in rot.refs:
+        raise TypeError(f"unsupported dtype {like.dtype}")
+    _check("eqat_rotary", lib().eqat_rotary(rot.refs[like.dtype], T, _p(positions), *_turned(rot, q, q_out, T, like.dtype), *_turned(rot, k, k_out, T, like.dtype),
+                                            1 if inverse else 0, _stream()))
+    return q_out, k_out
+
+
+def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q_out=None):
+    """The newest tokens' queries turned (returned, into q_out if given, which may be q itself), their keys turned and values into the cache: eqat_rotary and eqat_kv_write in one launch."""
+    if rot.head_dim != cache.head_dim:
+        raise ValueError(f"heads of {rot.head_dim} in a cache of heads of {cache.head_dim}")
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    qp, qs, heads, op, os_ = _turned(rot, q, q_out, batch.tokens, cache.dtype)
+    (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
+    _check("eqat_kv_rotary_write", lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[cache.dtype], qp, qs, heads, op, os_, kp, ks[0], vp, vs[0], _p(cache.pool), _stream()))
+    return q_out
+
+
+def eqat_gate_fwd(Y, kind=GATE_SILU, H=None):
+    """H [tokens, F] = act(G) U of Y = [G | U] [tokens, 2 F]."""
+    T, F = Y.shape[0], Y.shape[1] // 2
+    H = torch.empty((T, F), dtype=Y.dtype, device=Y.device) if H is None else H
+    _check("eqat_gate_fwd", lib().eqat_gate_fwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype), _like("H", H, (T, F), Y.dtype), _stream()))
+    return H
+
+
+def eqat_gate_bwd(Y, dH, kind=GATE_SILU, want=("dY",), out=None):
+    """The gradient dY of Y = [G | U] from that of H, and H itself where it is wanted."""
+    T, F = Y.shape[0], Y.shape[1] // 2
+    out = {} if out is None else out
+    if "dY" in want and "dY" not in out: out["dY"] = torch.empty_like(Y)
+    if "H" in want and "H" not in out: out["H"] = torch.empty((T, F), dtype=Y.dtype, device=Y.device)
+    get = lambda name: out.get(name) if name in want else None
+    _check("eqat_gate_bwd", lib().eqat_gate_bwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype), _like("dH", dH, (T, F), Y.dtype), _like("dY", get("dY"), Y.shape, Y.dtype),
+                                                _like("H", get("H"), (T, F), Y.dtype), _stream()))
+    return out
+
+
+def gated_workspace(tokens, in_features, F, bits, group, dtype=torch.bfloat16, prepared=False, device="cuda") -> torch.Tensor:
+    """The workspace of eqat_gated_fwd and eqat_gated_bwd (or their calls on a prepared layer); that of more tokens serves fewer."""
+    d = _desc_ref(int(tokens), int(in_features), 2 * int(F), int(bits), int(group), BF16 if dtype == torch.bfloat16 else F32, BF16)
+    n = lib().eqat_gated_workspace_bytes(d, 1 if prepared else 0)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def _gated(name, X, F, bits, group, layer, kind, dH, want, out, ws, prepared):
+    T, I = X.shape
+    d = _desc_ref(T, I, 2 * F, int(bits), int(group), _dt(X), BF16)
+    if "H" in want and "H" not in out: out["H"] = torch.empty((T, F), dtype=X.dtype, device=X.device)
+    if "dY" in want and "dY" not in out: out["dY"] = torch.empty((T, 2 * F), dtype=X.dtype, device=X.device)
+    ws = gated_workspace(T, I, F, bits, group, X.dtype, prepared, X.device) if ws is None else ws
+    H = _like("H", out["H"] if "H" in want else None, (T, F), X.dtype)
+    back = () if dH is None else (_like("dH", dH, (T, F), X.dtype), _like("dY", out["dY"] if "dY" in want else None, (T, 2 * F), X.dtype))
+    _check(name, getattr(lib(), name)(d, int(kind), _p(X), *layer, *back, H, _p(ws), ws.numel(), _stream()))
+    return out
+
+
+def eqat_gated_fwd(X, Wpacked, s, zpacked, bits, group, kind=GATE_SILU, H=None, ws=None):
+    """H [tokens, F] = act(X Wg^T) * (X Wu^T) from the packed layer of the stacked projections [Wg; Wu] (2 F rows)."""
+    return _gated("eqat_gated_fwd", X, Wpacked.shape[0] // 2, bits, group, (_p(Wpacked), _p(s), _p(zpacked)), kind, None, ("H",), {} if H is None else {"H": H}, ws, False)["H"]
+
+
+def eqat_gated_bwd(X, Wpacked, s, zpacked, dH, bits, group, kind=GATE_SILU, want=("dY", "H"), out=None, ws=None):
+    """The gradient dY [tokens, 2 F] of the stacked projections' outputs from that of H, and H again; both projections are made anew from X."""
+    return _gated("eqat_gated_bwd", X, Wpacked.shape[0] // 2, bits, group, (_p(Wpacked), _p(s), _p(zpacked)), kind, dH, want, {} if out is None else out, ws, False)
+
+
+def eqat_gated_fwd_prepared(X, prepared, s, F, bits, group, kind=GATE_SILU, H=None, ws=None):
+    """eqat_gated_fwd on a layer prepared by eqat_qlinear_prepare."""
+    return _gated("eqat_gated_fwd_prepared", X, int(F), bits, group, (_p(prepared), _p(s)), kind, None, ("H",), {} if H is None else {"H": H}, ws, True)["H"]
+
+
+def eqat_gated_bwd_prepared(X, prepared, s, dH, bits, group, kind=GATE_SILU, want=("dY", "H"), out=None, ws=None):
+    """eqat_gated_bwd on a layer prepared by eqat_qlinear_prepare."""
+    return _gated("eqat_gated_bwd_prepared", X, dH.shape[1], bits, group, (_p(prepared), _p(s)), kind, dH, want, {} if out is None else out, ws, True)
 
 
 def eqat_profile_start():

@@ -194,7 +194,7 @@ const char *eqat_status_string(int status)
     case EQAT_ERR_ALIGN: return "pointer not 16-byte aligned (workspace: 256-byte)";
     case EQAT_ERR_WORKSPACE: return "workspace missing or too small";
     case EQAT_ERR_DEVICE: return "HIP launch failed";
-    case EQAT_ERR_HYPER: return "constants out of range (optimizer: 0 <= beta < 1, eps >= 0, step >= 1; attention: 0 <= scale <= 2^100, window >= 0)";
+    case EQAT_ERR_HYPER: return "constants out of range (optimizer: 0 <= beta < 1, eps >= 0, step >= 1; attention: 0 <= scale <= 2^100, window >= 0; norm: eps >= 0, finite; rotary: amplitude finite; gate: known kind)";
     default: return "unknown status";
     }
 }
@@ -207,7 +207,7 @@ const char *eqat_profile_kernel_name(int k)
 {
     static const char *names[] = {"init_minmax", "quantize", "e2e_prepare", "gemm_fwd", "gemm_dx",
                                                 "gemm_dw", "gemm_bwd", "reduce_partials", "f32_path", "gemv", "recon_loss", "adamw_update",
-                                                "kv_write", "kv_read", "kv_attend"};
+                                                "kv_write", "kv_read", "kv_attend", "norm", "rotary", "gate"};
     static_assert(sizeof(names) / sizeof(names[0]) == eqat::PK_COUNT, "one name per kernel class");
     return (k >= 0 && k < eqat::PK_COUNT) ? names[k] : "?";
 }
@@ -608,6 +608,104 @@ eqat_status eqat_qlinear_bwd_prepared_kept(const eqat_desc *d, const void *X, co
                                            const void *dY, void *dX, float *ds, float *dz, void *ws, size_t ws_bytes, void *stream)
 {
     return bwd_prepared_any(d, X, prepared, s, z, dY, dX, ds, dz, ws, ws_bytes, stream, true);
+}
+
+// ---- gated feed-forward (d: the stacked projection, out_features = 2 F) ----------------------------------------------
+// codes in the working layout and (s, z) pairs; with fp32 activations the projections instead of the codes
+struct GatedWs { size_t y, codes, sz, total; };
+// which kernel: matrix-vector (forward, packed), the one for few output tiles, the tiles
+enum GatedKernel { GATED_GEMV, GATED_MID, GATED_TILES };
+static GatedKernel gated_kernel(const Problem &p, bool prepared, bool backward)
+{
+    if (!prepared && !backward && eqat::gemv_gated_applies(p)) return GATED_GEMV;
+    if (!eqat::group_by_magic(p)) return GATED_TILES;
+    return p.T <= 64 || eqat::mid_applies(p) ? GATED_MID : GATED_TILES;
+}
+static GatedWs gated_ws(const Problem &p, bool prepared)
+{
+    GatedWs l{};
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off += align256(bytes); return at; };
+    if (!p.act_bf16) l.y = take((size_t)p.T * p.O * 4);
+    else if (p.T <= 64 && eqat::group_by_magic(p)) return l;          // no kernel for so few tokens has anything in it
+    else if (!prepared) l.codes = take(eqat::work_code_bytes(p));
+    l.sz = take((size_t)p.O * p.G * 8);
+    l.total = off;
+    return l;
+}
+static eqat_status gated_any(const eqat_desc *d, int kind, const void *X, const void *layer, const float *s, const uint8_t *zpacked, bool prepared, const void *dH, void *dY, void *H,
+                             bool backward, void *ws, size_t ws_bytes, void *stream)
+{
+    Problem p;
+    if (d == nullptr) return EQAT_ERR_NULL;
+    eqat_desc as_packed = *d;
+    as_packed.w_dtype = EQAT_BF16;                    // not looked at
+    if (eqat_status e = check_desc(&as_packed, true, &p)) return e;
+    if (p.O % 16 != 0) return EQAT_ERR_SHAPE;
+    if (kind != EQAT_GATE_SILU && kind != EQAT_GATE_GELU) return EQAT_ERR_HYPER;
+    EQAT_REQUIRE(layer); EQAT_REQUIRE(s);
+    if (!prepared) EQAT_REQUIRE(zpacked);
+    const bool wanted = backward ? dY != nullptr || H != nullptr : true;
+    if (p.T > 0 && wanted) { EQAT_REQUIRE(X); if (backward) EQAT_REQUIRE(dH); else EQAT_REQUIRE(H); }
+    EQAT_ALIGNED(X); EQAT_ALIGNED(s); EQAT_ALIGNED(zpacked); EQAT_ALIGNED(dH); EQAT_ALIGNED(dY); EQAT_ALIGNED(H);
+    if (!aligned(layer, prepared ? 256 : 16)) return EQAT_ERR_ALIGN;
+    const GatedWs l = gated_ws(p, prepared);
+    if (l.total > 0 && (ws == nullptr || ws_bytes < l.total)) return EQAT_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return EQAT_ERR_ALIGN;
+    if (p.T == 0 || !wanted) return EQAT_OK;
+    hipStream_t st = (hipStream_t)stream;
+    char *w8 = (char *)ws;
+    const PreparedLayout pl = prepared ? prepared_layout(p) : PreparedLayout{};
+    const char *p8 = (const char *)layer;
+    const float *zb = prepared ? (const float *)(p8 + pl.zb) : nullptr;
+    const eqat::GatedOut out{H, dH, dY, kind};
+    if (!p.act_bf16) {
+        qlinear_prepare_into(p, nullptr, s, zpacked, zb, nullptr, w8 + l.sz, nullptr, 0, st);
+        { ProfScope ps(eqat::PK_F32, st); eqat::launch_f32_fwd(p, true, X, prepared ? p8 + pl.codes : p8, s, w8 + l.sz, w8 + l.y, st); }
+        return backward ? eqat_gate_bwd(p.T, p.O / 2, EQAT_F32, kind, w8 + l.y, dH, dY, H, stream) : eqat_gate_fwd(p.T, p.O / 2, EQAT_F32, kind, w8 + l.y, H, stream);
+    }
+    switch (gated_kernel(p, prepared, backward)) {
+    case GATED_GEMV: { ProfScope ps(eqat::PK_GEMV, st); eqat::launch_gemv_gated(p, kind, X, layer, s, zpacked, H, st); break; }
+    case GATED_MID: { ProfScope ps(eqat::PK_GEMM_FWD, st); eqat::launch_mid_gated(p, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); break; }
+    default: {
+        qlinear_prepare_into(p, prepared ? nullptr : (const uint8_t *)layer, s, zpacked, zb, prepared ? nullptr : w8 + l.codes, w8 + l.sz, nullptr, 0, st);
+        ProfScope ps(eqat::PK_GEMM_FWD, st);
+        eqat::launch_tiles_gated(p, out, X, prepared ? (const void *)(p8 + pl.codes) : (const void *)(w8 + l.codes), w8 + l.sz, st);
+    }
+    }
+    return launch_status();
+}
+
+size_t eqat_gated_workspace_bytes(const eqat_desc *d, int prepared)
+{
+    Problem p;
+    if (d == nullptr) return 0;
+    eqat_desc as_packed = *d;
+    as_packed.w_dtype = EQAT_BF16;
+    if (check_desc(&as_packed, true, &p) != EQAT_OK || p.O % 16 != 0) return 0;
+    return std::max<size_t>(gated_ws(p, prepared != 0).total, 256);
+}
+
+eqat_status eqat_gated_fwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, void *H, void *ws, size_t ws_bytes, void *stream)
+{
+    return gated_any(d, kind, X, Wpacked, s, zpacked, false, nullptr, nullptr, H, false, ws, ws_bytes, stream);
+}
+
+eqat_status eqat_gated_bwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, const void *dH, void *dY, void *H,
+                           void *ws, size_t ws_bytes, void *stream)
+{
+    return gated_any(d, kind, X, Wpacked, s, zpacked, false, dH, dY, H, true, ws, ws_bytes, stream);
+}
+
+eqat_status eqat_gated_fwd_prepared(const eqat_desc *d, int kind, const void *X, const void *prepared, const float *s, void *H, void *ws, size_t ws_bytes, void *stream)
+{
+    return gated_any(d, kind, X, prepared, s, nullptr, true, nullptr, nullptr, H, false, ws, ws_bytes, stream);
+}
+
+eqat_status eqat_gated_bwd_prepared(const eqat_desc *d, int kind, const void *X, const void *prepared, const float *s, const void *dH, void *dY, void *H,
+                                    void *ws, size_t ws_bytes, void *stream)
+{
+    return gated_any(d, kind, X, prepared, s, nullptr, true, dH, dY, H, true, ws, ws_bytes, stream);
 }
 
 // Test aid (host only): how a fwd / dX / dW launch divides its work.

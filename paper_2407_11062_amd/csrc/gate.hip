@@ -1,0 +1,73 @@
+// The gate of the feed-forward, element by element, for projections of any kind: H = act(G) U and its backward pass, [G | U] the rows of the stacked projection.
+//
+// Bound by bytes (the activation is some twenty instructions an element): eight neighbouring elements of both halves to a lane.
+#include "layer.h"
+
+#include <algorithm>
+
+namespace eqat {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct GateArgs {
+    const void *y, *dh;
+    void *h, *dy;
+    int64_t vecs;                       // of eight elements of H
+    int per_row;
+};
+
+template <typename T, int KIND, bool BACK> __global__ __launch_bounds__(kThreads) void k_gate(const GateArgs a)
+{
+    const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (v >= a.vecs) return;
+    const int64_t row = v / a.per_row, inter = (int64_t)a.per_row * 8, at = (v - row * a.per_row) * 8, of_g = row * 2 * inter + at, of_h = row * inter + at;
+    Eight<T> g, u, d;
+    g.load(static_cast<const T *>(a.y) + of_g);
+    u.load(static_cast<const T *>(a.y) + of_g + inter);
+    float h[8];
+    if constexpr (BACK) {
+        d.load(static_cast<const T *>(a.dh) + of_h);
+        float dg[8], du[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float act, slope;
+            gate_both<KIND>(g.get(e), act, slope);
+            h[e] = act * u.get(e);
+            dg[e] = d.get(e) * u.get(e) * slope;
+            du[e] = d.get(e) * act;
+        }
+        if (a.dy != nullptr) {
+            Eight<T> o;
+            o.set(dg);
+            o.store(static_cast<T *>(a.dy) + of_g);
+            o.set(du);
+            o.store(static_cast<T *>(a.dy) + of_g + inter);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = gate_act<KIND>(g.get(e)) * u.get(e);
+    }
+    if (a.h != nullptr) {
+        Eight<T> o;
+        o.set(h);
+        o.store(static_cast<T *>(a.h) + of_h);
+    }
+}
+
+}  // namespace
+
+void launch_gate(const GateCall &c, hipStream_t st)
+{
+    GateArgs a{};
+    a.y = c.y; a.dh = c.dh; a.h = c.h; a.dy = c.dy; a.per_row = c.inter / 8; a.vecs = c.tokens * a.per_row;
+    const unsigned blocks = (unsigned)((a.vecs + kThreads - 1) / kThreads);
+    const bool back = c.dh != nullptr, silu = c.kind == EQAT_GATE_SILU;
+#define EQAT_GATE(T) do { \
+        if (!back) { if (silu) k_gate<T, EQAT_GATE_SILU, false><<<blocks, kThreads, 0, st>>>(a); else k_gate<T, EQAT_GATE_GELU, false><<<blocks, kThreads, 0, st>>>(a); } \
+        else { if (silu) k_gate<T, EQAT_GATE_SILU, true><<<blocks, kThreads, 0, st>>>(a); else k_gate<T, EQAT_GATE_GELU, true><<<blocks, kThreads, 0, st>>>(a); } } while (0)
+    if (c.act_bf16) EQAT_GATE(bf16_t); else EQAT_GATE(float);
+#undef EQAT_GATE
+}
+
+}  // namespace eqat

@@ -8,7 +8,13 @@
 // 8192 tokens of 32 heads of 128, one group, bf16: a write takes 40 us for its 170 MB (4.2 TB/s), bound by arithmetic (18 instructions an element, 33 us of a SIMD's
 // issue), a read 28 us (6.1 TB/s; a large copy 4.8).  A token of 32 heads: 4.3 and 3.6 us, the launch.  Half words in banks of their own, stored by LDS instructions
 // rather than by flat ones: 42 and 29.
-#include "kv.h"
+//
+// eqat_kv_rotary_write is the same launch with the keys turned on their way in (rounded to the activations' type, as eqat_rotary leaves them, so that what is written is
+// bitwise what the two calls write) and workgroups beside it that turn the queries.  A workgroup makes the cosines and sines of its record's tokens in LDS first.
+#include "layer.h"
+#include "turn.h"
+
+#include <algorithm>
 
 namespace eqat {
 namespace {
@@ -159,15 +165,143 @@ template <int NS, typename T> __device__ __forceinline__ void load_token(const K
     }
 }
 
-template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves * 64) void k_kv_write(const CacheArgs a)
+// f(IC<0>{}) ... f(IC<N - 1>{})
+template <int N, int I = 0, typename F> __device__ __forceinline__ void static_for_heads(F &&f)
+{
+    if constexpr (I < N) { f(IC<I>{}); static_for_heads<N, I + 1>(f); }
+}
+
+// What the turned write has beside it.  blockIdx.y from kv_blocks on: queries, `block_heads` heads each.
+struct TurnArgs {
+    const float *freq;
+    KvRows q, q_out;
+    float amplitude;
+    int half, part, interleaved, q_heads, block_heads, kv_blocks;
+};
+__device__ __forceinline__ void turn(float &x, float &y, floatx2 cs)
+{
+    const float u = __builtin_fmaf(x, cs[0], -(y * cs[1]));
+    y = __builtin_fmaf(y, cs[0], x * cs[1]);
+    x = u;
+}
+
+// A token's key, lane c of its four: elements 32 j + 8 c ..; `turns` of its token; `from` its first element in memory, which nothing writes.  All lanes come here, with a token's
+// turns and memory where theirs is none: nothing but scalar branches, so that no register is parked while lanes are off.
+template <int NS, typename T> __device__ __forceinline__ void turn_key(const TurnArgs &r, const floatx2 *turns, const T *from, int c, float (&x)[NS][8])
+{
+    if (r.interleaved) {
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const int p = 16 * j + 4 * c + e / 2;
+                const floatx2 cs = turns[min(p, r.half - 1)];
+                float u = x[j][e], v = x[j][e + 1];
+                turn(u, v, cs);
+                x[j][e] = p < r.half ? u : x[j][e];
+                x[j][e + 1] = p < r.half ? v : x[j][e + 1];
+            }
+    } else if (r.half % 32 == 0) {                            // the partner is the lane's own
+        const int apart = r.half / 32;
+        static_for_heads<NS / 2>([&](auto h) {
+            constexpr int H = decltype(h)::value + 1;
+            if (apart != H) return;
+#pragma unroll
+            for (int j = 0; j < H; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) turn(x[j][e], x[j + H][e], turns[32 * j + 8 * c + e]);
+        });
+    } else {                                                  // it is another lane's: from memory
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = 32 * j + 8 * c + e, p = i < r.half ? i : min(i - r.half, r.half - 1);
+                const floatx2 cs = turns[p];
+                const float other = to_float(from[i < r.half ? i + r.half : p]);
+                float u = i < r.half ? x[j][e] : other, v = i < r.half ? other : x[j][e];
+                turn(u, v, cs);
+                x[j][e] = i < r.half ? u : i < r.part ? v : x[j][e];
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[j][e] = to_float((T)x[j][e]);
+}
+
+// The queries of a record's rows, heads head0 ..: a unit of work is eight neighbouring elements, or two times eight that are partners; pairs and single elements where eight do
+// not divide half of what is turned.  Both of a pair are read before either is written.
+template <int NS, typename T> __device__ __forceinline__ void turn_queries(const TurnArgs &r, const floatx2 *turns, const Place &at, int head0)
+{
+    constexpr int D = 32 * NS, kThreads = kCacheWaves * 64;
+    const int heads = min(r.block_heads, r.q_heads - head0), tokens = at.to - at.from;
+    const bool by_eight = r.interleaved || r.half % 8 == 0;
+    const int turned = r.interleaved ? D / 8 : by_eight ? r.half / 8 : r.half, units = r.interleaved ? D / 8 : by_eight ? (D - r.half) / 8 : D - r.half;
+    for (int u = threadIdx.x; u < tokens * heads * units; u += kThreads) {
+        const int th = quotient(u, units), p = u - th * units, t = quotient(th, heads), h = head0 + (th - t * heads);
+        const int64_t row = at.row + t;
+        const T *from = static_cast<const T *>(r.q.p) + row * r.q.token_stride + h * r.q.head_stride;
+        T *to = static_cast<T *>(r.q_out.p) + row * r.q_out.token_stride + h * r.q_out.head_stride;
+        const floatx2 *cs = turns + t * r.half;
+        if (!by_eight) {
+            if (p < turned) {
+                float x = to_float(from[p]), y = to_float(from[p + r.half]);
+                turn(x, y, cs[p]);
+                to[p] = (T)x; to[p + r.half] = (T)y;
+            } else {
+                to[p + r.half] = from[p + r.half];
+            }
+            continue;
+        }
+        float x[8], y[8];
+        if (r.interleaved) {
+            load8(from + 8 * p, x);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) if (8 * p + e < r.part) turn(x[e], x[e + 1], cs[4 * p + e / 2]);
+            store8(to + 8 * p, x);
+        } else if (p < turned) {
+            load8(from + 8 * p, x);
+            load8(from + 8 * p + r.half, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) turn(x[e], y[e], cs[8 * p + e]);
+            store8(to + 8 * p, x);
+            store8(to + 8 * p + r.half, y);
+        } else {
+            load8(from + 8 * p + r.half, x);
+            store8(to + 8 * p + r.half, x);
+        }
+    }
+}
+
+template <int NS, int SG, typename T, bool TURN> __device__ __forceinline__ void kv_write_body(const CacheArgs &a, const TurnArgs &turned)
 {
     using R = KvRecord<NS, SG>;
+    extern __shared__ __attribute__((aligned(16))) floatx2 turns[];           // [tokens of the record][half]
+    Place all{};
+    if constexpr (TURN) {
+        all = place_of(a, blockIdx.x, 0, R::kBytes);
+        if (!all.any) return;                                 // (the same in all waves)
+        for (int e = threadIdx.x; e < (all.to - all.from) * turned.half; e += kCacheWaves * 64) {
+            const int t = quotient(e, turned.half);
+            float cs, sn;
+            cos_sin(all.from + t, turned.freq[e - t * turned.half], cs, sn);
+            turns[e] = floatx2{cs * turned.amplitude, sn * turned.amplitude};
+        }
+        __syncthreads();
+        if ((int)blockIdx.y >= turned.kv_blocks) {
+            turn_queries<NS, T>(turned, turns, all, ((int)blockIdx.y - turned.kv_blocks) * turned.block_heads);
+            return;
+        }
+    }
     __shared__ __attribute__((aligned(16))) uint8_t lds[kCacheWaves / 2][16 * R::D];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, t = lane >> 2, c = lane & 3;
     const int head = blockIdx.y * (kCacheWaves / 2) + (wave >> 1);
     const bool values = (wave & 1) != 0;                      // this wave's part of the record
     if (head >= a.heads) return;
-    Place at = place_of(a, blockIdx.x, head, R::kBytes);
+    Place at = all;
+    if constexpr (TURN) at.record += (int64_t)head * a.page_records * R::kBytes;
+    else at = place_of(a, blockIdx.x, head, R::kBytes);
     if (!at.any || !at.there) return;
     at.to = min(at.to, at.held);
     const bool full = at.to - at.from == kKvRecord;
@@ -179,6 +313,12 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
         if (!__any(is)) continue;
         float x[NS][8];
         load_token<NS, T>(rows, at, pos, head, c, x);
+        if constexpr (TURN) {
+            if (!values) {
+                const int row = is ? pos - at.from : 0;
+                turn_key<NS, T>(turned, turns + row * turned.half, static_cast<const T *>(rows.p) + (int64_t)(at.row + row) * rows.token_stride + head * rows.head_stride, c, x);
+            }
+        }
         Step steps[R::G];
 #pragma unroll
         for (int g = 0; g < R::G; ++g) {
@@ -222,6 +362,9 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
             *reinterpret_cast<uintx4 *>(at.record + R::kValues + n * 1024 + lane * 16) = *reinterpret_cast<const uintx4 *>(lds[wave >> 1] + n * 1024 + lane * 16);
     }
 }
+
+template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves * 64) void k_kv_write(const CacheArgs a) { kv_write_body<NS, SG, T, false>(a, TurnArgs{}); }
+template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves * 64) void k_kv_rotary_write(const CacheArgs a, const TurnArgs r) { kv_write_body<NS, SG, T, true>(a, r); }
 
 __device__ __forceinline__ float stands_for(uint32_t code, uint32_t step)
 {
@@ -295,10 +438,17 @@ template <int NS, int SG, typename T> __global__ __launch_bounds__(kCacheWaves *
     }
 }
 
-template <int NS, int SG> void launch(const KvShape &s, const CacheArgs &a, int records, bool write, hipStream_t st)
+template <int NS, int SG> void launch(const KvShape &s, const CacheArgs &a, int records, bool write, const TurnArgs *turned, hipStream_t st)
 {
-    const dim3 grid((unsigned)records, (unsigned)(s.heads + kCacheWaves / 2 - 1) / (kCacheWaves / 2));
-    if (write) {
+    dim3 grid((unsigned)records, (unsigned)(s.heads + kCacheWaves / 2 - 1) / (kCacheWaves / 2));
+    if (turned != nullptr) {
+        TurnArgs r = *turned;
+        r.kv_blocks = (int)grid.y;
+        grid.y += (unsigned)((r.q_heads + r.block_heads - 1) / r.block_heads);
+        const size_t lds = (size_t)std::min(a.b.max_new, kKvRecord) * r.half * sizeof(floatx2);
+        if (s.act_bf16) k_kv_rotary_write<NS, SG, bf16_t><<<grid, kCacheWaves * 64, lds, st>>>(a, r);
+        else k_kv_rotary_write<NS, SG, float><<<grid, kCacheWaves * 64, lds, st>>>(a, r);
+    } else if (write) {
         if (s.act_bf16) k_kv_write<NS, SG, bf16_t><<<grid, kCacheWaves * 64, 0, st>>>(a);
         else k_kv_write<NS, SG, float><<<grid, kCacheWaves * 64, 0, st>>>(a);
     } else {
@@ -307,7 +457,7 @@ template <int NS, int SG> void launch(const KvShape &s, const CacheArgs &a, int 
     }
 }
 
-void launch_any(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, void *pool, bool write, hipStream_t st)
+void launch_any(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, void *pool, bool write, const TurnArgs *turned, hipStream_t st)
 {
     const CacheArgs a{b, k, v, static_cast<uint8_t *>(pool), s.pages, s.heads, s.page_records};
     // n newest tokens touch at most (n + 30) / 32 + 1 records
@@ -315,22 +465,34 @@ void launch_any(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRow
     const int records = (int)(each < all ? each : all);
     const int sg = s.group / 32;
     switch (s.head_dim) {
-    case 64: if (sg == 1) launch<2, 1>(s, a, records, write, st); else launch<2, 2>(s, a, records, write, st); break;
+    case 64: if (sg == 1) launch<2, 1>(s, a, records, write, turned, st); else launch<2, 2>(s, a, records, write, turned, st); break;
     case 128:
-        if (sg == 1) launch<4, 1>(s, a, records, write, st); else if (sg == 2) launch<4, 2>(s, a, records, write, st); else launch<4, 4>(s, a, records, write, st);
+        if (sg == 1) launch<4, 1>(s, a, records, write, turned, st); else if (sg == 2) launch<4, 2>(s, a, records, write, turned, st); else launch<4, 4>(s, a, records, write, turned, st);
         break;
     default:
-        if (sg == 1) launch<8, 1>(s, a, records, write, st); else if (sg == 2) launch<8, 2>(s, a, records, write, st);
-        else if (sg == 4) launch<8, 4>(s, a, records, write, st); else launch<8, 8>(s, a, records, write, st);
+        if (sg == 1) launch<8, 1>(s, a, records, write, turned, st); else if (sg == 2) launch<8, 2>(s, a, records, write, turned, st);
+        else if (sg == 4) launch<8, 4>(s, a, records, write, turned, st); else launch<8, 8>(s, a, records, write, turned, st);
     }
 }
 
 }  // namespace
 
-void launch_kv_write(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, void *pool, hipStream_t st) { launch_any(s, b, k, v, pool, true, st); }
+void launch_kv_write(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, void *pool, hipStream_t st) { launch_any(s, b, k, v, pool, true, nullptr, st); }
 void launch_kv_read(const KvShape &s, const KvBatch &b, const KvRows &k, const KvRows &v, const void *pool, hipStream_t st)
 {
-    launch_any(s, b, k, v, const_cast<void *>(pool), false, st);
+    launch_any(s, b, k, v, const_cast<void *>(pool), false, nullptr, st);
+}
+
+void launch_kv_rotary_write(const KvShape &s, const KvBatch &b, const Rotary &turned, const KvRows &q, const KvRows &q_out, int q_heads, const KvRows &k, const KvRows &v, void *pool,
+                            hipStream_t st)
+{
+    TurnArgs r{};
+    r.freq = turned.freq; r.q = q; r.q_out = q_out; r.amplitude = turned.amplitude; r.half = turned.part / 2; r.part = turned.part; r.interleaved = turned.interleaved;
+    r.q_heads = q_heads;
+    // A record's tokens of 16 heads, so that a prompt's cosines and sines are a fraction of the work; where a sequence has a token or a few, all the heads that 256 lanes turn at once
+    r.block_heads = std::max(16, 512 / (std::max(1, std::min(b.max_new, kKvRecord)) * s.head_dim / 8));
+    r.block_heads = std::max(r.block_heads, (q_heads + 16383) / 16384);
+    launch_any(s, b, k, v, pool, true, &r, st);
 }
 
 }  // namespace eqat

@@ -2,6 +2,7 @@
 // (a quarter of every K step each), computes 128 weight rows for a tile of tokens.
 #pragma once
 #include "common.h"
+#include "gate.h"
 
 #include <hip/hip_runtime.h>
 
@@ -17,6 +18,7 @@ struct MidArgs {
     uint32_t x_bytes, codes_bytes, s_bytes, z_bytes;
     int tiles_m, tiles_n, band;    // band: token tiles that an XCD walks together, 0: all of them
     float *pairs;                        // the launch of a prepared layer leaves the (s, z) pairs here; NULL: does not
+    const bf16_t *dH; bf16_t *dY; int kind;      // of the gated feed-forward, whose H is Y: see store_gated_sums
 };
 
 constexpr int kMidBN = 128, kMidKG = 4, kMidNT = 512;
@@ -90,6 +92,76 @@ __device__ __forceinline__ void store_sums(const MidArgs &a, const floatx16 (&ac
                 *reinterpret_cast<bf16x4 *>(a.Y + (size_t)(m0 + tok) * a.O + o) = y;
             }
         }
+    }
+}
+
+// Row `row` of the 128 of a workgroup's tile in the weight matrix.  GATED (O = 2 F, the gate's rows first): blocks of 32 rows of the gate and the same 32 of the other half take turns, so
+// that the two row blocks of a wave are a gate's rows and their partners.  Beyond F the rows are others', or none: nothing of them is stored.
+template <bool GATED> __device__ __forceinline__ int mid_row(const MidArgs &a, int n0, int row)
+{
+    if constexpr (!GATED) return n0 + row;
+    else return (n0 >> 1) + ((row >> 6) << 5) + (row & 31) + (row & 32 ? a.O >> 1 : 0);
+}
+// As store_sums, of a gated feed-forward: block 0 is G, block 1 U.  H = act(G) U, and where dH is given dY = [dH U act'(G) | dH act(G)]; H, or dY, may be NULL.
+template <int BM, uint32_t TOTAL>
+__device__ __forceinline__ void store_gated_sums(const MidArgs &a, const floatx16 (&acc)[2][BM / 32], unsigned char *smem_raw, int m0, int n0, int wave, int lane)
+{
+    const int wn = wave & 1, kg = wave >> 1, r = lane & 31, h = lane >> 5, F = a.O >> 1;
+    constexpr uint32_t WAVE_BYTES = BM * 32 * 4;
+    constexpr int NK = BM / 4 / 8;
+    floatx4 sum[2][NK];
+    bf16x4 dh[NK];
+    const int f = (n0 >> 1) + wn * 32 + (lane & 7) * 4;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {                     // under the sums' way through LDS
+        const int tok = kg * (BM / 4) + k * 8 + (lane >> 3);
+        if (a.dH != nullptr && m0 + tok < a.T && f < F) dh[k] = *reinterpret_cast<const bf16x4 *>(a.dH + (size_t)(m0 + tok) * F + f);
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < BM / 32; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                floatx4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[b][i][4 * q + e];
+                *reinterpret_cast<floatx4 *>(smem_raw + wave * WAVE_BYTES + (i * 32 + r) * 128 + (((2 * q + h) ^ (r & 7)) * 16)) = v;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            const int tok = kg * (BM / 4) + k * 8 + (lane >> 3), ch = lane & 7;
+            sum[b][k] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int g = 0; g < kMidKG; ++g) {
+                const floatx4 v = *reinterpret_cast<const floatx4 *>(smem_raw + (g * 2 + wn) * WAVE_BYTES + tok * 128 + ((ch ^ (tok & 7)) * 16));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[b][k][e] += v[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+        const int64_t m = m0 + kg * (BM / 4) + k * 8 + (lane >> 3);
+        if (m >= a.T || f >= F) continue;              // F is a multiple of 8
+        bf16x4 y, dg, du;
+        if (a.dH == nullptr) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (bf16_t)gated_by(a.kind, sum[0][k][e], sum[1][k][e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const Gated g = gated_both(a.kind, sum[0][k][e], sum[1][k][e], (float)dh[k][e]);
+                y[e] = (bf16_t)g.h; dg[e] = (bf16_t)g.dg; du[e] = (bf16_t)g.du;
+            }
+            if (a.dY != nullptr) {
+                *reinterpret_cast<bf16x4 *>(a.dY + m * a.O + f) = dg;
+                *reinterpret_cast<bf16x4 *>(a.dY + m * a.O + F + f) = du;
+            }
+        }
+        if (a.Y != nullptr) *reinterpret_cast<bf16x4 *>(a.Y + m * F + f) = y;
     }
 }
 

@@ -1,0 +1,340 @@
+// Root-mean-square norm with the residual's addition, and its backward pass.
+//
+//   S = round(X + R),  Y = w S rstd,  rstd = 1 / sqrt(mean S^2 + eps),  or Y in 8 bits: codes = e4m3(Y / scale), scale = max |Y| of a group / 448
+//   dX = dS + rstd (e - S rstd^2 mean(e S)),  e = w dY;     dw = sum over the rows of dY S rstd
+//
+// Bound by bytes: every row is read once and kept in registers, eight neighbouring elements to a lane, LANES lanes to a row: part of a wave, a wave, or a workgroup that
+// meets in LDS once (a row's maximum, for 8 bits with one scale a row, a second time).  Sums, means and products are binary32; S is what stands in memory, so that the
+// backward pass, which makes rstd from S again, is that of what the forward computed.
+#include "layer.h"
+
+#include <algorithm>
+
+namespace eqat {
+namespace {
+
+constexpr float kFp8Most = 448.0f, kLeastScale = 0x1p-126f;
+
+template <int LANES, typename F> __device__ __forceinline__ float lanes_all(float v, F f)
+{
+#pragma unroll
+    for (int d = (LANES < 64 ? LANES : 64) / 2; d >= 1; d >>= 1) v = f(v, __shfl_xor(v, d, 64));
+    return v;
+}
+// over the LANES lanes of a row, in every one of them; `part`: an LDS word a wave, of this call's own
+template <int LANES, typename F> __device__ __forceinline__ float row_all(float v, float *part, F f)
+{
+    v = lanes_all<LANES>(v, f);
+    if constexpr (LANES > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = part[0];
+#pragma unroll
+        for (int w = 1; w < LANES / 64; ++w) v = f(v, part[w]);
+    }
+    return v;
+}
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+__device__ __forceinline__ float most_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }        // NaN wins
+
+struct NormArgs {
+    int64_t rows;
+    const void *x, *r, *w, *dy;
+    void *s, *y, *codes;
+    float *scales, *part;
+    int width, group, w_bf16;
+    float eps, per_width;
+};
+
+__device__ __forceinline__ void load_w(const NormArgs &a, int at, float (&w)[8])
+{
+    if (a.w == nullptr) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = 1.0f;
+    } else if (a.w_bf16) {
+        Eight<bf16_t> v;
+        v.load(static_cast<const bf16_t *>(a.w) + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = v.get(e);
+    } else {
+        Eight<float> v;
+        v.load(static_cast<const float *>(a.w) + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = v.get(e);
+    }
+}
+
+template <typename T, int LANES, int NV, bool ONCE>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_fwd(const NormArgs a)
+{
+    constexpr int kThreads = LANES > 256 ? LANES : 256;
+    __shared__ float part[2][kThreads / 64];
+    const int lane = threadIdx.x % LANES;
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+    const bool there = row < a.rows;                          // (LANES >= 256: the whole workgroup)
+    const T *x = static_cast<const T *>(a.x) + row * a.width, *r = static_cast<const T *>(a.r) + row * a.width;
+    Eight<T> s[NV], add[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int at = (k * LANES + lane) * 8;
+        s[k].zero();
+        add[k].zero();
+        if (there && at < a.width) {
+            s[k].template load<ONCE>(x + at);
+            if (a.r != nullptr) add[k].template load<ONCE>(r + at);
+        }
+    }
+    float w[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) if ((k * LANES + lane) * 8 < a.width) load_w(a, (k * LANES + lane) * 8, w[k]);
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int at = (k * LANES + lane) * 8;
+        if (a.r != nullptr) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = s[k].get(e) + add[k].get(e);
+            s[k].set(v);
+        }
+        if (a.s != nullptr && there && at < a.width) s[k].store(static_cast<T *>(a.s) + row * a.width + at);
+        float t = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t = __builtin_fmaf(s[k].get(e), s[k].get(e), t);
+        sum += t;
+    }
+    sum = row_all<LANES>(sum, part[0], sum_of);
+    const float rstd = 1.0f / sqrtf(__builtin_fmaf(sum, a.per_width, a.eps));
+    float y[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[k][e] = s[k].get(e) * rstd * w[k][e];
+    if (a.y != nullptr) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * 8;
+            Eight<T> o;
+            o.set(y[k]);
+            if (there && at < a.width) o.store(static_cast<T *>(a.y) + row * a.width + at);
+        }
+    }
+    if (a.codes != nullptr) {
+        float most[NV], all = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            most[k] = 0.0f;
+            if ((k * LANES + lane) * 8 < a.width) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most[k] = most_of(most[k], fabsf(y[k][e]));
+            }
+            all = most_of(all, most[k]);
+        }
+        const int lanes = a.group / 8, groups = a.width / a.group;
+        if (a.group == a.width) {                             // a row
+            all = row_all<LANES>(all, part[1], most_of);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) most[k] = all;
+        } else {                                              // neighbouring lanes, 4 to 64 of them
+            for (int d = 1; d < lanes; d <<= 1) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) most[k] = most_of(most[k], __shfl_xor(most[k], d, 64));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * 8;
+            if (!there || at >= a.width) continue;
+            const float scale = most_of(most[k] / kFp8Most, kLeastScale), by = 1.0f / scale;
+            uintx2 code;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][4 * h] * by, y[k][4 * h + 1] * by, 0, false);
+                v = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][4 * h + 2] * by, y[k][4 * h + 3] * by, v, true);
+                code[h] = (uint32_t)v;
+            }
+            *reinterpret_cast<uintx2 *>(static_cast<uint8_t *>(a.codes) + row * a.width + at) = code;
+            if (at % a.group == 0) a.scales[row * groups + at / a.group] = scale;
+        }
+    }
+}
+
+// Workgroup b takes the rows b, b + grid, ... (of kThreads / LANES each) and keeps its part of dw in registers: part[b][width], summed over b by k_norm_dw.
+template <typename T, int LANES, int NV>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const NormArgs a)
+{
+    constexpr int kThreads = LANES > 256 ? LANES : 256, kRows = kThreads / LANES;
+    __shared__ float part[2][2][kThreads / 64];
+    extern __shared__ float sums[];                           // [width], where several rows are in the workgroup and dw is wanted
+    const int lane = threadIdx.x % LANES;
+    float w[NV][8], dw[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int at = (k * LANES + lane) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[k][e] = w[k][e] = 0.0f;
+        if (at < a.width) load_w(a, at, w[k]);
+    }
+    const int64_t n = (a.rows + kRows - 1) / kRows;
+    int turn = 0;
+    for (int64_t b = blockIdx.x; b < n; b += gridDim.x, turn ^= 1) {
+        const int64_t row = b * kRows + threadIdx.x / LANES;
+        const bool there = row < a.rows;
+        Eight<T> s[NV], dy[NV], ds[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * 8;
+            s[k].zero(); dy[k].zero(); ds[k].zero();
+            if (there && at < a.width) {
+                s[k].load(static_cast<const T *>(a.x) + row * a.width + at);
+                dy[k].load(static_cast<const T *>(a.dy) + row * a.width + at);
+                if (a.r != nullptr) ds[k].load(static_cast<const T *>(a.r) + row * a.width + at);
+            }
+        }
+        float ss = 0.0f, es = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float t = 0.0f, u = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = s[k].get(e);
+                t = __builtin_fmaf(x, x, t);
+                u = __builtin_fmaf(dy[k].get(e) * w[k][e], x, u);
+            }
+            ss += t; es += u;
+        }
+        ss = lanes_all<LANES>(ss, sum_of);
+        es = lanes_all<LANES>(es, sum_of);
+        if constexpr (LANES > 64) {                           // (the words of the turn before may still be read)
+            if ((threadIdx.x & 63) == 0) { part[turn][0][threadIdx.x >> 6] = ss; part[turn][1][threadIdx.x >> 6] = es; }
+            __syncthreads();
+            ss = part[turn][0][0]; es = part[turn][1][0];
+#pragma unroll
+            for (int v = 1; v < LANES / 64; ++v) { ss += part[turn][0][v]; es += part[turn][1][v]; }
+        }
+        const float rstd = 1.0f / sqrtf(__builtin_fmaf(ss, a.per_width, a.eps)), c = es * a.per_width * rstd * rstd;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * 8;
+            float d[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = s[k].get(e), g = dy[k].get(e);
+                d[e] = __builtin_fmaf(rstd, __builtin_fmaf(-x, c, g * w[k][e]), ds[k].get(e));
+                dw[k][e] = __builtin_fmaf(g * rstd, x, dw[k][e]);
+            }
+            if (a.y != nullptr && there && at < a.width) {
+                Eight<T> o;
+                o.set(d);
+                o.store(static_cast<T *>(a.y) + row * a.width + at);
+            }
+        }
+    }
+    if (a.part == nullptr) return;
+    float *to = a.part + (int64_t)blockIdx.x * a.width;
+    if constexpr (kRows > 1) {                                // the rows' parts one after the other: a fixed order
+        for (int v = 0; v < kRows; ++v) {
+            if ((int)threadIdx.x / LANES == v) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int at = (k * LANES + lane) * 8 + e;
+                        if (at < a.width) sums[at] = v == 0 ? dw[k][e] : sums[at] + dw[k][e];
+                    }
+            }
+            __syncthreads();
+        }
+        for (int i = threadIdx.x; i < a.width; i += kThreads) to[i] = sums[i];
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * 8;
+            if (at < a.width) {
+                Eight<float> o;
+                o.set(dw[k]);
+                o.store(to + at);
+            }
+        }
+    }
+}
+
+// dw[i] = the sum over b of part[b][i]: 16 columns of four to a workgroup, 16 threads a column, each every 16th part, then theirs in order
+__global__ __launch_bounds__(256) void k_norm_dw(const float *__restrict__ part, float *__restrict__ dw, int parts, int width)
+{
+    __shared__ floatx4 sums[256];
+    const int c = threadIdx.x & 15, k = threadIdx.x >> 4, at = ((int)blockIdx.x * 16 + c) * 4;
+    floatx4 s = {0.f, 0.f, 0.f, 0.f};
+    if (at < width) {
+#pragma unroll 4
+        for (int b = k; b < parts; b += 16) s += *reinterpret_cast<const floatx4 *>(part + (int64_t)b * width + at);
+    }
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (k == 0 && at < width) {
+#pragma unroll
+        for (int v = 1; v < 16; ++v) s += sums[v * 16 + c];
+        *reinterpret_cast<floatx4 *>(dw + at) = s;
+    }
+}
+
+constexpr int kNormParts = 512;         // workgroups of a backward pass at most
+
+template <typename F> void by_width(int width, F f)
+{
+    const int n = width / 8;            // vectors of a row
+    if (n <= 8) f(IC<8>{}, IC<1>{});
+    else if (n <= 16) f(IC<16>{}, IC<1>{});
+    else if (n <= 32) f(IC<32>{}, IC<1>{});
+    else if (n <= 64) f(IC<64>{}, IC<1>{});
+    else if (n <= 128) f(IC<64>{}, IC<2>{});
+    else if (n <= 256) f(IC<256>{}, IC<1>{});
+    else if (n <= 512) f(IC<256>{}, IC<2>{});
+    else if (n <= 768) f(IC<256>{}, IC<3>{});
+    else if (n <= 1024) f(IC<256>{}, IC<4>{});
+    else if (n <= 2048) f(IC<512>{}, IC<4>{});
+    else f(IC<1024>{}, IC<4>{});
+}
+
+int bwd_blocks(int64_t rows, int width)
+{
+    int per = 1;
+    by_width(width, [&](auto lanes, auto) { per = decltype(lanes)::value < 256 ? 256 / decltype(lanes)::value : 1; });
+    const int64_t n = (rows + per - 1) / per;
+    return (int)std::min<int64_t>(n, kNormParts);
+}
+
+}  // namespace
+
+size_t norm_ws_bytes(int64_t rows, int width) { return rows > 0 ? (size_t)bwd_blocks(rows, width) * width * sizeof(float) : 0; }
+
+void launch_norm_fwd(const NormFwd &n, hipStream_t st)
+{
+    NormArgs a{};
+    a.rows = n.rows; a.x = n.x; a.r = n.r; a.w = n.w; a.s = n.s; a.y = n.y; a.codes = n.codes; a.scales = n.scales;
+    a.width = n.width; a.group = n.group; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
+    by_width(n.width, [&](auto lanes, auto nv) {
+        constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
+        const unsigned blocks = (unsigned)((n.rows + kThreads / L - 1) / (kThreads / L));
+        if (n.act_bf16) k_norm_fwd<bf16_t, L, N, false><<<blocks, kThreads, 0, st>>>(a);
+        else k_norm_fwd<float, L, N, false><<<blocks, kThreads, 0, st>>>(a);
+    });
+}
+
+void launch_norm_bwd(const NormBwd &n, void *ws, hipStream_t st)
+{
+    NormArgs a{};
+    const int blocks = bwd_blocks(n.rows, n.width);
+    a.rows = n.rows; a.x = n.s; a.r = n.ds; a.w = n.w; a.dy = n.dy; a.y = n.dx;
+    a.part = n.dw == nullptr ? nullptr : blocks == 1 ? n.dw : static_cast<float *>(ws);
+    a.width = n.width; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
+    if (blocks > 0) by_width(n.width, [&](auto lanes, auto nv) {
+        constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
+        const size_t lds = L < 256 && n.dw != nullptr ? (size_t)n.width * sizeof(float) : 0;
+        if (n.act_bf16) k_norm_bwd<bf16_t, L, N><<<blocks, kThreads, lds, st>>>(a);
+        else k_norm_bwd<float, L, N><<<blocks, kThreads, lds, st>>>(a);
+    });
+    if (n.dw != nullptr && blocks != 1) k_norm_dw<<<(n.width / 4 + 15) / 16, 256, 0, st>>>(a.part, n.dw, blocks, n.width);
+}
+
+}  // namespace eqat

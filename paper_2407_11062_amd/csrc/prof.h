@@ -8,7 +8,7 @@
 namespace eqat {
 
 enum ProfKernel {
-    PK_INIT_MINMAX = 0, PK_QUANTIZE, PK_PREPARE, PK_GEMM_FWD, PK_GEMM_DX, PK_GEMM_DW, PK_GEMM_BWD, PK_REDUCE, PK_F32, PK_GEMV, PK_LOSS, PK_UPDATE, PK_KV_WRITE, PK_KV_READ, PK_KV_ATTEND, PK_COUNT
+    PK_INIT_MINMAX = 0, PK_QUANTIZE, PK_PREPARE, PK_GEMM_FWD, PK_GEMM_DX, PK_GEMM_DW, PK_GEMM_BWD, PK_REDUCE, PK_F32, PK_GEMV, PK_LOSS, PK_UPDATE, PK_KV_WRITE, PK_KV_READ, PK_KV_ATTEND, PK_NORM, PK_ROTARY, PK_GATE, PK_COUNT
 };
 
 extern std::atomic<bool> g_prof_on;

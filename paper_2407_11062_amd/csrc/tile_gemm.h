@@ -6,6 +6,7 @@
 // The paddings make both read patterns bank-conflict free.
 #pragma once
 #include "common.h"
+#include "gate.h"
 #include "gemm_tiles.h"
 #include "kernels.h"
 
@@ -228,6 +229,7 @@ struct GemmQArgs {
     int tiles_m, tiles_n;
     int band;              // tile rows walked together by one XCD (see tile_of_xcd_slot)
     SkPlan sk;             // which tiles, or parts of tiles, a workgroup computes
+    const bf16_t *dH; bf16_t *dY; uint32_t dh_bytes, dy_bytes; int kind;      // of the gated feed-forward (GateMode), whose H is C [M, N / 2]
 };
 
 // f(IC<0>{}), f(IC<1>{}), ..., f(IC<N - 1>{}): a loop whose index is a compile-time constant inside the body
@@ -256,7 +258,11 @@ template <int ACC_REGS> __device__ __forceinline__ void want_agpr_accumulators()
 // any contraction length; kWhole: whole tiles, a contraction of a multiple of two K tiles, and none of that code (the main loop is sensitive to it).
 // (bid, grid): this workgroup's number among those of the GEMM, which may share its launch with another one.
 enum QMode { kWhole, kCut, kRagged };
-template <int BITS, bool BT, int MODE, int BM, int BN, int BK, int WGM, int WGN>
+// GATE (forward, N = 2 F, the gate's rows of the weights first): blocks of 32 rows of the gate and the same 32 of the other half take turns in a tile's columns, so that the two blocks of
+// a wave's columns are a gate's and their partners, in the same registers of the same lanes.  kGateFwd: C [M, F] = H = act(G) U.  kGateBwd: dH [M, F] comes through the patch of
+// LDS that the results leave through, and with it leave H and dY = [dH U act'(G) | dH act(G)] (an absent one: a buffer of no bytes, whose stores are dropped).
+enum GateMode { kNoGate, kGateFwd, kGateBwd };
+template <int BITS, bool BT, int MODE, int BM, int BN, int BK, int WGM, int WGN, int GATE = kNoGate>
 __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, const int grid)
 {
     constexpr bool CUT = MODE == kCut;
@@ -394,7 +400,8 @@ __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, c
             const int sidx = it * NT + tid;
             int wrow, wcol;   // position in the weight matrix [O][I]
             if (!BT) { wrow = c_n0 + sidx / (BK / 32); wcol = c_k0 + (sidx % (BK / 32)) * 32; }
-            else     { wrow = c_k0 + sidx / (BN / 32); wcol = c_n0 + (sidx % (BN / 32)) * 32; }
+            if constexpr (GATE != kNoGate) { const int v = sidx / (BK / 32); wrow = (c_n0 >> 1) + ((v >> 6) << 5) + (v & 31) + (v & 32 ? a.N >> 1 : 0); }
+            if (BT) { wrow = c_k0 + sidx / (BN / 32); wcol = c_n0 + (sidx % (BN / 32)) * 32; }
             const bool ok = wcol < a.I;
             stC[S][it] = load_work_codes<BITS>(rC, (uint32_t)wrow * code_row_bytes + (uint32_t)(wcol >> 5) * (4u * WorkCodes<BITS>::kWords));
             const intx2 sv = buf_load8(rS, ok ? ((uint32_t)wrow * (uint32_t)a.G + (uint32_t)grp[it]) * 8u : kOobOffset);
@@ -560,7 +567,59 @@ __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, c
         // the registers that is sixteen 2-byte stores per block, each to two rows; instead the block goes through a
         // 2 KB patch of LDS of the wave's own (behind the tile ring, which the loads of the next tile are filling) and
         // leaves as two 16-byte stores per lane, 64 bytes of a row from four neighbouring lanes.
-        {
+        if constexpr (GATE != kNoGate) {
+            static_assert(!BT && NI == 2, "a wave's columns are a block of the gate's and one of the others");
+            unsigned char *const stg = smem_raw + kRingBytes + wave * kStoreStageBytes;
+            bf16_t *const cell = reinterpret_cast<bf16_t *>(stg) + (lane >> 5) * (4 * 32) + (lane & 31);
+            const int F = a.N >> 1, f = (n0 >> 1) + wn * 32 + (lane & 3) * 8;
+            auto place = [&](int i, int k, int row) -> uint32_t {          // of 16 bytes of row m in rows of `row` elements
+                const int m = m0 + wm * WTM + i * 32 + k * 16 + (lane >> 2);
+                return m < a.M && f < F ? ((uint32_t)m * (uint32_t)row + (uint32_t)f) * 2u : kOobOffset;
+            };
+            auto meet = [&]() { asm volatile("" ::: "memory"); __builtin_amdgcn_wave_barrier(); };          // LDS accesses of a wave complete in order
+            auto leave = [&](__amdgpu_buffer_rsrc_t to, int i, int row, uint32_t at) {
+                meet();
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t o = place(i, k, row);
+                    __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const intx4 *>(stg + k * 1024 + lane * 16), to, (int)(o == kOobOffset ? o : o + at), 0, 0);
+                }
+                meet();
+            };
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                if constexpr (GATE == kGateFwd) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        cell[(8 * (r >> 2) + (r & 3)) * 32] = (bf16_t)gated_by(a.kind, acc[i][0][r], acc[i][1][r]);
+                        acc[i][0][r] = acc[i][1][r] = 0.0f;
+                    }
+                    leave(rCst, i, F, 0u);
+                } else {
+                    const __amdgpu_buffer_rsrc_t rDh = make_rsrc(a.dH, a.dh_bytes), rDy = make_rsrc(a.dY, a.dy_bytes);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) *reinterpret_cast<intx4 *>(stg + k * 1024 + lane * 16) = buf_load16(rDh, place(i, k, F));
+                    meet();
+                    bf16x2 pair[16];                                       // dg, du
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        bf16_t *const at = cell + (8 * (r >> 2) + (r & 3)) * 32;
+                        const Gated g = gated_both(a.kind, acc[i][0][r], acc[i][1][r], (float)*at);
+                        *at = (bf16_t)g.h;
+                        pair[r][0] = (bf16_t)g.dg; pair[r][1] = (bf16_t)g.du;
+                        acc[i][0][r] = acc[i][1][r] = 0.0f;
+                    }
+                    leave(rCst, i, F, 0u);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) cell[(8 * (r >> 2) + (r & 3)) * 32] = pair[r][half];
+                        leave(rDy, i, a.N, half ? (uint32_t)F * 2u : 0u);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
             unsigned char *const stg = smem_raw + kRingBytes + wave * kStoreStageBytes;
             bf16_t *const cell = reinterpret_cast<bf16_t *>(stg) + (lane >> 5) * (4 * 32) + (lane & 31);
 #pragma unroll
