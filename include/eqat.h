@@ -549,7 +549,7 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *              alone between its passes; dY is what eqat_qlinear_bwd of the layer takes (dX, ds), H the input of the next linear in its own backward pass.
  *   _prepared  the same on a layer prepared by eqat_qlinear_prepare, s the current step sizes, the zero points those that it was prepared with.  Like the calls of eqat_qlinear_fwd_prepared,
  *              calls on one prepared layer must not overlap in time.
- *   ws         eqat_gated_workspace_bytes(d, prepared) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
+ *   ws         eqat_gated_workspace_bytes(d) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
  * With fp32 activations the projections are those of eqat_qlinear_fwd, in the workspace, and the gate a launch of its own.
  * EQAT_ERR_HYPER for an unknown kind.
  */
@@ -557,7 +557,7 @@ typedef enum { EQAT_GATE_SILU = 0, EQAT_GATE_GELU = 1 } eqat_gate_kind;
 
 eqat_status eqat_gate_fwd(int64_t tokens, int64_t F, int32_t dtype, int kind, const void *Y, void *H, void *stream);
 eqat_status eqat_gate_bwd(int64_t tokens, int64_t F, int32_t dtype, int kind, const void *Y, const void *dH, void *dY, void *H, void *stream);
-size_t eqat_gated_workspace_bytes(const eqat_desc *d, int prepared);                 /* 0 for a bad descriptor */
+size_t eqat_gated_workspace_bytes(const eqat_desc *d);                 /* 0 for a bad descriptor */
 eqat_status eqat_gated_fwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, void *H, void *ws, size_t ws_bytes, void *stream);
 eqat_status eqat_gated_bwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, const void *dH, void *dY, void *H,
                            void *ws, size_t ws_bytes, void *stream);

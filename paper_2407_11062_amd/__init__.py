@@ -149,7 +149,7 @@ def lib():
         L.eqat_kv_rotary_write.argtypes = [kd, kb, kr, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.eqat_gate_fwd.argtypes = [i64, i64, ctypes.c_int32, i32, vp, vp, vp]
         L.eqat_gate_bwd.argtypes = [i64, i64, ctypes.c_int32, i32, vp, vp, vp, vp, vp]
-        L.eqat_gated_workspace_bytes.restype, L.eqat_gated_workspace_bytes.argtypes = sz, [dp, i32]
+        L.eqat_gated_workspace_bytes.restype, L.eqat_gated_workspace_bytes.argtypes = sz, [dp]
         L.eqat_gated_fwd.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
         L.eqat_gated_bwd.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.eqat_gated_fwd_prepared.argtypes = [dp, i32, vp, vp, vp, vp, vp, sz, vp]
@@ -577,45 +577,61 @@ def _norm_ref(tokens, width, group, act_dtype, w_dtype, eps):
     return ctypes.byref(NormDesc(tokens, _i32("width", width), _i32("group", group), act_dtype, w_dtype, eps))
 
 
+# As above, what happens here is what bounds the smallest calls: shapes are compared as they are, and what a call goes by is looked up once.
 def _like(name, t, shape, dtype):
     """The pointer of a tensor whose shape and type the call goes by; None stays None."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    return _p(t)
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} device tensor {list(shape)}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _codes_ptr(codes, T, n):
-    if codes is None:
-        return None
-    if codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or tuple(codes.shape) != (T, n):
-        raise ValueError(f"codes: expected float8_e4m3fn or uint8 [{T}, {n}], got {codes.dtype} {list(codes.shape)}")
-    return _p(codes)
+def _like_w(W, n):
+    """(pointer, type) of a norm's weights; None stays None."""
+    if W is None:
+        return None, F32
+    code = _dt(W)
+    return _like("W", W, (n,), W.dtype), code
+
+
+def _codes_ptr(codes, shape):
+    if codes.dtype is not torch.uint8 and codes.dtype is not torch.float8_e4m3fn:
+        raise ValueError(f"codes: expected float8_e4m3fn or uint8, got {codes.dtype}")
+    return _like("codes", codes, shape, codes.dtype)
 
 
 def eqat_norm_fwd(X, W, eps, R=None, group=0, want=None, out=None):
     """Root-mean-square norm of S = X + R (R None: of X) over the rows of [tokens, width]; W [width] or None.  `want`: which of "S", "Y", "codes" (float8_e4m3fn, with "scales", one
     for `group` neighbouring elements, -1: a row) to make, by default Y, or the codes where a group is given, and S where R is; tensors in `out` are filled."""
-    T, n = X.shape
-    group = _i32("group", group)
+    shape, dtype, act = X.shape, X.dtype, _dt(X)
+    T, n = shape
     if want is None:
         want = (("S",) if R is not None else ()) + (("codes",) if group else ("Y",))
     out = {} if out is None else out
-    per = 1 if group == -1 else n // group if group > 0 else 0
-    for name in ("S", "Y"):
-        if name in want and name not in out: out[name] = torch.empty_like(X)
-    codes = "codes" in want or "scales" in want
-    if codes:
-        if per == 0:
+    S = Y = codes = scales = None
+    if "S" in want:
+        S = out.get("S")
+        if S is None: S = out["S"] = torch.empty_like(X)
+        S = _like("S", S, shape, dtype)
+    if "Y" in want:
+        Y = out.get("Y")
+        if Y is None: Y = out["Y"] = torch.empty_like(X)
+        Y = _like("Y", Y, shape, dtype)
+    if "codes" in want or "scales" in want:
+        group = _i32("group", group)
+        if group == 0:
             raise ValueError("codes need a group (-1: one scale a row)")
+        per = n // group if group > 0 else 1
         if "codes" not in out: out["codes"] = torch.empty((T, n), dtype=torch.float8_e4m3fn, device=X.device)
         if "scales" not in out: out["scales"] = torch.empty((T, per), dtype=torch.float32, device=X.device)
-    get = lambda name: out.get(name) if name in want else None
-    d = _norm_ref(T, n, group if codes else -1, _dt(X), _dt(X) if W is None else _dt(W), float(eps))
-    _check("eqat_norm_fwd", lib().eqat_norm_fwd(
-        d, _p(X), _like("R", R, X.shape, X.dtype), _like("W", W, (n,), W.dtype) if W is not None else None, _like("S", get("S"), X.shape, X.dtype),
-        _like("Y", get("Y"), X.shape, X.dtype), _codes_ptr(out["codes"], T, n) if codes else None, _like("scales", out["scales"], (T, per), torch.float32) if codes else None, _stream()))
+        codes, scales = _codes_ptr(out["codes"], shape), _like("scales", out["scales"], (T, per), torch.float32)
+    else:
+        group = -1
+    w, w_type = _like_w(W, n)
+    status = lib().eqat_norm_fwd(_norm_ref(T, n, group, act, w_type, eps), _p(X), _like("R", R, shape, dtype), w, S, Y, codes, scales, _stream())
+    if status:
+        _check("eqat_norm_fwd", status)
     return out
 
 
@@ -627,17 +643,24 @@ def norm_workspace(tokens, width, dtype=torch.bfloat16, device="cuda") -> torch.
 
 def eqat_norm_bwd(S, W, eps, dY, dS=None, want=("dX", "dW"), out=None, ws=None):
     """Gradients of eqat_norm_fwd from S (what it left, or its X): dX (also that of R) in S's type, dW fp32 [width].  dS: the gradient that reaches S along the residual."""
-    T, n = S.shape
+    shape, dtype, act = S.shape, S.dtype, _dt(S)
+    T, n = shape
     out = {} if out is None else out
-    if "dX" in want and "dX" not in out: out["dX"] = torch.empty_like(S)
-    if "dW" in want and "dW" not in out: out["dW"] = torch.empty(n, dtype=torch.float32, device=S.device)
-    if ws is None and "dW" in want:
-        ws = norm_workspace(T, n, S.dtype, S.device)
-    get = lambda name: out.get(name) if name in want else None
-    d = _norm_ref(T, n, -1, _dt(S), _dt(S) if W is None else _dt(W), float(eps))
-    _check("eqat_norm_bwd", lib().eqat_norm_bwd(
-        d, _p(S), _like("W", W, (n,), W.dtype) if W is not None else None, _like("dY", dY, S.shape, S.dtype), _like("dS", dS, S.shape, S.dtype),
-        _like("dX", get("dX"), S.shape, S.dtype), _like("dW", get("dW"), (n,), torch.float32), _p(ws), 0 if ws is None else ws.numel(), _stream()))
+    dX = dW = None
+    if "dX" in want:
+        dX = out.get("dX")
+        if dX is None: dX = out["dX"] = torch.empty_like(S)
+        dX = _like("dX", dX, shape, dtype)
+    if "dW" in want:
+        dW = out.get("dW")
+        if dW is None: dW = out["dW"] = torch.empty(n, dtype=torch.float32, device=S.device)
+        dW = _like("dW", dW, (n,), torch.float32)
+        if ws is None: ws = norm_workspace(T, n, dtype, S.device)
+    w, w_type = _like_w(W, n)
+    status = lib().eqat_norm_bwd(_norm_ref(T, n, -1, act, w_type, eps), _p(S), w, _like("dY", dY, shape, dtype), _like("dS", dS, shape, dtype), dX, dW,
+                                 _p(ws), 0 if ws is None else ws.numel(), _stream())
+    if status:
+        _check("eqat_norm_bwd", status)
     return out
 
 
@@ -665,35 +688,45 @@ class Rotary:
         self.refs = {dt: ctypes.byref(d) for dt, d in self.descs.items()}
 
 
+@functools.lru_cache(maxsize=1024)
+def _rows_of(shape, stride, tokens, head_dim):
+    """(heads, address of the {token, head} strides in memory, their array) of a [tokens, heads, head_dim] tensor; the cache is by value"""
+    if len(shape) != 3:
+        raise ValueError("expected [tokens, heads, head_dim]")
+    at, both = _kv_strides(shape, stride, tokens, shape[1], head_dim)
+    return shape[1], at, both
+
+
 def _turned(rot, t, out, tokens, dtype):
     """(pointer, strides, heads, pointer, strides) of what is turned and of where it goes"""
     if t is None:
         if out is not None:
             raise ValueError("an output without its input")
         return None, None, 0, None, None
-    for x in (t, out):
-        if x.dtype != dtype or not x.is_cuda:
-            raise ValueError(f"expected a {dtype} device tensor, got {x.dtype} on {x.device}")
-        if x.dim() != 3:
-            raise ValueError("expected [tokens, heads, head_dim]")
-    heads = t.shape[1]
-    return (t.data_ptr(), _kv_strides(t.shape, t.stride(), tokens, heads, rot.head_dim)[0], heads, out.data_ptr(),
-            _kv_strides(out.shape, out.stride(), tokens, heads, rot.head_dim)[0])
+    if t.dtype is not dtype or out.dtype is not dtype or not t.is_cuda or not out.is_cuda:
+        raise ValueError(f"expected {dtype} device tensors, got {t.dtype} on {t.device} and {out.dtype} on {out.device}")
+    if out.shape != t.shape:
+        raise ValueError(f"expected {list(t.shape)}, got {list(out.shape)}")
+    heads, at, _ = _rows_of(t.shape, t.stride(), tokens, rot.head_dim)
+    return t.data_ptr(), at, heads, out.data_ptr(), _rows_of(out.shape, out.stride(), tokens, rot.head_dim)[1]
 
 
 def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, inverse=False):
     """(q, k) [tokens, heads, head_dim] (any token and head strides) turned by their tokens' positions (int32 [tokens]); into q_out, k_out (which may be q and k themselves)."""
-    if positions.dtype != torch.int32 or positions.dim() != 1:
+    if positions.dtype is not torch.int32 or positions.dim() != 1:
         raise TypeError("positions are int32 [tokens]")
     T, like = positions.numel(), q if q is not None else k
     if like is None:
         return None, None
     if q is not None and q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if k is not None and k_out is None: k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    if like.dtype not in rot.refs:
-        raise TypeError(f"unsupported dtype {like.dtype}")
-    _check("eqat_rotary", lib().eqat_rotary(rot.refs[like.dtype], T, _p(positions), *_turned(rot, q, q_out, T, like.dtype), *_turned(rot, k, k_out, T, like.dtype),
-                                            1 if inverse else 0, _stream()))
+    dtype = like.dtype
+    ref = rot.refs.get(dtype)
+    if ref is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    status = lib().eqat_rotary(ref, T, _p(positions), *_turned(rot, q, q_out, T, dtype), *_turned(rot, k, k_out, T, dtype), 1 if inverse else 0, _stream())
+    if status:
+        _check("eqat_rotary", status)
     return q_out, k_out
 
 
@@ -702,9 +735,10 @@ def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q
     if rot.head_dim != cache.head_dim:
         raise ValueError(f"heads of {rot.head_dim} in a cache of heads of {cache.head_dim}")
     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    qp, qs, heads, op, os_ = _turned(rot, q, q_out, batch.tokens, cache.dtype)
     (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
-    _check("eqat_kv_rotary_write", lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[cache.dtype], qp, qs, heads, op, os_, kp, ks[0], vp, vs[0], _p(cache.pool), _stream()))
+    status = lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[cache.dtype], *_turned(rot, q, q_out, batch.tokens, cache.dtype), kp, ks[0], vp, vs[0], _p(cache.pool), _stream())
+    if status:
+        _check("eqat_kv_rotary_write", status)
     return q_out
 
 
@@ -731,19 +765,27 @@ def eqat_gate_bwd(Y, dH, kind=GATE_SILU, want=("dY",), out=None):
 def gated_workspace(tokens, in_features, F, bits, group, dtype=torch.bfloat16, prepared=False, device="cuda") -> torch.Tensor:
     """The workspace of eqat_gated_fwd and eqat_gated_bwd (or their calls on a prepared layer); that of more tokens serves fewer."""
     d = _desc_ref(int(tokens), int(in_features), 2 * int(F), int(bits), int(group), BF16 if dtype == torch.bfloat16 else F32, BF16)
-    n = lib().eqat_gated_workspace_bytes(d, 1 if prepared else 0)
+    n = lib().eqat_gated_workspace_bytes(d)
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
 def _gated(name, X, F, bits, group, layer, kind, dH, want, out, ws, prepared):
     T, I = X.shape
-    d = _desc_ref(T, I, 2 * F, int(bits), int(group), _dt(X), BF16)
-    if "H" in want and "H" not in out: out["H"] = torch.empty((T, F), dtype=X.dtype, device=X.device)
-    if "dY" in want and "dY" not in out: out["dY"] = torch.empty((T, 2 * F), dtype=X.dtype, device=X.device)
-    ws = gated_workspace(T, I, F, bits, group, X.dtype, prepared, X.device) if ws is None else ws
-    H = _like("H", out["H"] if "H" in want else None, (T, F), X.dtype)
-    back = () if dH is None else (_like("dH", dH, (T, F), X.dtype), _like("dY", out["dY"] if "dY" in want else None, (T, 2 * F), X.dtype))
-    _check(name, getattr(lib(), name)(d, int(kind), _p(X), *layer, *back, H, _p(ws), ws.numel(), _stream()))
+    dtype, h, y = X.dtype, (T, F), (T, 2 * F)
+    H = back = None
+    if "H" in want:
+        H = out.get("H")
+        if H is None: H = out["H"] = torch.empty(h, dtype=dtype, device=X.device)
+        H = _like("H", H, h, dtype)
+    if "dY" in want:
+        back = out.get("dY")
+        if back is None: back = out["dY"] = torch.empty(y, dtype=dtype, device=X.device)
+        back = _like("dY", back, y, dtype)
+    back = () if dH is None else (_like("dH", dH, h, dtype), back)
+    ws = gated_workspace(T, I, F, bits, group, dtype, prepared, X.device) if ws is None else ws
+    status = getattr(lib(), name)(_desc_ref(T, I, 2 * F, bits, group, _dt(X), BF16), kind, _p(X), *layer, *back, H, _p(ws), ws.numel(), _stream())
+    if status:
+        _check(name, status)
     return out
 
 

@@ -611,24 +611,26 @@ eqat_status eqat_qlinear_bwd_prepared_kept(const eqat_desc *d, const void *X, co
 }
 
 // ---- gated feed-forward (d: the stacked projection, out_features = 2 F) ----------------------------------------------
-// codes in the working layout and (s, z) pairs; with fp32 activations the projections instead of the codes
-struct GatedWs { size_t y, codes, sz, total; };
-// which kernel: matrix-vector (forward, packed), the one for few output tiles, the tiles
+// (s, z) pairs; with fp32 activations the projections, too
+struct GatedWs { size_t y, sz, total; };
+// which kernel: matrix-vector (forward), the one for few output tiles, the tiles
 enum GatedKernel { GATED_GEMV, GATED_MID, GATED_TILES };
-static GatedKernel gated_kernel(const Problem &p, bool prepared, bool backward)
+static GatedKernel gated_kernel(const Problem &p, bool prepared, bool backward, int *tokens)
 {
-    if (!prepared && !backward && eqat::gemv_gated_applies(p)) return GATED_GEMV;
-    if (!eqat::group_by_magic(p)) return GATED_TILES;
-    return p.T <= 64 || eqat::mid_applies(p) ? GATED_MID : GATED_TILES;
+    int mid = 0;
+    const double tiles_us = eqat::tiles_gated_us(p, tokens), mid_us = eqat::mid_gated_us(p, !prepared, &mid);
+    if (!backward && eqat::gemv_gated_applies(p, !prepared, mid_us)) return GATED_GEMV;
+    if (!eqat::group_by_magic(p) || (p.T > 64 && tiles_us <= mid_us)) return GATED_TILES;
+    *tokens = mid;
+    return GATED_MID;
 }
-static GatedWs gated_ws(const Problem &p, bool prepared)
+static GatedWs gated_ws(const Problem &p)
 {
     GatedWs l{};
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += align256(bytes); return at; };
     if (!p.act_bf16) l.y = take((size_t)p.T * p.O * 4);
     else if (p.T <= 64 && eqat::group_by_magic(p)) return l;          // no kernel for so few tokens has anything in it
-    else if (!prepared) l.codes = take(eqat::work_code_bytes(p));
     l.sz = take((size_t)p.O * p.G * 8);
     l.total = off;
     return l;
@@ -649,7 +651,7 @@ static eqat_status gated_any(const eqat_desc *d, int kind, const void *X, const 
     if (p.T > 0 && wanted) { EQAT_REQUIRE(X); if (backward) EQAT_REQUIRE(dH); else EQAT_REQUIRE(H); }
     EQAT_ALIGNED(X); EQAT_ALIGNED(s); EQAT_ALIGNED(zpacked); EQAT_ALIGNED(dH); EQAT_ALIGNED(dY); EQAT_ALIGNED(H);
     if (!aligned(layer, prepared ? 256 : 16)) return EQAT_ERR_ALIGN;
-    const GatedWs l = gated_ws(p, prepared);
+    const GatedWs l = gated_ws(p);
     if (l.total > 0 && (ws == nullptr || ws_bytes < l.total)) return EQAT_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return EQAT_ERR_ALIGN;
     if (p.T == 0 || !wanted) return EQAT_OK;
@@ -664,26 +666,27 @@ static eqat_status gated_any(const eqat_desc *d, int kind, const void *X, const 
         { ProfScope ps(eqat::PK_F32, st); eqat::launch_f32_fwd(p, true, X, prepared ? p8 + pl.codes : p8, s, w8 + l.sz, w8 + l.y, st); }
         return backward ? eqat_gate_bwd(p.T, p.O / 2, EQAT_F32, kind, w8 + l.y, dH, dY, H, stream) : eqat_gate_fwd(p.T, p.O / 2, EQAT_F32, kind, w8 + l.y, H, stream);
     }
-    switch (gated_kernel(p, prepared, backward)) {
-    case GATED_GEMV: { ProfScope ps(eqat::PK_GEMV, st); eqat::launch_gemv_gated(p, kind, X, layer, s, zpacked, H, st); break; }
-    case GATED_MID: { ProfScope ps(eqat::PK_GEMM_FWD, st); eqat::launch_mid_gated(p, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); break; }
+    int tokens = 0;
+    switch (gated_kernel(p, prepared, backward, &tokens)) {
+    case GATED_GEMV: { ProfScope ps(eqat::PK_GEMV, st); eqat::launch_gemv_gated(p, kind, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, H, st); break; }
+    case GATED_MID: { ProfScope ps(eqat::PK_GEMM_FWD, st); eqat::launch_mid_gated(p, tokens, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); break; }
     default: {
-        qlinear_prepare_into(p, prepared ? nullptr : (const uint8_t *)layer, s, zpacked, zb, prepared ? nullptr : w8 + l.codes, w8 + l.sz, nullptr, 0, st);
+        qlinear_prepare_into(p, nullptr, s, zpacked, zb, nullptr, w8 + l.sz, nullptr, 0, st);
         ProfScope ps(eqat::PK_GEMM_FWD, st);
-        eqat::launch_tiles_gated(p, out, X, prepared ? (const void *)(p8 + pl.codes) : (const void *)(w8 + l.codes), w8 + l.sz, st);
+        eqat::launch_tiles_gated(p, tokens, !prepared, out, X, prepared ? p8 + pl.codes : p8, w8 + l.sz, st);
     }
     }
     return launch_status();
 }
 
-size_t eqat_gated_workspace_bytes(const eqat_desc *d, int prepared)
+size_t eqat_gated_workspace_bytes(const eqat_desc *d)
 {
     Problem p;
     if (d == nullptr) return 0;
     eqat_desc as_packed = *d;
     as_packed.w_dtype = EQAT_BF16;
     if (check_desc(&as_packed, true, &p) != EQAT_OK || p.O % 16 != 0) return 0;
-    return std::max<size_t>(gated_ws(p, prepared != 0).total, 256);
+    return std::max<size_t>(gated_ws(p).total, 256);
 }
 
 eqat_status eqat_gated_fwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, void *H, void *ws, size_t ws_bytes, void *stream)

@@ -2,6 +2,8 @@
 //
 // The main loop is the plain forward's (the weight operand rebuilt from codes in LDS, v_mfma_f32_32x32x16_bf16); rows of the two halves take turns in its columns, and G and U meet in
 // the registers that they were summed in, binary32.  Against the plain forward and a gate behind it this leaves out 3 T F elements of traffic and a launch, and two roundings.
+// A packed layer's codes are read as packed: the same main loop with another segment load and some more arithmetic, against a re-layout in front of it, us, re-laid / as packed: 333 tokens, 3 bit,
+// 5120 -> 2 x 13824 123 / 111; 2048 tokens, 4 bit, 8192 -> 2 x 28672 1641 / 1572, 2 bit, 4096 -> 2 x 11008 315 / 311; only 3-bit codes lose from some 3000 tokens on (4096 tokens 945 / 958).
 // Whole tiles only: no tile is cut along the contraction, and no scratch is needed.
 #include "common.h"
 #include "kernels.h"
@@ -13,10 +15,12 @@
 namespace eqat {
 namespace {
 
-template <int BITS, int MODE, typename TS, int GATE>
+typedef Tile<192, 256, 64, 2, 4> TileMiddle;      // 8 waves, 96x64 per wave
+
+template <int BITS, int MODE, typename TS, int GATE, bool DENSE>
 __global__ __launch_bounds__(64 * TS::WGM * TS::WGN) void k_gemm_gated(const GemmQArgs a)
 {
-    gemm_q_body<BITS, false, MODE, TS::BM, TS::BN, TS::BK, TS::WGM, TS::WGN, GATE>(a, (int)blockIdx.x, (int)gridDim.x);
+    gemm_q_body<BITS, false, MODE, TS::BM, TS::BN, TS::BK, TS::WGM, TS::WGN, GATE, DENSE>(a, (int)blockIdx.x, (int)gridDim.x);
 }
 
 int device_now()
@@ -25,7 +29,7 @@ int device_now()
     return hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < 64 ? dev : 0;
 }
 
-template <int BITS, int MODE, typename TS, int GATE> void launch_t(GemmQArgs a, hipStream_t st)
+template <int BITS, int MODE, typename TS, int GATE, bool DENSE> void launch_t(GemmQArgs a, hipStream_t st)
 {
     constexpr size_t smem = q_smem_bytes<false, TS>();
     static_assert(smem <= 160 * 1024, "LDS of one CU");
@@ -34,7 +38,7 @@ template <int BITS, int MODE, typename TS, int GATE> void launch_t(GemmQArgs a, 
     static std::atomic<int> cus_of[64];
     const int dev = device_now();
     if (!((allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {
-        (void)hipFuncSetAttribute((const void *)k_gemm_gated<BITS, MODE, TS, GATE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        (void)hipFuncSetAttribute((const void *)k_gemm_gated<BITS, MODE, TS, GATE, DENSE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         int n = 0;
         if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 8) n = 256;
         cus_of[dev].store(n, std::memory_order_relaxed);
@@ -49,33 +53,51 @@ template <int BITS, int MODE, typename TS, int GATE> void launch_t(GemmQArgs a, 
     a.sk.pairs = ((a.K + TS::BK - 1) / TS::BK + 1) / 2;
     a.sk.walk = ntiles > resident ? 1 : 0;            // several tiles to a workgroup: the first of the next is on its way when one ends
     a.sk.dp_rounds = (ntiles + resident - 1) / resident;
-    k_gemm_gated<BITS, MODE, TS, GATE><<<dim3((unsigned)(a.sk.walk ? resident : ntiles)), dim3(64 * TS::WGM * TS::WGN), smem, st>>>(a);
+    k_gemm_gated<BITS, MODE, TS, GATE, DENSE><<<dim3((unsigned)(a.sk.walk ? resident : ntiles)), dim3(64 * TS::WGM * TS::WGN), smem, st>>>(a);
 }
 
-template <int BITS, int GATE> void launch_bits(const GemmQArgs &a, hipStream_t st)
+template <int BITS, int GATE, bool DENSE> void launch_bits(const GemmQArgs &a, int tokens, hipStream_t st)
 {
-    // as the plain forward: big tiles where they fill most of the chip or the small ones do not fit twice a compute unit
-    const int64_t big = (int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256), small = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
     const bool whole = a.K % 128 == 0;
-    if (big >= 160 || small > 512) {
-        if (whole) launch_t<BITS, kWhole, TileBig, GATE>(a, st); else launch_t<BITS, kRagged, TileBig, GATE>(a, st);
+    if (tokens == TileBig::BM) {
+        if (whole) launch_t<BITS, kWhole, TileBig, GATE, DENSE>(a, st); else launch_t<BITS, kRagged, TileBig, GATE, DENSE>(a, st);
     } else {
-        if (whole) launch_t<BITS, kWhole, TileSmall, GATE>(a, st); else launch_t<BITS, kRagged, TileSmall, GATE>(a, st);
+        if (whole) launch_t<BITS, kWhole, TileMiddle, GATE, DENSE>(a, st); else launch_t<BITS, kRagged, TileMiddle, GATE, DENSE>(a, st);
     }
+}
+
+template <int BITS, int GATE> void launch_dense(const GemmQArgs &a, int tokens, bool dense, hipStream_t st)
+{
+    if (dense) launch_bits<BITS, GATE, true>(a, tokens, st); else launch_bits<BITS, GATE, false>(a, tokens, st);
 }
 
 }  // namespace
 
-void launch_tiles_gated(const Problem &p, const GatedOut &out, const void *X, const void *codes, const void *sz, hipStream_t st)
+// What it takes, in us, with the better of its token tiles: rounds of one workgroup a compute unit, a beginning each and so much for every K tile of 64, the more the longer they run (the chip's power).
+// Fitted to the same sizes as mid_gated_us, which also says why there are tiles of 192: 333 tokens are two of them, 11008 x 4096 91 -> 77 us, 515 tokens of 28672 x 8192 640 -> 527, 1500 of 4096 301 -> 251.
+// (128 x 128, two workgroups a compute unit, was never the best.)
+double tiles_gated_us(const Problem &p, int *tokens)
+{
+    const double k = (double)((p.I + 63) / 64);
+    auto us = [&](int bm, double first, double each, double more) {
+        const int64_t tiles = ((p.T + bm - 1) / bm) * ((p.O + 255) / 256);
+        return (double)((tiles + 255) / 256) * (first + k * (each + more * k));
+    };
+    const double big = us(256, 10.0, 1.27, 0.003), middle = us(192, 8.0, 1.03, 0.0025);
+    *tokens = middle < big ? 192 : 256;
+    return (middle < big ? middle : big) + 2.5;            // the launch in front that pairs step sizes and zero points
+}
+
+void launch_tiles_gated(const Problem &p, int tokens, bool dense, const GatedOut &out, const void *X, const void *codes, const void *sz, hipStream_t st)
 {
     GemmQArgs a{};
     a.A = (const bf16_t *)X; a.codes = (const uint32_t *)codes; a.sz = (const floatx2 *)sz; a.C = (bf16_t *)out.H;
     a.M = (int)p.T; a.N = (int)p.O; a.K = (int)p.I; a.I = (int)p.I; a.G = (int)p.G; a.g = (int)p.g;
-    a.a_bytes = (uint32_t)(p.T * p.I * 2); a.codes_bytes = (uint32_t)work_code_bytes(p); a.sz_bytes = (uint32_t)(p.O * p.G * 8);
+    a.a_bytes = (uint32_t)(p.T * p.I * 2); a.codes_bytes = dense ? (uint32_t)(p.O * p.I * p.bits / 8) : (uint32_t)work_code_bytes(p); a.sz_bytes = (uint32_t)(p.O * p.G * 8);
     a.c_bytes = out.H != nullptr ? (uint32_t)(p.T * p.O) : 0u;
     a.dH = (const bf16_t *)out.dH; a.dY = (bf16_t *)out.dY; a.kind = out.kind;
     a.dh_bytes = out.dH != nullptr ? (uint32_t)(p.T * p.O) : 0u; a.dy_bytes = out.dY != nullptr ? (uint32_t)(p.T * p.O * 2) : 0u;
-#define EQAT_GATED(B) do { if (out.dH != nullptr) launch_bits<B, kGateBwd>(a, st); else launch_bits<B, kGateFwd>(a, st); } while (0)
+#define EQAT_GATED(B) do { if (out.dH != nullptr) launch_dense<B, kGateBwd>(a, tokens, dense, st); else launch_dense<B, kGateFwd>(a, tokens, dense, st); } while (0)
     if (p.bits == 2) EQAT_GATED(2); else if (p.bits == 3) EQAT_GATED(3); else EQAT_GATED(4);
 #undef EQAT_GATED
 }

@@ -713,9 +713,9 @@ int token_tile(const Problem &p)
     return tall_applies(p) && launch_us(p, 128) < launch_us(p, low) ? 128 : low;
 }
 
-template <int SRC, bool GATED = false> void launch_src(const Problem &p, const MidArgs &a, hipStream_t st)
+template <int SRC, bool GATED = false> void launch_src(const Problem &p, const MidArgs &a, hipStream_t st, int bm = 0)
 {
-    const int bm = token_tile(p);
+    if (bm == 0) bm = token_tile(p);
 #define EQAT_MID(B) do { if (bm == 128) launch_t<B, SRC, 128, GATED>(a, st); else if (bm == 96) launch_t<B, SRC, 96, GATED>(a, st); else launch_t<B, SRC, 64, GATED>(a, st); } while (0)
     if (p.bits == 2) EQAT_MID(2); else if (p.bits == 3) EQAT_MID(3); else EQAT_MID(4);
 #undef EQAT_MID

@@ -375,7 +375,7 @@ template <int TR, bool DIRECT> constexpr int kWideRowBytes = 4 * kWideSub<TR, DI
 // What a wave fetches of the weights per run and 16-row block, straight into LDS: row pieces of 16 segments of codes, then the step sizes and
 // zero points of their groups.  The chunk c (16 bytes) of a row lies where the 16 rows that a read serves together meet different banks.
 template <int BITS, int SRC, int NG> struct WideRun {
-    static constexpr int WPS = SRC == kWorking ? WorkCodes<BITS>::kWords : BITS;                  // words per segment (the working layout is read by the lanes)
+    static constexpr int WPS = kRelaid<SRC> ? WorkCodes<BITS>::kWords : BITS;                      // words per segment (the working layout is read by the lanes)
     static constexpr int CPR = 4 * WPS;                                                           // chunks of a row piece
     static constexpr int CODES = 16 * CPR * 16, S = NG * 256, Z = SRC == kPackedZ ? 256 : NG * 256, BYTES = CODES + S + Z;
     static __device__ __forceinline__ int place(int row, int c)
@@ -396,7 +396,7 @@ template <int BITS, int SRC, int NG> struct WideRun {
 // of two segments a lane group, 8 KB a wave in all.  us, by the lanes / so: 8 tokens, 3 bit, 5120 / 13824 block 98 / 86 (with a patch of four segments 102, of one 92),
 // 2 bit, 28672 x 8192 29.4 / 26.6.  More tokens leave no such room: 16 tokens, 2 bit, 4096 / 11008 50 / 55, 13 tokens, 3 bit, 3200 /
 // 10880 54 / 60 (though 5120 / 13824 118 / 111), 24 tokens, 3 bit, g = 32 88 / 90.
-template <int SRC, int TR> constexpr bool kWideDirect = SRC != kWorking && TR == 8;
+template <int SRC, int TR> constexpr bool kWideDirect = !kRelaid<SRC> && TR == 8;
 template <int BITS, int SRC, int NG, int TR, int RB, bool DIRECT>
 constexpr int kWideWaveBytes = TR * kWideRowBytes<TR, DIRECT> + (DIRECT ? RB * WideRun<BITS, SRC, NG>::BYTES : 0);
 // Where the pieces are the faster way.  A wave with little to fetch ahead waits the longer for its first run: 1024 inputs, 0.2 to 0.5 us of 3 to 4.  8 tokens, us, by the
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(64 * kGemvMaxWaves) void k_gemv_wide(const GemvArgs
 
     const __amdgpu_buffer_rsrc_t rX = make_rsrc(a.X, a.x_bytes);
     const RawRsrc rW = make_raw_rsrc(a.Wp, a.w_bytes), rS = make_raw_rsrc(a.s, a.s_bytes);
-    const RawRsrc rZ = make_raw_rsrc(SRC == kFloatZ ? (const void *)a.zf : (const void *)a.zp, a.z_bytes);
+    const RawRsrc rZ = make_raw_rsrc(kTwoFloats<SRC> ? (const void *)a.zf : (const void *)a.zp, a.z_bytes);
 
     // Piece `sub` of run `sc`: 16-byte chunk i of this lane is number (lane + 64 i) of [token][lane group][SUB][4], so that
     // neighbouring lanes read neighbouring chunks; tokens and segments past the end come as zeros.
@@ -503,7 +503,7 @@ __global__ __launch_bounds__(64 * kGemvMaxWaves) void k_gemv_wide(const GemvArgs
     };
     struct Run { uintx4 cq[RB][WPS]; float sq[RB][NG], zq[RB][NG]; uint32_t zw[RB][2]; };
     // the same by the lanes that use them
-    [[maybe_unused]] const __amdgpu_buffer_rsrc_t bW = make_rsrc(a.Wp, a.w_bytes), bS = make_rsrc(a.s, a.s_bytes), bZ = make_rsrc(SRC == kFloatZ ? (const void *)a.zf : (const void *)a.zp, a.z_bytes);
+    [[maybe_unused]] const __amdgpu_buffer_rsrc_t bW = make_rsrc(a.Wp, a.w_bytes), bS = make_rsrc(a.s, a.s_bytes), bZ = make_rsrc(kTwoFloats<SRC> ? (const void *)a.zf : (const void *)a.zp, a.z_bytes);
     auto fetch_run = [&](int sc, Run &into) {
         const int seg0 = (sc * 4 + kq) * RS;
         const uint32_t j0 = group_of(seg0);
@@ -540,7 +540,7 @@ __global__ __launch_bounds__(64 * kGemvMaxWaves) void k_gemv_wide(const GemvArgs
             } else {
                 wide(bS, into.sq[rb]);
             }
-            if constexpr (SRC == kFloatZ) {
+            if constexpr (kTwoFloats<SRC>) {
                 wide(bZ, into.zq[rb]);
             } else if constexpr (SRC == kPackedZ) {
                 const uint32_t wi = (j0 * BITS) >> 5;
@@ -627,7 +627,7 @@ __global__ __launch_bounds__(64 * kGemvMaxWaves) void k_gemv_wide(const GemvArgs
                     } else if (seg0 + u >= n_segs) {
                         tab[rb].build(0.0f, 0.0f);
                     }
-                    if constexpr (SRC == kWorking) {
+                    if constexpr (kRelaid<SRC>) {
                         WorkCodes<BITS> cw;
 #pragma unroll
                         for (int j = 0; j < WPS; ++j) cw.w[j] = run.cq[rb][(u * WPS + j) / 4][(u * WPS + j) % 4];
@@ -757,7 +757,7 @@ static bool wide_keeps_words(int I, int O, int rows)
 template <int BITS, int SRC, int NG, int TR, int RB, bool GATED = false, bool KEEP = true, bool DIRECT = kWideDirect<SRC, TR>>
 static void launch_wide_t(const GemvArgs &a, hipStream_t st)
 {
-    if constexpr (KEEP && BITS == 4 && SRC != kWorking && NG == 2 && TR == 32) {
+    if constexpr (KEEP && BITS == 4 && !kRelaid<SRC> && NG == 2 && TR == 32) {
         if (!wide_keeps_words(a.I, a.O, RB * kGemvRows)) return launch_wide_t<BITS, SRC, NG, TR, RB, GATED, false>(a, st);
     }
     if constexpr (DIRECT) {
@@ -779,7 +779,7 @@ static void launch_wide_t(const GemvArgs &a, hipStream_t st)
     }
     kern<<<dim3((unsigned)((a.O + RB * kGemvRows - 1) / (RB * kGemvRows))), dim3(64 * waves), smem, st>>>(a);
 }
-template <int BITS, int SRC, bool GATED>
+template <int BITS, int SRC>
 static void launch_wide_z(int ng, const FwdRoute &way, const GemvArgs &a, hipStream_t st)
 {
     const bool two = way.rows != kGemvRows;
@@ -787,26 +787,24 @@ static void launch_wide_z(int ng, const FwdRoute &way, const GemvArgs &a, hipStr
 #define EQAT_WIDE_NB(NG)                                                                          \
     do {                                                                                          \
         if constexpr (SRC != kWorking) {                                                          \
-            if (way.tokens == 8) { launch_wide_t<BITS, SRC, NG, 8, 1, GATED>(a, st); break; }     \
-            if (way.tokens == 16) { launch_wide_t<BITS, SRC, NG, 16, 1, GATED>(a, st); break; }   \
+            if (way.tokens == 8) { launch_wide_t<BITS, SRC, NG, 8, 1>(a, st); break; }            \
+            if (way.tokens == 16) { launch_wide_t<BITS, SRC, NG, 16, 1>(a, st); break; }          \
         }                                                                                         \
-        if constexpr (!GATED) {                                                                   \
         if (way.tokens == 32 && !two) launch_wide_t<BITS, SRC, NG, 32, 1>(a, st);            \
         else if (way.tokens == 32) launch_wide_t<BITS, SRC, NG, 32, 2>(a, st);                    \
         else if (!two) launch_wide_t<BITS, SRC, NG, 64, 1>(a, st);                                \
         else launch_wide_t<BITS, SRC, NG, 64, 2>(a, st);                                          \
-        }                                                                                         \
     } while (0)
     if (ng == 4) EQAT_WIDE_NB(4); else if (ng == 2) EQAT_WIDE_NB(2); else EQAT_WIDE_NB(1);
 #undef EQAT_WIDE_NB
 }
-template <int SRC, bool GATED = false> static void launch_wide(const Problem &p, const GemvArgs &a, hipStream_t st)
+template <int SRC> static void launch_wide(const Problem &p, const GemvArgs &a, hipStream_t st)
 {
     const int ng = wide_groups(p);
     const FwdRoute way = gemv_route(p, false);
-    if (p.bits == 2) launch_wide_z<2, SRC, GATED>(ng, way, a, st);
-    else if (p.bits == 3) launch_wide_z<3, SRC, GATED>(ng, way, a, st);
-    else launch_wide_z<4, SRC, GATED>(ng, way, a, st);
+    if (p.bits == 2) launch_wide_z<2, SRC>(ng, way, a, st);
+    else if (p.bits == 3) launch_wide_z<3, SRC>(ng, way, a, st);
+    else launch_wide_z<4, SRC>(ng, way, a, st);
 }
 
 static GemvArgs gemv_args(const Problem &p, const void *X, const void *codes, const void *s, void *Y)
@@ -819,7 +817,7 @@ static GemvArgs gemv_args(const Problem &p, const void *X, const void *codes, co
     return a;
 }
 
-// from the packed arrays; GATED: packed zero points, up to 16 tokens (gemv_gated_applies)
+// from the packed arrays; GATED: packed zero points, token rows that fit LDS together
 template <bool GATED>
 static void launch_gemv_packed(const Problem &p, const void *X, const void *Wpacked, const float *s, const void *zpacked,
                                const float *zfloat, void *Y, int kind, hipStream_t st)
@@ -831,12 +829,11 @@ static void launch_gemv_packed(const Problem &p, const void *X, const void *Wpac
     a.w_bytes = (uint32_t)(p.O * p.I * p.bits / 8);
     a.s_bytes = (uint32_t)(p.O * p.G * 4);
     a.z_bytes = zfloat != nullptr ? a.s_bytes : (uint32_t)(p.O * a.z_row_words * 4);
-    const FwdKernel kernel = gemv_route(p, zfloat != nullptr).kernel;
-    if (kernel == FWD_GEMV_WIDE) {
-        if constexpr (GATED) launch_wide<kPackedZ, true>(p, a, st);
-        else if (zfloat != nullptr) launch_wide<kFloatZ>(p, a, st);
-        else launch_wide<kPackedZ>(p, a, st);
-        return;
+    if constexpr (!GATED) {
+        if (gemv_route(p, zfloat != nullptr).kernel == FWD_GEMV_WIDE) {
+            if (zfloat != nullptr) launch_wide<kFloatZ>(p, a, st); else launch_wide<kPackedZ>(p, a, st);
+            return;
+        }
     }
     const int ng = run_groups(p);
     // a wave per run of 1024 inputs when four waves per row block would leave the chip short of waves (see k_gemv_run)

@@ -95,14 +95,17 @@ void launch_gemv(const Problem &p, const void *X, const void *Wpacked, const flo
                  const float *zfloat, void *Y, hipStream_t st);
 
 // ---- gemv_gated.hip (gated feed-forward, p.O = 2 F rows of the stacked projection, H [T, F]) -----
-bool gemv_gated_applies(const Problem &p);
-void launch_gemv_gated(const Problem &p, int kind, const void *X, const void *Wpacked, const float *s, const void *zpacked, void *H, hipStream_t st);
+bool gemv_gated_applies(const Problem &p, bool packed, double mid_us);
+void launch_gemv_gated(const Problem &p, int kind, const void *X, const void *codes, const float *s, const void *zpacked, const float *z, void *H, hipStream_t st);
 
 // what a gated feed-forward leaves: H = act(G) U (forward, or may be NULL), and where dH is given dY = [dH U act'(G) | dH act(G)] (may be NULL)
 struct GatedOut { void *H; const void *dH; void *dY; int kind; };
-void launch_mid_gated(const Problem &p, const GatedOut &out, const void *X, const void *codes, const float *s, const void *zpacked, const float *z, hipStream_t st);      // gemm_mid_gated.hip
-// codes in the working layout and (s, z) pairs
-void launch_tiles_gated(const Problem &p, const GatedOut &out, const void *X, const void *codes, const void *sz, hipStream_t st);                    // gemm_gated.hip
+// gemm_mid_gated.hip, gemm_gated.hip: what a launch takes, as the rule of dispatch estimates it, and with which token tiles; the launches
+double mid_gated_us(const Problem &p, bool packed, int *tokens);
+double tiles_gated_us(const Problem &p, int *tokens);
+void launch_mid_gated(const Problem &p, int tokens, const GatedOut &out, const void *X, const void *codes, const float *s, const void *zpacked, const float *z, hipStream_t st);
+// codes in the working layout or, `dense`, as packed; (s, z) pairs
+void launch_tiles_gated(const Problem &p, int tokens, bool dense, const GatedOut &out, const void *X, const void *codes, const void *sz, hipStream_t st);
 
 // whether mulhi(segment, ceil(2^32 / (g / 32))) is the group of every segment of a row
 inline bool group_by_magic(const Problem &p) { return (p.I / 32) * (p.g / 32) < ((int64_t)1 << 32); }

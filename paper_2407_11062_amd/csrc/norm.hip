@@ -9,6 +9,7 @@
 #include "layer.h"
 
 #include <algorithm>
+#include <atomic>
 
 namespace eqat {
 namespace {
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_fwd(const No
             for (int e = 0; e < 8; ++e) v[e] = s[k].get(e) + add[k].get(e);
             s[k].set(v);
         }
-        if (a.s != nullptr && there && at < a.width) s[k].store(static_cast<T *>(a.s) + row * a.width + at);
+        if (a.s != nullptr && there && at < a.width) s[k].template store<ONCE>(static_cast<T *>(a.s) + row * a.width + at);
         float t = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) t = __builtin_fmaf(s[k].get(e), s[k].get(e), t);
@@ -160,48 +161,56 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_fwd(const No
 }
 
 // Workgroup b takes the rows b, b + grid, ... (of kThreads / LANES each) and keeps its part of dw in registers: part[b][width], summed over b by k_norm_dw.
-template <typename T, int LANES, int NV>
+template <typename T, int LANES, int NV, bool ONCE>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const NormArgs a)
 {
     constexpr int kThreads = LANES > 256 ? LANES : 256, kRows = kThreads / LANES;
+    constexpr bool kHold = LANES < 1024;                      // 16 waves leave no registers for w and dw (in LDS instead), and dS is fetched where it is wanted
     __shared__ float part[2][2][kThreads / 64];
-    extern __shared__ float sums[];                           // [width], where several rows are in the workgroup and dw is wanted
+    extern __shared__ __attribute__((aligned(16))) float sums[];              // [width], where several rows are in the workgroup, or rows are wide, and dw is wanted
     const int lane = threadIdx.x % LANES;
-    float w[NV][8], dw[NV][8];
+    float w[kHold ? NV : 1][8], dw[kHold ? NV : 1][8];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int at = (k * LANES + lane) * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dw[k][e] = w[k][e] = 0.0f;
-        if (at < a.width) load_w(a, at, w[k]);
+        for (int e = 0; e < 8; ++e) {
+            dw[kHold ? k : 0][e] = w[kHold ? k : 0][e] = 0.0f;
+            if (!kHold && a.part != nullptr && at < a.width) sums[at + e] = 0.0f;
+        }
+        if (kHold && at < a.width) load_w(a, at, w[kHold ? k : 0]);
     }
     const int64_t n = (a.rows + kRows - 1) / kRows;
     int turn = 0;
     for (int64_t b = blockIdx.x; b < n; b += gridDim.x, turn ^= 1) {
         const int64_t row = b * kRows + threadIdx.x / LANES;
         const bool there = row < a.rows;
-        Eight<T> s[NV], dy[NV], ds[NV];
+        Eight<T> s[NV], dy[NV], ds[kHold ? NV : 1];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = (k * LANES + lane) * 8;
-            s[k].zero(); dy[k].zero(); ds[k].zero();
+            s[k].zero(); dy[k].zero(); ds[kHold ? k : 0].zero();
             if (there && at < a.width) {
-                s[k].load(static_cast<const T *>(a.x) + row * a.width + at);
-                dy[k].load(static_cast<const T *>(a.dy) + row * a.width + at);
-                if (a.r != nullptr) ds[k].load(static_cast<const T *>(a.r) + row * a.width + at);
+                s[k].template load<ONCE>(static_cast<const T *>(a.x) + row * a.width + at);
+                dy[k].template load<ONCE>(static_cast<const T *>(a.dy) + row * a.width + at);
+                if (kHold && a.r != nullptr) ds[kHold ? k : 0].template load<ONCE>(static_cast<const T *>(a.r) + row * a.width + at);
             }
         }
         float ss = 0.0f, es = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * 8;
+            if (!kHold && at < a.width) load_w(a, at, w[0]);
+            const float (&wk)[8] = w[kHold ? k : 0];
             float t = 0.0f, u = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float x = s[k].get(e);
                 t = __builtin_fmaf(x, x, t);
-                u = __builtin_fmaf(dy[k].get(e) * w[k][e], x, u);
+                u = __builtin_fmaf(dy[k].get(e) * wk[e], x, u);
             }
             ss += t; es += u;
+            if (!kHold) __builtin_amdgcn_sched_barrier(0);    // one vector's weights at a time
         }
         ss = lanes_all<LANES>(ss, sum_of);
         es = lanes_all<LANES>(es, sum_of);
@@ -216,18 +225,35 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const No
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = (k * LANES + lane) * 8;
+            if (!kHold && there && at < a.width) {
+                load_w(a, at, w[0]);
+                if (a.r != nullptr) ds[0].load(static_cast<const T *>(a.r) + row * a.width + at);
+            }
+            const float (&wk)[8] = w[kHold ? k : 0];
+            const Eight<T> &dsk = ds[kHold ? k : 0];
             float d[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float x = s[k].get(e), g = dy[k].get(e);
-                d[e] = __builtin_fmaf(rstd, __builtin_fmaf(-x, c, g * w[k][e]), ds[k].get(e));
-                dw[k][e] = __builtin_fmaf(g * rstd, x, dw[k][e]);
+                d[e] = __builtin_fmaf(rstd, __builtin_fmaf(-x, c, g * wk[e]), dsk.get(e));
+                if (kHold) dw[kHold ? k : 0][e] = __builtin_fmaf(g * rstd, x, dw[kHold ? k : 0][e]);
+            }
+            if (!kHold && a.part != nullptr && at < a.width) {          // the lane's own
+                floatx4 *const mine = reinterpret_cast<floatx4 *>(sums + at);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    floatx4 v = mine[h];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(dy[k].get(4 * h + e) * rstd, s[k].get(4 * h + e), v[e]);
+                    mine[h] = v;
+                }
             }
             if (a.y != nullptr && there && at < a.width) {
                 Eight<T> o;
                 o.set(d);
                 o.store(static_cast<T *>(a.y) + row * a.width + at);
             }
+            if (!kHold) __builtin_amdgcn_sched_barrier(0);
         }
     }
     if (a.part == nullptr) return;
@@ -240,7 +266,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const No
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int at = (k * LANES + lane) * 8 + e;
-                        if (at < a.width) sums[at] = v == 0 ? dw[k][e] : sums[at] + dw[k][e];
+                        if (at < a.width) sums[at] = v == 0 ? dw[kHold ? k : 0][e] : sums[at] + dw[kHold ? k : 0][e];
                     }
             }
             __syncthreads();
@@ -252,31 +278,36 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const No
             const int at = (k * LANES + lane) * 8;
             if (at < a.width) {
                 Eight<float> o;
-                o.set(dw[k]);
+                if constexpr (kHold) o.set(dw[k]); else o.load(sums + at);
                 o.store(to + at);
             }
         }
     }
 }
 
-// dw[i] = the sum over b of part[b][i]: 16 columns of four to a workgroup, 16 threads a column, each every 16th part, then theirs in order
+// dw[i] = the sum over b of part[b][i]: 32 neighbouring columns, four to a thread, to a workgroup, 32 threads a column, each every 32nd part, then theirs in order
+constexpr int kDwRows = 32, kDwColumns = 8;
 __global__ __launch_bounds__(256) void k_norm_dw(const float *__restrict__ part, float *__restrict__ dw, int parts, int width)
 {
-    __shared__ floatx4 sums[256];
-    const int c = threadIdx.x & 15, k = threadIdx.x >> 4, at = ((int)blockIdx.x * 16 + c) * 4;
+    __shared__ floatx4 sums[kDwRows * kDwColumns];
+    const int c = threadIdx.x % kDwColumns, k = threadIdx.x / kDwColumns, at = ((int)blockIdx.x * kDwColumns + c) * 4;
     floatx4 s = {0.f, 0.f, 0.f, 0.f};
     if (at < width) {
-#pragma unroll 4
-        for (int b = k; b < parts; b += 16) s += *reinterpret_cast<const floatx4 *>(part + (int64_t)b * width + at);
+#pragma unroll 8
+        for (int b = k; b < parts; b += kDwRows) s += *reinterpret_cast<const floatx4 *>(part + (int64_t)b * width + at);
     }
     sums[threadIdx.x] = s;
     __syncthreads();
     if (k == 0 && at < width) {
 #pragma unroll
-        for (int v = 1; v < 16; ++v) s += sums[v * 16 + c];
+        for (int v = 1; v < kDwRows; ++v) s += sums[v * kDwColumns + c];
         *reinterpret_cast<floatx4 *>(dw + at) = s;
     }
 }
+
+// From this many bytes of rows on what is read goes past the caches, and S with it, which is next wanted a layer on; Y and dX, which the next call reads, do not.  Graph replays over three
+// states, us, through the caches / past them: norm 67 MB 13.4 / 13.8, 134 MB 29.5 / 25.6, 269 MB 58 / 51, 537 MB 103 / 96; its gradients 67 MB 18.7 / 20.7, 134 MB 34.0 / 30.0, 269 MB 57 / 50.
+constexpr int64_t kOnceBytes = (int64_t)96 << 20;
 
 constexpr int kNormParts = 512;         // workgroups of a backward pass at most
 
@@ -313,11 +344,16 @@ void launch_norm_fwd(const NormFwd &n, hipStream_t st)
     NormArgs a{};
     a.rows = n.rows; a.x = n.x; a.r = n.r; a.w = n.w; a.s = n.s; a.y = n.y; a.codes = n.codes; a.scales = n.scales;
     a.width = n.width; a.group = n.group; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
+    const int64_t per = n.rows * n.width * (n.act_bf16 ? 2 : 4);
+    const bool once = per * (1 + (n.r != nullptr) + (n.s != nullptr) + (n.y != nullptr)) > kOnceBytes;
     by_width(n.width, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
         const unsigned blocks = (unsigned)((n.rows + kThreads / L - 1) / (kThreads / L));
-        if (n.act_bf16) k_norm_fwd<bf16_t, L, N, false><<<blocks, kThreads, 0, st>>>(a);
-        else k_norm_fwd<float, L, N, false><<<blocks, kThreads, 0, st>>>(a);
+        if (n.act_bf16) {
+            if (once) k_norm_fwd<bf16_t, L, N, true><<<blocks, kThreads, 0, st>>>(a); else k_norm_fwd<bf16_t, L, N, false><<<blocks, kThreads, 0, st>>>(a);
+        } else {
+            if (once) k_norm_fwd<float, L, N, true><<<blocks, kThreads, 0, st>>>(a); else k_norm_fwd<float, L, N, false><<<blocks, kThreads, 0, st>>>(a);
+        }
     });
 }
 
@@ -330,11 +366,25 @@ void launch_norm_bwd(const NormBwd &n, void *ws, hipStream_t st)
     a.width = n.width; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
     if (blocks > 0) by_width(n.width, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
-        const size_t lds = L < 256 && n.dw != nullptr ? (size_t)n.width * sizeof(float) : 0;
-        if (n.act_bf16) k_norm_bwd<bf16_t, L, N><<<blocks, kThreads, lds, st>>>(a);
-        else k_norm_bwd<float, L, N><<<blocks, kThreads, lds, st>>>(a);
+        const size_t lds = (L < 256 || L == 1024) && n.dw != nullptr ? (size_t)n.width * sizeof(float) : 0;
+        if constexpr (L == 1024) {      // more than the default limit: once per device
+            static std::atomic<uint64_t> allowed{0};
+            int dev = 0;
+            if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev > 63) dev = 0;
+            if (!((allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {
+                (void)hipFuncSetAttribute((const void *)k_norm_bwd<bf16_t, L, N, false>, hipFuncAttributeMaxDynamicSharedMemorySize, kNormMostWidth * (int)sizeof(float));
+                (void)hipFuncSetAttribute((const void *)k_norm_bwd<float, L, N, false>, hipFuncAttributeMaxDynamicSharedMemorySize, kNormMostWidth * (int)sizeof(float));
+                allowed.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
+            }
+        }
+        const bool once = L < 1024 && n.rows * n.width * (n.act_bf16 ? 2 : 4) * (2 + (n.ds != nullptr) + (n.dx != nullptr)) > kOnceBytes;
+        if (n.act_bf16) {
+            if (once) k_norm_bwd<bf16_t, L, N, L < 1024><<<blocks, kThreads, lds, st>>>(a); else k_norm_bwd<bf16_t, L, N, false><<<blocks, kThreads, lds, st>>>(a);
+        } else {
+            if (once) k_norm_bwd<float, L, N, L < 1024><<<blocks, kThreads, lds, st>>>(a); else k_norm_bwd<float, L, N, false><<<blocks, kThreads, lds, st>>>(a);
+        }
     });
-    if (n.dw != nullptr && blocks != 1) k_norm_dw<<<(n.width / 4 + 15) / 16, 256, 0, st>>>(a.part, n.dw, blocks, n.width);
+    if (n.dw != nullptr && blocks != 1) k_norm_dw<<<(n.width / 4 + kDwColumns - 1) / kDwColumns, 256, 0, st>>>(a.part, n.dw, blocks, n.width);
 }
 
 }  // namespace eqat

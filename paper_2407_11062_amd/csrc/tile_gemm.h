@@ -6,9 +6,12 @@
 // The paddings make both read patterns bank-conflict free.
 #pragma once
 #include "common.h"
+#include "dense_codes.h"
 #include "gate.h"
 #include "gemm_tiles.h"
 #include "kernels.h"
+
+#include <type_traits>
 
 namespace eqat {
 
@@ -262,7 +265,8 @@ enum QMode { kWhole, kCut, kRagged };
 // a wave's columns are a gate's and their partners, in the same registers of the same lanes.  kGateFwd: C [M, F] = H = act(G) U.  kGateBwd: dH [M, F] comes through the patch of
 // LDS that the results leave through, and with it leave H and dY = [dH U act'(G) | dH act(G)] (an absent one: a buffer of no bytes, whose stores are dropped).
 enum GateMode { kNoGate, kGateFwd, kGateBwd };
-template <int BITS, bool BT, int MODE, int BM, int BN, int BK, int WGM, int WGN, int GATE = kNoGate>
+// DENSE: the codes as packed, not in the working layout.
+template <int BITS, bool BT, int MODE, int BM, int BN, int BK, int WGM, int WGN, int GATE = kNoGate, bool DENSE = false>
 __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, const int grid)
 {
     constexpr bool CUT = MODE == kCut;
@@ -312,9 +316,10 @@ __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, c
     const __amdgpu_buffer_rsrc_t rCst = make_rsrc(a.C, a.c_bytes);
     const __amdgpu_buffer_rsrc_t rC = make_rsrc(a.codes, a.codes_bytes);
     const __amdgpu_buffer_rsrc_t rS = make_rsrc(a.sz, a.sz_bytes);
-    const uint32_t code_row_bytes = (uint32_t)a.I / 32u * (4u * WorkCodes<BITS>::kWords);
+    constexpr uint32_t kSegBytes = 4u * (DENSE ? BITS : WorkCodes<BITS>::kWords);
+    const uint32_t code_row_bytes = (uint32_t)a.I / 32u * kSegBytes;
 
-    WorkCodes<BITS> stC[2][B_SEGS];
+    std::conditional_t<DENSE, CodeWords<BITS>, WorkCodes<BITS>> stC[2][B_SEGS];
     floatx2 stS[2][B_SEGS];
     WhatTable<BITS> tabs[2][B_SEGS];
 
@@ -403,7 +408,9 @@ __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, c
             if constexpr (GATE != kNoGate) { const int v = sidx / (BK / 32); wrow = (c_n0 >> 1) + ((v >> 6) << 5) + (v & 31) + (v & 32 ? a.N >> 1 : 0); }
             if (BT) { wrow = c_k0 + sidx / (BN / 32); wcol = c_n0 + (sidx % (BN / 32)) * 32; }
             const bool ok = wcol < a.I;
-            stC[S][it] = load_work_codes<BITS>(rC, (uint32_t)wrow * code_row_bytes + (uint32_t)(wcol >> 5) * (4u * WorkCodes<BITS>::kWords));
+            const uint32_t code_at = (uint32_t)wrow * code_row_bytes + (uint32_t)(wcol >> 5) * kSegBytes;
+            if constexpr (DENSE) stC[S][it] = load_code_words<BITS>(rC, code_at);
+            else stC[S][it] = load_work_codes<BITS>(rC, code_at);
             const intx2 sv = buf_load8(rS, ok ? ((uint32_t)wrow * (uint32_t)a.G + (uint32_t)grp[it]) * 8u : kOobOffset);
             stS[S][it][0] = __int_as_float(sv[0]);
             stS[S][it][1] = __int_as_float(sv[1]);
@@ -425,6 +432,10 @@ __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, c
         if (a_left == 0) a_enter_tile();
         if (c_left == 0) c_enter_tile();
     };
+    [[maybe_unused]] auto eight = [](const WhatTable<BITS> &tab, const auto &c, auto q) -> bf16x8 {
+        if constexpr (DENSE) return unslot_of<BITS>(eight_of<BITS, decltype(q)::value>(tab, c));
+        else return tab.template eight<decltype(q)::value>(c);
+    };
     // piece P of KK: every KK-th 16-byte store of the staged weight tile
     auto commit_piece = [&](auto set, auto piece, int buf) {
         constexpr int S = decltype(set)::value, P = decltype(piece)::value;
@@ -439,10 +450,10 @@ __device__ __forceinline__ void gemm_q_body(const GemmQArgs &a, const int bid, c
             if constexpr (P == 0) tab.build(stS[S][it][0], stS[S][it][1]);     // piece 0 of a tile always runs first
             bf16x8 *dst = reinterpret_cast<bf16x8 *>(dB + r * LDB + c);
             const int sw = BT ? km_chunk_swz(r, c >> 5) : 0;                    // KM tile: see km_chunk_swz
-            if ((it * 4 + 0) % KK == P) dst[0 ^ sw] = tab.template eight<0>(stC[S][it]);
-            if ((it * 4 + 1) % KK == P) dst[1 ^ sw] = tab.template eight<1>(stC[S][it]);
-            if ((it * 4 + 2) % KK == P) dst[2 ^ sw] = tab.template eight<2>(stC[S][it]);
-            if ((it * 4 + 3) % KK == P) dst[3 ^ sw] = tab.template eight<3>(stC[S][it]);
+            if ((it * 4 + 0) % KK == P) dst[0 ^ sw] = eight(tab, stC[S][it], IC<0>{});
+            if ((it * 4 + 1) % KK == P) dst[1 ^ sw] = eight(tab, stC[S][it], IC<1>{});
+            if ((it * 4 + 2) % KK == P) dst[2 ^ sw] = eight(tab, stC[S][it], IC<2>{});
+            if ((it * 4 + 3) % KK == P) dst[3 ^ sw] = eight(tab, stC[S][it], IC<3>{});
         }
     };
 

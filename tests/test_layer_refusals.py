@@ -122,12 +122,12 @@ def gated_calls(d, kind=0, X=P, layer=P, s=P, z=P, dH=P, dY=P, H=P, ws=P, n=1 <<
     (dict(tokens=1 << 21, out_features=1024), SHAPE), (dict(in_features=1 << 22, group=-1, out_features=16), SHAPE)])
 def test_gated_descriptor(kw, status):
     assert gated_calls(gated(**kw)) == [status] * 4
-    assert L().eqat_gated_workspace_bytes(ctypes.byref(gated(**kw)), 0) == 0 and L().eqat_gated_workspace_bytes(ctypes.byref(gated(**kw)), 1) == 0
+    assert L().eqat_gated_workspace_bytes(ctypes.byref(gated(**kw))) == 0
 
 
 def test_gated_arguments():
     d = gated(tokens=100)
-    assert gated_calls(None) == [NULL] * 4 and L().eqat_gated_workspace_bytes(None, 0) == 0
+    assert gated_calls(None) == [NULL] * 4 and L().eqat_gated_workspace_bytes(None) == 0
     assert gated_calls(d, kind=2) == [HYPER] * 4 and gated_calls(d, kind=-1) == [HYPER] * 4
     for name in ("X", "layer", "s"):
         assert gated_calls(d, **{name: None}) == [NULL] * 4, name
@@ -137,18 +137,16 @@ def test_gated_arguments():
     assert [gated_calls(d, H=None)[i] for i in (0, 2)] == [NULL] * 2 and [gated_calls(d, dH=None)[i] for i in (1, 3)] == [NULL] * 2
     assert [gated_calls(d, H=None, dY=None, dH=None)[i] for i in (1, 3)] == [OK] * 2                                      # nothing wanted
     for prepared in (0, 1):
-        need = L().eqat_gated_workspace_bytes(ctypes.byref(d), prepared)
+        need = L().eqat_gated_workspace_bytes(ctypes.byref(d))
         assert gated_calls(d, ws=None)[2 * prepared] == WORKSPACE and gated_calls(d, n=need - 1)[2 * prepared] == WORKSPACE and gated_calls(d, ws=P + 16)[2 * prepared] == ALIGN
-        assert L().eqat_gated_workspace_bytes(ctypes.byref(gated(tokens=1)), prepared) == 256                             # a few tokens need none
+        assert L().eqat_gated_workspace_bytes(ctypes.byref(gated(tokens=1))) == 256                             # a few tokens need none
     assert gated_calls(gated(tokens=0), X=None, H=None, dH=None) == [OK] * 4
 
 
 def test_gated_workspace_of_more_tokens_serves_fewer():
     for act in (eq.F32, eq.BF16):
-        for prepared in (0, 1):
-            sizes = [L().eqat_gated_workspace_bytes(ctypes.byref(gated(tokens=t, act_dtype=act, in_features=1024, out_features=5504)), prepared)
-                     for t in (1, 2, 16, 17, 64, 65, 100, 333, 1000, 4096, 8192)]
-            assert sizes == sorted(sizes)
+        sizes = [L().eqat_gated_workspace_bytes(ctypes.byref(gated(tokens=t, act_dtype=act, in_features=1024, out_features=5504))) for t in (1, 2, 16, 17, 64, 65, 100, 333, 1000, 4096, 8192)]
+        assert sizes == sorted(sizes)
 
 
 @pytest.mark.parametrize("back", (False, True))
