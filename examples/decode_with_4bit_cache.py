@@ -2,8 +2,9 @@
 
     python examples/decode_with_4bit_cache.py [--layers 2] [--tokens 32]
 
-Every linear is a packed layer (eqat_qlinear_fwd), q, k and v stacked in one; keys and values are slices of its output and go into the cache as they lie
-(eqat_kv_write), attention reads the cache (eqat_kv_attention).  The decoding step is captured in a graph once and replayed: lengths, page table and tokens live on
+Every linear is a packed layer (eqat_qlinear_fwd), q, k and v stacked in one; queries, keys and values are slices of its output, and one call turns queries and keys by their
+positions and writes keys and values into the cache (eqat_kv_rotary_write), attention reads the cache (eqat_kv_attention).  The residual's addition and the norm behind it are one
+call (eqat_norm_fwd), and so are the feed-forward's two projections with their gate (eqat_gated_fwd).  The decoding step is captured in a graph once and replayed: lengths, page table and tokens live on
 the device.  Weights are random; --check compares the last step's attention with one over the values that the cache stands for (eqat_kv_read).
 """
 import argparse
@@ -29,16 +30,7 @@ class Linear:
         return eq.eqat_qlinear_fwd(x, self.Wq, self.s, self.zq, self.bits, self.group)
 
 
-def rotated(x, pos):
-    """rotary embedding: pairs (i, i + dim / 2) of every head turned by pos / 10000^(2 i / dim)"""
-    half = x.shape[-1] // 2
-    angle = pos[:, None, None].float() * torch.exp(torch.arange(half, device=x.device) * (-2 * math.log(10000.0) / x.shape[-1]))
-    a, b = x[..., :half].float(), x[..., half:].float()
-    return torch.cat((a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()), -1).to(x.dtype)
-
-
-def normed(x):
-    return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-5)).to(x.dtype)
+EPS = 1e-5
 
 
 class Layer:
@@ -49,17 +41,18 @@ class Layer:
         self.o = Linear(gen, h, h, args.bits, args.group)
         self.up, self.down = Linear(gen, 2 * args.inter, h, args.bits, args.group), Linear(gen, h, args.inter, args.bits, args.group)
         self.cache = eq.KvCache(self.kv, d, args.kv_group, args.page, pages)
+        self.rot = eq.Rotary(eq.rotary_frequencies(d, stretch=args.stretch).cuda(), d)
+        self.w1, self.w2 = (torch.empty(h, device="cuda").normal_(1.0, 0.1, generator=gen) for _ in range(2))
 
-    def __call__(self, x, batch, pos, ws):
-        T, q_rows, kv_rows = x.shape[0], self.heads * self.d, self.kv * self.d
-        y = self.qkv(normed(x))
-        q = rotated(y[:, :q_rows].view(T, self.heads, self.d), pos)
-        k = rotated(y[:, q_rows:q_rows + kv_rows].view(T, self.kv, self.d), pos)
-        eq.eqat_kv_write(self.cache, batch, k, y[:, q_rows + kv_rows:].view(T, self.kv, self.d))
-        self.q, self.a = q, eq.eqat_kv_attention(self.cache, batch, q, ws=ws)
-        x = x + self.o(self.a.view(T, q_rows))
-        gate, up = self.up(normed(x)).chunk(2, -1)
-        return x + self.down((torch.nn.functional.silu(gate) * up).contiguous())
+    def __call__(self, x, residual, batch, ws):
+        """x, what the last layer's feed-forward left, and the residual that it goes on top of -> the same for the next layer"""
+        T, heads, kv = x.shape[0], self.heads, self.kv
+        n = eq.eqat_norm_fwd(x, self.w1, EPS, R=residual, want=("S", "Y"))
+        y = self.qkv(n["Y"]).view(T, heads + 2 * kv, self.d)
+        self.q = eq.eqat_kv_rotary_write(self.cache, batch, self.rot, y[:, :heads], y[:, heads:heads + kv], y[:, heads + kv:])
+        self.a = eq.eqat_kv_attention(self.cache, batch, self.q, ws=ws)
+        n = eq.eqat_norm_fwd(self.o(self.a.view(T, heads * self.d)), self.w2, EPS, R=n["S"], want=("S", "Y"))
+        return self.down(eq.eqat_gated_fwd(n["Y"], self.up.Wq, self.up.s, self.up.zq, self.up.bits, self.up.group)), n["S"]
 
 
 def run(args):
@@ -76,12 +69,18 @@ def run(args):
     # the prompts, all sequences in one call
     starts = [sum(args.prompts[:b]) for b in range(B + 1)]
     first = eq.KvBatch(table, i32(args.prompts), i32(starts), tokens=starts[-1], max_new=max(args.prompts), max_len=max(args.prompts))
-    pos = torch.cat([torch.arange(n) for n in args.prompts]).int().cuda()
     ws = eq.kv_workspace(layers[0].cache, first, layers[0].heads)
-    x = embed[torch.randint(0, args.vocab, (starts[-1],), device="cuda", generator=gen)]
-    for layer in layers:
-        x = layer(x, first, pos, ws)
-    tokens = head(normed(x)[[s - 1 for s in starts[1:]]].contiguous()).argmax(-1)
+    w = torch.empty(args.hidden, device="cuda").normal_(1.0, 0.1, generator=gen)
+
+    def through(tokens, batch, rows=None):
+        x, residual = embed[tokens], None
+        for layer in layers:
+            x, residual = layer(x, residual, batch, ws)
+        if rows is not None:
+            x, residual = x[rows], residual[rows]
+        return head(eq.eqat_norm_fwd(x, w, EPS, R=residual, want=("Y",))["Y"]).argmax(-1)
+
+    tokens = through(torch.randint(0, args.vocab, (starts[-1],), device="cuda", generator=gen), first, [s - 1 for s in starts[1:]])
 
     # one token a sequence from here on
     lens = i32(args.prompts)
@@ -90,10 +89,7 @@ def run(args):
 
     def step():
         lens.add_(1)
-        x = embed[tokens]
-        for layer in layers:
-            x = layer(x, batch, lens - 1, ws)
-        tokens.copy_(head(normed(x)).argmax(-1))
+        tokens.copy_(through(tokens, batch))
 
     step()                                               # outside the capture once: first uses
     out[0] = tokens
@@ -135,6 +131,7 @@ def parser():
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     for name, value in dict(layers=2, hidden=4096, inter=11008, head_dim=128, kv_heads=8, vocab=32000, bits=2, group=64, kv_group=64, page=64, tokens=32).items():
         p.add_argument("--" + name.replace("_", "-"), type=int, default=value)
+    p.add_argument("--stretch", type=float, default=1.0, help="rotary positions for contexts that many times longer")
     p.add_argument("--prompts", type=int, nargs="+", default=[333, 1000, 17, 515])
     p.add_argument("--check", action="store_true")
     return p

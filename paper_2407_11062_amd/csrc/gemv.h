@@ -230,6 +230,7 @@ __global__ __launch_bounds__(64 * (MW ? kGemvMaxWaves : kGemvWaves)) void k_gemv
     const __amdgpu_buffer_rsrc_t rS = make_rsrc(a.s, a.s_bytes);
     const __amdgpu_buffer_rsrc_t rZ = make_rsrc(FLOATZ ? (const void *)a.zf : (const void *)a.zp, a.z_bytes);
     constexpr int CW = 2 * BITS;                      // 16-byte loads per run of 8 segments
+    constexpr bool kAhead = GATED && BITS == 4;
     constexpr int SW = NG >= 4 ? NG / 4 : 1;          // 16-byte loads of step sizes (shorter loads for NG = 2, 1)
 
     auto load_run = [&](int sc, uintx4 (&cq)[CW], floatx4 (&sq)[SW], floatx4 (&zq)[SW], uint32_t (&zw)[2]) {
@@ -269,19 +270,36 @@ __global__ __launch_bounds__(64 * (MW ? kGemvMaxWaves : kGemvWaves)) void k_gemv
     };
 
     const int n_runs = (n_segs + 31) / 32;            // trips of one wave cover 32 segments (4 lane groups x 8)
+    struct First { uintx4 cq[CW]; floatx4 sq[SW], zq[SW]; uint32_t zw[2]; };
+    [[maybe_unused]] First first;                     // kAhead: of the wave
 
     // ---- stage the token rows in slot order (one 32-input segment per thread and trip) ---------------------
-    for (int e = tid; e < a.T * n_segs; e += 64 * n_waves) {
+    auto stage = [&](int e, auto between) {
         const int n = e / n_segs, seg = e - n * n_segs;
         const bf16_t *src = a.X + (size_t)n * a.I + seg * 32;
         bf16_t *dst = xs + (size_t)n * a.I + seg * 32;
         bf16x8 v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const bf16x8 *>(src + 8 * q);
+        between();
 #pragma unroll
         for (int c = 0; c < 32; ++c) dst[run_code_slot<BITS, FORM>(c)] = v[c / 8][c % 8];
+    };
+    if constexpr (kAhead) {
+        // 4-bit codes of a gated projection: a wave's first run is on its way behind the first tokens (one token, 4096 -> 2 x 11008 20.5 -> 15.4 us; 2 and 3 bit lose 0.7 to 1.8 us
+        // that way: their conversions then wait for all of it)
+        const int n_all = a.T * n_segs;
+        stage(min(tid, n_all - 1), [&]() { load_run(wave, first.cq, first.sq, first.zq, first.zw); });          // (the last segment several times: the same values)
+        for (int e = tid + 64 * n_waves; e < n_all; e += 64 * n_waves) stage(e, []() {});
+        // a barrier that leaves loads on their way: only what lies in LDS has to be there
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    } else {
+        for (int e = tid; e < a.T * n_segs; e += 64 * n_waves) stage(e, []() {});
+        __syncthreads();
     }
-    __syncthreads();
 
     const bf16_t *xlane = xs + (size_t)((lane & 15) < a.T ? (lane & 15) : 0) * a.I;
     floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -290,7 +308,16 @@ __global__ __launch_bounds__(64 * (MW ? kGemvMaxWaves : kGemvWaves)) void k_gemv
         uintx4 cq[CW];
         floatx4 sq[SW], zq[SW];
         uint32_t zw[2] = {0u, 0u};
-        load_run(sc, cq, sq, zq, zw);
+        if constexpr (kAhead) {
+            if (sc != wave) load_run(sc, first.cq, first.sq, first.zq, first.zw);
+#pragma unroll
+            for (int q = 0; q < CW; ++q) cq[q] = first.cq[q];
+#pragma unroll
+            for (int q = 0; q < SW; ++q) sq[q] = first.sq[q];
+            zw[0] = first.zw[0]; zw[1] = first.zw[1];
+        } else {
+            load_run(sc, cq, sq, zq, zw);
+        }
         WhatTable<BITS> tab;
         const uint32_t j0 = NG > 1 ? (uint32_t)(seg0 >> 3) * NG : (a.spg_magic ? __umulhi((uint32_t)seg0, a.spg_magic) : (uint32_t)seg0);
         const uint64_t zbits = ((uint64_t)zw[0] | ((uint64_t)zw[1] << 32)) >> ((j0 * BITS) & 31u);

@@ -21,8 +21,14 @@ template <int SRC> void wide(const Problem &p, const GemvArgs &a, hipStream_t st
     if (p.bits == 2) wide_ng<2, SRC>(ng, a, st); else if (p.bits == 3) wide_ng<3, SRC>(ng, a, st); else wide_ng<4, SRC>(ng, a, st);
 }
 
-// the kernel that stages all token rows, from the packed arrays, where it is not the slower one
-bool staged(const Problem &p, bool packed) { return packed && gemv_tokens_fit(p) && !wide_is_faster(p); }
+// The kernel that stages all token rows, from the packed arrays.  Where the wide one takes the groups it is the faster one from four tokens on, and with 4-bit codes of up to 2^25 weights for any
+// number.  us, staged / wide: 4096 -> 2 x 11008, 2 bit, 2 tokens 11.4 / 14.5, 4 14.9 / 14.5, 6 17.5 / 14.4; 3 bit, 5120 -> 2 x 13824, 2 tokens 19.6 / 23.7, 4 24.1 / 23.8, 6 34 / 24; 4 bit, 4096 -> 2 x 11008, one 15.4 / 17.2,
+// 2048 -> 2 x 5504 7.5 / 6.6.
+bool staged(const Problem &p, bool packed)
+{
+    if (!packed || !gemv_tokens_fit(p)) return false;
+    return wide_groups(p) == 0 || (p.T <= 3 && !wide_is_faster(p) && (p.bits != 4 || p.O * p.I > (int64_t)1 << 25));
+}
 
 }  // namespace
 
