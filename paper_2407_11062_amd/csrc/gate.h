@@ -37,14 +37,25 @@ template <int KIND> __device__ __forceinline__ void gate_both(float x, float &a,
 }
 
 
-// of one element: act(g) u, and with the gradient d of it d u act'(g), d act(g)
-__device__ __forceinline__ float gated_by(int kind, float g, float u) { return (kind == EQAT_GATE_SILU ? gate_act<EQAT_GATE_SILU>(g) : gate_act<EQAT_GATE_GELU>(g)) * u; }
+// What the kernels with bf16 results take, whose epilogue is arithmetic and little else: exp(-t) without the rest of its product (off by |t| 2^-23 of itself, where a result keeps 2^-9), q = 1 - p, no
+// clamp (exp(-t) = inf leaves p = 0).
+__device__ __forceinline__ float gate_p_near(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.44269504088896340736f)); }
+template <int KIND> __device__ __forceinline__ float gated_near(float g, float u) { return g * gate_p_near(gate_t<KIND>(g)) * u; }
 struct Gated { float h, dg, du; };
+template <int KIND> __device__ __forceinline__ Gated gated_both_near(float g, float u, float d)
+{
+    constexpr float k2 = 1.5957691216057307f;
+    const float p = gate_p_near(gate_t<KIND>(g)), act = g * p, du = d * act;
+    float slope;
+    if constexpr (KIND == EQAT_GATE_SILU) slope = __builtin_fmaf(act, 1.0f - p, p);
+    else slope = __builtin_fmaf(act * (1.0f - p), k2 * __builtin_fmaf(0.134145f * g, g, 1.0f), p);
+    return Gated{act * u, d * u * slope, du};
+}
+// of one element: act(g) u, and with the gradient d of it d u act'(g), d act(g)
+__device__ __forceinline__ float gated_by(int kind, float g, float u) { return kind == EQAT_GATE_SILU ? gated_near<EQAT_GATE_SILU>(g, u) : gated_near<EQAT_GATE_GELU>(g, u); }
 __device__ __forceinline__ Gated gated_both(int kind, float g, float u, float d)
 {
-    float act, slope;
-    if (kind == EQAT_GATE_SILU) gate_both<EQAT_GATE_SILU>(g, act, slope); else gate_both<EQAT_GATE_GELU>(g, act, slope);
-    return Gated{act * u, d * u * slope, d * act};
+    return kind == EQAT_GATE_SILU ? gated_both_near<EQAT_GATE_SILU>(g, u, d) : gated_both_near<EQAT_GATE_GELU>(g, u, d);
 }
 
 }  // namespace eqat

@@ -82,10 +82,11 @@ def act(kind, g):
     return g * p, p + 2 * g * p * (1 - p) * k * (1 + 3 * 0.044715 * g * g)
 
 
-def gate(kind, g, u, dH, dtype, dg=0.0, du=0.0):
+def gate(kind, g, u, dH, dtype, dg=0.0, du=0.0, near=False):
     """{name: (value, bound)} of H and dY from G and U that are good to dg and du (absolute).  act(x) = x p(t), act'(x) = p + x p q t', q = 1 - p; the derivative of either activation
     is below 1.13, its own derivative below 1.1 (silu 0.5).  p and q are good to eight roundings each; gelu's t = 2 k x (1 + 0.044715 x^2) has four roundings of its own, each of which moves p
     by q |t| of them and q by p |t|.  t', the products and the sum behind act': six more of x p q t'.
+    `near`, as the kernels with bf16 results have it: exp(-t) by a product that is rounded once (t and log2 e: 2 |t| roundings, of which p has q's share), and q = 1 - p, off by what p is.
     Where 1 + exp(-t) is 2^126 or more, p <= 2^-126 is no normal binary32 number and may be 0: act is off by |x| 2^-126 there, and act' by 2^-126 (1 + |x| t'), t' <= 1 for silu and below
     2 x^2 for the |x| > 5 where gelu's p is so small."""
     a, slope = act(kind, g)
@@ -96,7 +97,12 @@ def gate(kind, g, u, dH, dtype, dg=0.0, du=0.0):
     p, q, far = torch.sigmoid(t), torch.sigmoid(-t), 4 * t.abs() if kind == 1 else 0.0
     gone = 2.0 ** -126 * g.abs()
     da = 1.13 * dg + (8 + far * q) * F32 * a.abs() + gone
-    ds = 1.1 * dg + F32 * (p * (8 + far * q) + g.abs() * p * q * t1 * (8 + 8 + 6 + far)) + 2.0 ** -126 + gone * (1 if kind == 0 else 2 * g.square() + 1)
+    rp, rq = 8 + far * q, 8 + far * p                        # roundings of p and q
+    if near:
+        rp = rp + 2 * t.abs() * q
+        rq = rp * p / q.clamp_min(2.0 ** -60) + 1
+        da = da + 2 * t.abs() * q * F32 * a.abs()
+    ds = 1.1 * dg + F32 * (p * rp + g.abs() * p * q * t1 * (rp + rq + 6)) + 2.0 ** -126 + gone * (1 if kind == 0 else 2 * g.square() + 1)
     out = {"H": (a * u, h * (a * u).abs() + da * u.abs() + a.abs() * du + da * du + 2 * F32 * (a * u).abs())}
     if dH is not None:
         d = dH.double()

@@ -34,7 +34,7 @@ class Layer:
         d = loose * (self.I + 3) * ref.F32
         F = self.F
         for b in back:
-            want = ref.gate(kind, y[:, :F], y[:, F:], dH if b else None, dtype, d[:, :F], d[:, F:])
+            want = ref.gate(kind, y[:, :F], y[:, F:], dH if b else None, dtype, d[:, :F], d[:, F:], near=dtype == torch.bfloat16)
             for p in prepared:
                 if p:
                     layer = self.prepared(dtype)
