@@ -482,11 +482,11 @@ eqat_status eqat_kv_attention(const eqat_kv_desc *d, const eqat_kv_batch *b, con
  *   Backward, of S (what the forward left in S, or its X without R), the gradients dY of Y and dS of S (along the residual; NULL: none):
  *                   dX = dS + rstd (w dY - S rstd^2 mean(w dY S)),  which is the gradient of X and of R;   dw = sum over the rows of dY S rstd,   rstd = 1 / sqrt(mean S^2 + eps).
  *   All tensors are contiguous: X, R, S, Y, dY, dS, dX [tokens, width] in act_dtype, w [width] in w_dtype, codes [tokens, width] bytes, scales [tokens, width / group] and dw [width]
- *   fp32.  S may be X or R itself, Y may be any of the three, dX may be dY, dS or S (a row is read before it is written); no other overlap.
+ *   fp32, of any size (offsets are 64 bits).  S may be X or R itself, and so may Y (not the one that S is), dX may be dY, dS or S (a row is read before it is written); no other overlap.
  *   Sums, means and products are binary32: a row whose squares pass binary32 gives zeros, a NaN or infinity stays in its row (and in dw).
  *   width: a multiple of 8, up to 32768 (a multiple of `group` where codes are asked for); group 32, 64, 128, 256 or 512, or -1: one scale a row.
  *   tokens >= 0 of any number below 2^31; none leaves dw at zero.  eps >= 0, finite (EQAT_ERR_HYPER otherwise).
- *   ws: eqat_norm_workspace_bytes(d) bytes, 256-byte aligned, wanted for dw only; contents undefined before and after.
+ *   ws: eqat_norm_workspace_bytes(d) bytes, 256-byte aligned, wanted for dw only; contents undefined before and after; calls that share one must not overlap in time.
  * S, Y, (codes and scales together), dX and dw may each be NULL (skipped).  Same inputs give bitwise the same outputs.
  */
 typedef struct eqat_norm_desc {
@@ -511,7 +511,7 @@ eqat_status eqat_norm_bwd(const eqat_norm_desc *d, const void *S, const void *w,
  *   positions   int32 [tokens], device, any values.
  *   Q, K        [tokens, heads, head_dim] in act_dtype, strides { token, head } in elements; pointers and strides in bytes are multiples of 16, elements of a head contiguous.
  *               Either may be NULL (with its output).  An output may be its input (same pointer and strides); no other overlap.
- *   head_dim    a multiple of 8 up to 1024; part even, 2 .. head_dim.  tokens x heads below 2^31.
+ *   head_dim    a multiple of 8 up to 1024; part even, 2 .. head_dim.  tokens x heads below 2^31; tensors of any size.
  * EQAT_ERR_HYPER for an amplitude that is not finite.
  */
 typedef struct eqat_rotary_desc {
@@ -539,17 +539,17 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *   kind   EQAT_GATE_SILU  act(x) = x / (1 + exp(-x));   EQAT_GATE_GELU  act(x) = x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2
  *
  * eqat_gate_fwd / _bwd: element by element, for projections of any kind (Y = [G | U] as eqat_fq_linear_fwd leaves it on stacked weights).
- *   Y, dY [tokens, 2 F], H, dH [tokens, F] in `dtype`, contiguous; F a multiple of 8.  dY = [dH U act'(G) | dH act(G)].  In the backward pass H, or dY, may be NULL (skipped); dY
+ *   Y, dY [tokens, 2 F], H, dH [tokens, F] in `dtype`, contiguous; F a multiple of 8, tokens x F below 2^34.  dY = [dH U act'(G) | dH act(G)].  In the backward pass H, or dY, may be NULL (skipped); dY
  *   may be Y itself, H may be dH itself; no other overlap.
  *
  * eqat_gated_fwd / _bwd: both projections from the packed layer, the activation and the product in one kernel where activations are bf16 (G and U are not rounded and not stored):
  *   d          the stacked layer: out_features = 2 F, F a multiple of 8; tokens, in_features, bits, group, act_dtype as for eqat_qlinear_fwd (w_dtype is ignored).
  *   forward    X -> H [tokens, F].
  *   backward   X, dH -> dY = [dH U act'(G) | dH act(G)] [tokens, 2 F], and H again (either may be NULL): both projections are made anew, so that a training step keeps X
- *              alone between its passes; dY is what eqat_qlinear_bwd of the layer takes (dX, ds), H the input of the next linear in its own backward pass.
- *   _prepared  the same on a layer prepared by eqat_qlinear_prepare, s the current step sizes, the zero points those that it was prepared with.  Like the calls of eqat_qlinear_fwd_prepared,
- *              calls on one prepared layer must not overlap in time.
+ *              alone between its passes (H bitwise that of the forward where both take the same kernel: more than 64 tokens, or fp32); dY is what eqat_qlinear_bwd of the layer takes (dX, ds), H the input of the next linear in its own backward pass.
+ *   _prepared  the same on a layer prepared by eqat_qlinear_prepare, which is only read; s the current step sizes, the zero points those that it was prepared with.
  *   ws         eqat_gated_workspace_bytes(d) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
+ *              Calls that share one must not overlap in time.
  * With fp32 activations the projections are those of eqat_qlinear_fwd, in the workspace, and the gate a launch of its own.
  * EQAT_ERR_HYPER for an unknown kind.
  */

@@ -769,6 +769,31 @@ def gated_workspace(tokens, in_features, F, bits, group, dtype=torch.bfloat16, p
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
+@functools.lru_cache(maxsize=1024)
+def _packed_ok(w, s, z, I, bits, group):
+    """Whether these are the shapes of a packed layer of an even number of rows and I inputs."""
+    G = _groups(I, group)
+    return len(w) == 2 and w[0] % 2 == 0 and tuple(w) == (w[0], I * bits // 8) and tuple(s) == (w[0], G) and tuple(z) == (w[0], 4 * ((G * bits + 31) // 32))
+
+
+def _packed_layer(X, Wpacked, s, zpacked, bits, group):
+    if Wpacked.dtype is not torch.uint8 or zpacked.dtype is not torch.uint8 or s.dtype is not torch.float32 or not _packed_ok(Wpacked.shape, s.shape, zpacked.shape, X.shape[1], bits, group):
+        raise ValueError(f"not a packed layer of {X.shape[1]} inputs at {bits} bits in groups of {group}: codes {list(Wpacked.shape)}, step sizes {list(s.shape)}, zero points {list(zpacked.shape)}")
+    return _p(Wpacked), _p(s), _p(zpacked)
+
+
+@functools.lru_cache(maxsize=1024)
+def _prepared_bytes(F, I, bits, group, act_dtype):
+    return lib().eqat_prepared_bytes(_desc_ref(0, I, 2 * F, bits, group, act_dtype, BF16))
+
+
+def _prepared_layer(X, prepared, s, F, bits, group):
+    I = X.shape[1]
+    if prepared.dtype is not torch.uint8 or prepared.numel() < _prepared_bytes(F, I, bits, group, _dt(X)) or s.dtype is not torch.float32 or s.shape != (2 * F, _groups(I, group)):
+        raise ValueError(f"not a prepared layer of {I} inputs and 2 x {F} outputs at {bits} bits in groups of {group}: {prepared.numel()} bytes, step sizes {list(s.shape)}")
+    return _p(prepared), _p(s)
+
+
 def _gated(name, X, F, bits, group, layer, kind, dH, want, out, ws, prepared):
     T, I = X.shape
     dtype, h, y = X.dtype, (T, F), (T, 2 * F)
@@ -791,22 +816,22 @@ def _gated(name, X, F, bits, group, layer, kind, dH, want, out, ws, prepared):
 
 def eqat_gated_fwd(X, Wpacked, s, zpacked, bits, group, kind=GATE_SILU, H=None, ws=None):
     """H [tokens, F] = act(X Wg^T) * (X Wu^T) from the packed layer of the stacked projections [Wg; Wu] (2 F rows)."""
-    return _gated("eqat_gated_fwd", X, Wpacked.shape[0] // 2, bits, group, (_p(Wpacked), _p(s), _p(zpacked)), kind, None, ("H",), {} if H is None else {"H": H}, ws, False)["H"]
+    return _gated("eqat_gated_fwd", X, Wpacked.shape[0] // 2, bits, group, _packed_layer(X, Wpacked, s, zpacked, bits, group), kind, None, ("H",), {} if H is None else {"H": H}, ws, False)["H"]
 
 
 def eqat_gated_bwd(X, Wpacked, s, zpacked, dH, bits, group, kind=GATE_SILU, want=("dY", "H"), out=None, ws=None):
     """The gradient dY [tokens, 2 F] of the stacked projections' outputs from that of H, and H again; both projections are made anew from X."""
-    return _gated("eqat_gated_bwd", X, Wpacked.shape[0] // 2, bits, group, (_p(Wpacked), _p(s), _p(zpacked)), kind, dH, want, {} if out is None else out, ws, False)
+    return _gated("eqat_gated_bwd", X, Wpacked.shape[0] // 2, bits, group, _packed_layer(X, Wpacked, s, zpacked, bits, group), kind, dH, want, {} if out is None else out, ws, False)
 
 
 def eqat_gated_fwd_prepared(X, prepared, s, F, bits, group, kind=GATE_SILU, H=None, ws=None):
     """eqat_gated_fwd on a layer prepared by eqat_qlinear_prepare."""
-    return _gated("eqat_gated_fwd_prepared", X, int(F), bits, group, (_p(prepared), _p(s)), kind, None, ("H",), {} if H is None else {"H": H}, ws, True)["H"]
+    return _gated("eqat_gated_fwd_prepared", X, int(F), bits, group, _prepared_layer(X, prepared, s, int(F), bits, group), kind, None, ("H",), {} if H is None else {"H": H}, ws, True)["H"]
 
 
 def eqat_gated_bwd_prepared(X, prepared, s, dH, bits, group, kind=GATE_SILU, want=("dY", "H"), out=None, ws=None):
     """eqat_gated_bwd on a layer prepared by eqat_qlinear_prepare."""
-    return _gated("eqat_gated_bwd_prepared", X, dH.shape[1], bits, group, (_p(prepared), _p(s)), kind, dH, want, {} if out is None else out, ws, True)
+    return _gated("eqat_gated_bwd_prepared", X, dH.shape[1], bits, group, _prepared_layer(X, prepared, s, dH.shape[1], bits, group), kind, dH, want, {} if out is None else out, ws, True)
 
 
 def eqat_profile_start():

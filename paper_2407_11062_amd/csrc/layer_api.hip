@@ -124,7 +124,7 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
 static eqat_status gate_any(int64_t tokens, int64_t F, int32_t dtype, int kind, const void *Y, const void *dH, void *dY, void *H, bool back, void *stream)
 {
     if (!known(dtype)) return EQAT_ERR_DTYPE;
-    if (tokens < 0 || F < 8 || F % 8 != 0 || F >= kMost || tokens >= kMost || (tokens > 0 && F / 8 > ((kMost - 1) * 256) / tokens)) return EQAT_ERR_SHAPE;
+    if (tokens < 0 || F < 8 || F % 8 != 0 || F >= kMost || tokens >= kMost || (tokens > 0 && F / 8 > (kMost - 1) / tokens)) return EQAT_ERR_SHAPE;
     if (kind != EQAT_GATE_SILU && kind != EQAT_GATE_GELU) return EQAT_ERR_HYPER;
     if (tokens == 0 || (back && dY == nullptr && H == nullptr)) return EQAT_OK;
     if (Y == nullptr || (back ? dH == nullptr : H == nullptr)) return EQAT_ERR_NULL;

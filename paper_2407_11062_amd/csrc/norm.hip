@@ -342,17 +342,27 @@ size_t norm_ws_bytes(int64_t rows, int width) { return rows > 0 ? (size_t)bwd_bl
 void launch_norm_fwd(const NormFwd &n, hipStream_t st)
 {
     NormArgs a{};
-    a.rows = n.rows; a.x = n.x; a.r = n.r; a.w = n.w; a.s = n.s; a.y = n.y; a.codes = n.codes; a.scales = n.scales;
+    a.w = n.w;
     a.width = n.width; a.group = n.group; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
     const int64_t per = n.rows * n.width * (n.act_bf16 ? 2 : 4);
     const bool once = per * (1 + (n.r != nullptr) + (n.s != nullptr) + (n.y != nullptr)) > kOnceBytes;
     by_width(n.width, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
-        const unsigned blocks = (unsigned)((n.rows + kThreads / L - 1) / (kThreads / L));
-        if (n.act_bf16) {
-            if (once) k_norm_fwd<bf16_t, L, N, true><<<blocks, kThreads, 0, st>>>(a); else k_norm_fwd<bf16_t, L, N, false><<<blocks, kThreads, 0, st>>>(a);
-        } else {
-            if (once) k_norm_fwd<float, L, N, true><<<blocks, kThreads, 0, st>>>(a); else k_norm_fwd<float, L, N, false><<<blocks, kThreads, 0, st>>>(a);
+        // a launch has fewer than 2^32 threads
+        constexpr int64_t kRows = kThreads / L, kMostRows = ((int64_t)1 << 31) / kThreads * kRows;
+        const int64_t ax = n.act_bf16 ? 2 : 4;
+        for (int64_t done = 0; done < n.rows; done += kMostRows) {
+            auto from = [&](const void *p, int64_t bytes) { return p == nullptr ? nullptr : static_cast<char *>(const_cast<void *>(p)) + done * bytes; };
+            a.rows = std::min(n.rows - done, kMostRows);
+            a.x = from(n.x, n.width * ax); a.r = from(n.r, n.width * ax); a.s = from(n.s, n.width * ax); a.y = from(n.y, n.width * ax); a.codes = from(n.codes, n.width);
+            a.scales = reinterpret_cast<float *>(from(n.scales, n.width / n.group * 4));
+            const unsigned blocks = (unsigned)((a.rows + kRows - 1) / kRows);
+            auto go = [&](auto kern) { kern<<<blocks, kThreads, 0, st>>>(a); };
+            if (n.act_bf16) {
+                if (once) go(k_norm_fwd<bf16_t, L, N, true>); else go(k_norm_fwd<bf16_t, L, N, false>);
+            } else {
+                if (once) go(k_norm_fwd<float, L, N, true>); else go(k_norm_fwd<float, L, N, false>);
+            }
         }
     });
 }

@@ -127,6 +127,8 @@ def test_outputs_that_are_not_wanted():
             assert set(one) == {name} and torch.equal(one[name], both[name])
         again = eq.eqat_gated_bwd(X, layer.Wp, layer.s, layer.zp, dH, 3, 64)
         assert all(torch.equal(again[k], both[k]) for k in both)
+        if T > 64:                        # one kernel for both directions
+            assert torch.equal(eq.eqat_gated_fwd(X, layer.Wp, layer.s, layer.zp, 3, 64), both["H"])
     assert eq.eqat_gated_fwd(X[:0], layer.Wp, layer.s, layer.zp, 3, 64).shape == (0, 5504)
 
 
@@ -212,3 +214,16 @@ def test_extremes_of_the_gate():
         inf = big.clone()
         inf[0, 0] = float("inf")
         assert eq.eqat_gate_fwd(inf, kind)[0, 0] == float("inf")
+
+
+def test_the_gate_beyond_32_bits():
+    T, F = 100_000, 11008                             # Y is 4.4 GB
+    Y = torch.zeros((T, 2 * F), dtype=torch.bfloat16, device="cuda")
+    Y[-1] = torch.randn(2 * F, device="cuda")
+    H = eq.eqat_gate_fwd(Y)
+    assert torch.equal(H[-1:], eq.eqat_gate_fwd(Y[-1:])) and not H[:-1].any()
+    dH = torch.zeros_like(H)
+    dH[-1] = 1.0
+    want = eq.eqat_gate_bwd(Y[-1:].clone(), dH[-1:])["dY"]
+    eq.eqat_gate_bwd(Y, dH, out={"dY": Y})
+    assert torch.equal(Y[-1:], want) and not Y[:-1].any()

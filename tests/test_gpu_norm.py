@@ -195,3 +195,22 @@ def test_replayed_and_on_another_stream():
             step()
         side.synchronize()
         assert torch.equal(bwd["dW"], back["dW"]) and torch.equal(fwd["Y"], want["Y"])
+
+
+def test_offsets_beyond_32_bits():
+    """4.3 GB a tensor: the last rows are those of a call of their own"""
+    T, n, dt = 525_000, 4096, torch.bfloat16
+    tail = 3
+    X = torch.zeros((T, n), dtype=dt, device="cuda")
+    X[-tail:] = rows(1, tail, n, dt)
+    W = weight(2, n, torch.float32)
+    Y = torch.empty_like(X)
+    eq.eqat_norm_fwd(X, W, EPS, want=("Y",), out={"Y": Y})
+    assert torch.equal(Y[-tail:], eq.eqat_norm_fwd(X[-tail:], W, EPS)["Y"]) and not Y[:5].any() and not Y[T // 2:T // 2 + 5].any()
+    dY = torch.zeros_like(X)
+    dY[-tail:] = rows(3, tail, n, dt)
+    out = eq.eqat_norm_bwd(X, W, EPS, dY, out={"dX": Y})
+    want = eq.eqat_norm_bwd(X[-tail:], W, EPS, dY[-tail:])
+    assert torch.equal(Y[-tail:], want["dX"]) and not Y[:-tail].any()
+    _, dW, _, terms = ref.norm_back(X[-tail:], W, EPS, dY[-tail:])
+    ref.within(out["dW"], dW, terms.abs().sum(0) * (T // 512 + 1 + 8 + 48 + ref.NORM_ROUNDINGS + 2) * ref.F32)

@@ -219,3 +219,14 @@ def test_replayed_with_other_lengths():
         torch.cuda.synchronize()
         want = two_calls(caches[0], batch, rot, lens - 1, q, k, v)
         assert torch.equal(out, want) and torch.equal(caches[0].pool, caches[1].pool)
+
+
+def test_offsets_beyond_32_bits():
+    T, H, D = 270_000, 64, 128                       # 4.4 GB, in place
+    q = torch.zeros((T, H, D), dtype=torch.bfloat16, device="cuda")
+    tail = heads(1, 2, H, D, torch.bfloat16)
+    q[-2:] = tail
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    rot = eq.Rotary(freq(D), D)
+    eq.eqat_rotary(rot, pos, q, q_out=q)
+    assert torch.equal(q[-2:], eq.eqat_rotary(rot, pos[-2:].clone(), tail)[0]) and not q[:-2].any()

@@ -154,7 +154,7 @@ def test_gate_arguments(back):
     def call(T=4, F=64, dtype=eq.BF16, kind=0, Y=P, dH=P, dY=P, H=P):
         return L().eqat_gate_bwd(T, F, dtype, kind, Y, dH, dY, H, None) if back else L().eqat_gate_fwd(T, F, dtype, kind, Y, H, None)
     assert call(T=-1) == SHAPE and call(F=0) == SHAPE and call(F=12) == SHAPE and call(F=1 << 31) == SHAPE and call(T=1 << 31) == SHAPE and call(dtype=2) == DTYPE
-    assert call(T=(1 << 31) - 1, F=(1 << 30)) == SHAPE
+    assert call(T=(1 << 31) - 1, F=16) == SHAPE and call(T=1 << 28, F=64) == SHAPE
     assert call(kind=2) == HYPER and call(Y=None) == NULL and call(Y=P + 8) == ALIGN and call(H=P + 8) == ALIGN and call(T=0, Y=None) == OK
     if back:
         assert call(dH=None) == NULL and call(dH=P + 8) == ALIGN and call(dY=P + 8) == ALIGN and call(dY=None, H=None) == OK
@@ -174,3 +174,16 @@ def test_binding_refusals():
         eq.eqat_norm_fwd(x.half(), None, 1e-5)
     with pytest.raises(ValueError, match="32 bits"):
         eq.eqat_norm_fwd(x, None, 1e-5, group=1 << 33, want=("codes",), out={"codes": x, "scales": x})
+
+
+def test_binding_looks_at_the_layer():
+    X, s, z = torch.zeros(4, 64), torch.zeros(32, 2), torch.zeros(32, 4, dtype=torch.uint8)
+    for W, s_, z_ in ((torch.zeros(32, 16, dtype=torch.uint8), s, z[:16]), (torch.zeros(32, 24, dtype=torch.uint8), s, z), (torch.zeros(31, 16, dtype=torch.uint8), s[:31], z[:31]),
+                      (torch.zeros(32, 16, dtype=torch.uint8), s[:, :1], z), (torch.zeros(32, 16, dtype=torch.int8), s, z)):
+        with pytest.raises(ValueError, match="packed layer"):
+            eq.eqat_gated_fwd(X, W, s_, z_, 2, 32)
+    need = eq._prepared_bytes(16, 64, 2, 32, eq.F32)
+    assert need > 0
+    for n, s_ in ((need - 1, s), (need, s[:30])):
+        with pytest.raises(ValueError, match="prepared layer"):
+            eq.eqat_gated_fwd_prepared(X, torch.zeros(n, dtype=torch.uint8), s_, 16, 2, 32)
