@@ -311,26 +311,37 @@ constexpr int64_t kOnceBytes = (int64_t)96 << 20;
 
 constexpr int kNormParts = 512;         // workgroups of a backward pass at most
 
-template <typename F> void by_width(int width, F f)
+// Lanes and vectors a lane of a row.  Few vectors a lane where the chip has waves to spare: a row is a chain of a fetch, a sum, the results, and the shorter its links the better; with more rows than
+// compute units whole workgroups hide each other's.  Forward, us, 256 lanes / 512 / 1024: one row of 4096 3.3 / 2.9, 515 rows 5.5 / 5.3, one of 8192 4.5 / 3.5 / 3.1, 256 rows 6.4 / 5.2 / 4.9, 515 rows
+// 9.5 / 8.9 / 9.6, 4096 rows 50.9 / 46.3 / 45.5.  Backward: 1024 rows of 4096 14.1 / 13.2; 64 of 8192 8.6 / 7.9 / 7.9, 333 14.8 / 15.1 / 14.7, 4096 52 / 60 / 68.
+template <bool BACK, typename F> void by_width(int64_t rows, int width, F f)
 {
     const int n = width / 8;            // vectors of a row
+    const bool few = rows <= 256;
     if (n <= 8) f(IC<8>{}, IC<1>{});
     else if (n <= 16) f(IC<16>{}, IC<1>{});
     else if (n <= 32) f(IC<32>{}, IC<1>{});
     else if (n <= 64) f(IC<64>{}, IC<1>{});
     else if (n <= 128) f(IC<64>{}, IC<2>{});
     else if (n <= 256) f(IC<256>{}, IC<1>{});
-    else if (n <= 512) f(IC<256>{}, IC<2>{});
-    else if (n <= 768) f(IC<256>{}, IC<3>{});
-    else if (n <= 1024) f(IC<256>{}, IC<4>{});
-    else if (n <= 2048) f(IC<512>{}, IC<4>{});
-    else f(IC<1024>{}, IC<4>{});
+    else if (n <= 512) f(IC<512>{}, IC<1>{});
+    else if (n > 2048) f(IC<1024>{}, IC<4>{});
+    else if constexpr (BACK) {
+        if (n > 1024) f(IC<512>{}, IC<4>{});
+        else if (few) f(IC<512>{}, IC<2>{});
+        else if (n <= 768) f(IC<256>{}, IC<3>{});
+        else f(IC<256>{}, IC<4>{});
+    } else {
+        if (n <= 1024) { if (few) f(IC<1024>{}, IC<1>{}); else f(IC<512>{}, IC<2>{}); }
+        else if (few) f(IC<1024>{}, IC<2>{});
+        else f(IC<512>{}, IC<4>{});
+    }
 }
 
 int bwd_blocks(int64_t rows, int width)
 {
     int per = 1;
-    by_width(width, [&](auto lanes, auto) { per = decltype(lanes)::value < 256 ? 256 / decltype(lanes)::value : 1; });
+    by_width<true>(rows, width, [&](auto lanes, auto) { per = decltype(lanes)::value < 256 ? 256 / decltype(lanes)::value : 1; });
     const int64_t n = (rows + per - 1) / per;
     return (int)std::min<int64_t>(n, kNormParts);
 }
@@ -346,7 +357,7 @@ void launch_norm_fwd(const NormFwd &n, hipStream_t st)
     a.width = n.width; a.group = n.group; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
     const int64_t per = n.rows * n.width * (n.act_bf16 ? 2 : 4);
     const bool once = per * (1 + (n.r != nullptr) + (n.s != nullptr) + (n.y != nullptr)) > kOnceBytes;
-    by_width(n.width, [&](auto lanes, auto nv) {
+    by_width<false>(n.rows, n.width, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
         // a launch has fewer than 2^32 threads
         constexpr int64_t kRows = kThreads / L, kMostRows = ((int64_t)1 << 31) / kThreads * kRows;
@@ -374,7 +385,7 @@ void launch_norm_bwd(const NormBwd &n, void *ws, hipStream_t st)
     a.rows = n.rows; a.x = n.s; a.r = n.ds; a.w = n.w; a.dy = n.dy; a.y = n.dx;
     a.part = n.dw == nullptr ? nullptr : blocks == 1 ? n.dw : static_cast<float *>(ws);
     a.width = n.width; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
-    if (blocks > 0) by_width(n.width, [&](auto lanes, auto nv) {
+    if (blocks > 0) by_width<true>(n.rows, n.width, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
         const size_t lds = (L < 256 || L == 1024) && n.dw != nullptr ? (size_t)n.width * sizeof(float) : 0;
         if constexpr (L == 1024) {      // more than the default limit: once per device

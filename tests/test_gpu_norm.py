@@ -91,6 +91,20 @@ def test_backward_of_many_rows(T, n):
     assert set(one) == {"dX"} and set(other) == {"dW"} and torch.equal(one["dX"], out["dX"]) and torch.equal(other["dW"], out["dW"])
 
 
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float32))
+@pytest.mark.parametrize("T, n", [(257, 4104), (300, 6152), (300, 8192), (260, 8200), (257, 16384), (259, 1024), (1030, 8)])
+def test_more_rows_than_compute_units(T, n, dtype):
+    """other forms of the kernels take these"""
+    X, R, W = rows(n, T, n, dtype), rows(n + 1, T, n, dtype), weight(n + 2, n, torch.float32)
+    out = eq.eqat_norm_fwd(X, W, EPS, R=R, group=-1, want=("S", "Y", "codes"))
+    S, _, Y = ref.norm(X, W, EPS, R)
+    assert torch.equal(out["S"], S)
+    ref.within(out["Y"], Y, Y.abs() * (ref.half(dtype) + ref.NORM_ROUNDINGS * ref.F32))
+    scale = Y.abs().amax(-1, keepdim=True) / 448.0
+    ref.within(out["scales"], scale, scale * (ref.NORM_ROUNDINGS + 1) * ref.F32)
+    check_back(T, n, dtype)
+
+
 def test_gradient_against_differences():
     T, n, h = 2, 72, 1e-3
     X, R, W, dY, dS = (rows(i, T, n, torch.float32) for i in range(5))
