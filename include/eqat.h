@@ -550,7 +550,7 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *   _prepared  the same on a layer prepared by eqat_qlinear_prepare, which is only read; s the current step sizes, the zero points those that it was prepared with.
  *   ws         eqat_gated_workspace_bytes(d) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
  *              Calls that share one must not overlap in time.
- * With fp32 activations the projections are those of eqat_qlinear_fwd, in the workspace, and the gate a launch of its own.
+ * With fp32 activations a few tokens (4; 16 of a large layer) are one launch, too; more are the projections of eqat_qlinear_fwd, in the workspace, and the gate a launch of its own.
  * EQAT_ERR_HYPER for an unknown kind.
  */
 typedef enum { EQAT_GATE_SILU = 0, EQAT_GATE_GELU = 1 } eqat_gate_kind;

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.environ.get("EQAT_OBJ_DIR", os.path.join(HERE, "_build"))
 LIB = os.environ.get("EQAT_LIB_OUT", os.path.join(HERE, "libeqat.so"))
-SOURCES = ["gemm_mfma.hip", "gemm_bwd_ap_bf16.hip", "gemm_bwd_ap_f32.hip", "gemm_bwd_e2e.hip", "gemm_mid.hip", "gemv.hip", "api.hip", "quant.hip", "gemm_f32.hip", "gemm_ksplit.hip", "gemm_mid_dx.hip", "train_step.hip", "kv_api.hip", "kv_cache.hip", "kv_attend.hip", "kv_prompt.hip", "gemm_gated.hip", "gemm_mid_gated.hip", "gemv_gated.hip",
+SOURCES = ["gemm_mfma.hip", "gemm_bwd_ap_bf16.hip", "gemm_bwd_ap_f32.hip", "gemm_bwd_e2e.hip", "gemm_mid.hip", "gemv.hip", "api.hip", "quant.hip", "gemm_f32.hip", "gemm_ksplit.hip", "gemm_mid_dx.hip", "train_step.hip", "kv_api.hip", "kv_cache.hip", "kv_attend.hip", "kv_prompt.hip", "gemm_gated.hip", "gemm_mid_gated.hip", "gemv_gated.hip", "gated_f32.hip",
            "layer_api.hip", "norm.hip", "rotary.hip", "gate.hip"]
 # measurement aids of bench.py (a bare MFMA loop, a plain copy): a library of their own, not part of the product
 PEAKS_SOURCE = "bench_peaks.hip"

@@ -629,6 +629,7 @@ static GatedWs gated_ws(const Problem &p)
     GatedWs l{};
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += align256(bytes); return at; };
+    if (eqat::gated_few_f32_applies(p)) return l;
     if (!p.act_bf16) l.y = take((size_t)p.T * p.O * 4);
     else if (p.T <= 64 && eqat::group_by_magic(p)) return l;          // no kernel for so few tokens has anything in it
     l.sz = take((size_t)p.O * p.G * 8);
@@ -661,6 +662,7 @@ static eqat_status gated_any(const eqat_desc *d, int kind, const void *X, const 
     const char *p8 = (const char *)layer;
     const float *zb = prepared ? (const float *)(p8 + pl.zb) : nullptr;
     const eqat::GatedOut out{H, dH, dY, kind};
+    if (eqat::gated_few_f32_applies(p)) { ProfScope ps(eqat::PK_F32, st); eqat::launch_gated_few_f32(p, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); return launch_status(); }
     if (!p.act_bf16) {
         qlinear_prepare_into(p, nullptr, s, zpacked, zb, nullptr, w8 + l.sz, nullptr, 0, st);
         { ProfScope ps(eqat::PK_F32, st); eqat::launch_f32_fwd(p, true, X, prepared ? p8 + pl.codes : p8, s, w8 + l.sz, w8 + l.y, st); }

@@ -99,13 +99,4 @@ __device__ __forceinline__ uint32_t lanes_greatest(uint32_t x)
     return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
-// x / d for 0 <= x, 0 < d: twice by a reciprocal, the second time of what the first left (its error is below 2^10), and put right by one.  The compiler's own is four
-// times as long, and these stand in a row before anything is fetched.
-__device__ __forceinline__ int quotient(int x, int d)
-{
-    const float by = __builtin_amdgcn_rcpf((float)d);
-    const int q = (int)((float)x * by), left = x - q * d, p = (int)((float)left * by), r = left - p * d;
-    return q + p + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0);
-}
-
 }  // namespace eqat

@@ -78,10 +78,10 @@ def test_many_tiles(T, I, F, group, bits):
     Layer(T, I, F, bits, group).check(T, kind=bits % 2)
 
 
-@pytest.mark.parametrize("bits, I, F, group", [(2, 256, 24, 64), (3, 480, 520, 96), (4, 1024, 200, -1)])
+@pytest.mark.parametrize("bits, I, F, group", [(2, 256, 24, 64), (3, 480, 520, 96), (4, 1024, 200, -1), (3, 2080, 72, 32), (2, 32, 8, 32), (4, 4128, 40, 32)])
 def test_fp32(bits, I, F, group):
     layer = Layer(I, I, F, bits, group)
-    for T in (1, 33, 200):
+    for T in (1, 2, 5, 16, 17, 33, 200):
         layer.check(T, dtype=torch.float32, kind=T % 2)
 
 
