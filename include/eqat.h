@@ -548,6 +548,7 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *   backward   X, dH -> dY = [dH U act'(G) | dH act(G)] [tokens, 2 F], and H again (either may be NULL): both projections are made anew, so that a training step keeps X
  *              alone between its passes (H bitwise that of the forward where both take the same kernel: more than 64 tokens, or fp32); dY is what eqat_qlinear_bwd of the layer takes (dX, ds), H the input of the next linear in its own backward pass.
  *   _prepared  the same on a layer prepared by eqat_qlinear_prepare, which is only read; s the current step sizes, the zero points those that it was prepared with.
+ *   No tensor may overlap another.
  *   ws         eqat_gated_workspace_bytes(d) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
  *              Calls that share one must not overlap in time.
  * With fp32 activations a few tokens (4; 16 of a large layer) are one launch, too; more are the projections of eqat_qlinear_fwd, in the workspace, and the gate a launch of its own.

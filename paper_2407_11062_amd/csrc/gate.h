@@ -24,15 +24,15 @@ template <int KIND> __device__ __forceinline__ float gate_t(float x)
     constexpr float k2 = 1.5957691216057307f;                         // 2 sqrt(2 / pi)
     return KIND == EQAT_GATE_SILU ? x : k2 * x * __builtin_fmaf(0.044715f * x, x, 1.0f);
 }
+// gelu's t'; where x^2 passes binary32, p or q has long been 0, and has to stay it in the product
+__device__ __forceinline__ float slope_of_t(float x) { return fminf(1.5957691216057307f * __builtin_fmaf(0.134145f * x, x, 1.0f), 0x1p100f); }
 template <int KIND> __device__ __forceinline__ float gate_act(float x) { return x * gate_p(gate_t<KIND>(x)).p; }
 // value and derivative
 template <int KIND> __device__ __forceinline__ void gate_both(float x, float &a, float &slope)
 {
-    constexpr float k2 = 1.5957691216057307f;
     const GateP r = gate_p(gate_t<KIND>(x));
-    const float t1 = KIND == EQAT_GATE_SILU ? 1.0f : k2 * __builtin_fmaf(0.134145f * x, x, 1.0f);
+    const float t1 = KIND == EQAT_GATE_SILU ? 1.0f : slope_of_t(x);
     a = x * r.p;
-    // for large x, q is 0 (and t' x finite as long as x^3 is a binary32 number)
     slope = __builtin_fmaf(a * r.q, t1, r.p);
 }
 
@@ -44,11 +44,10 @@ template <int KIND> __device__ __forceinline__ float gated_near(float g, float u
 struct Gated { float h, dg, du; };
 template <int KIND> __device__ __forceinline__ Gated gated_both_near(float g, float u, float d)
 {
-    constexpr float k2 = 1.5957691216057307f;
     const float p = gate_p_near(gate_t<KIND>(g)), act = g * p, du = d * act;
     float slope;
     if constexpr (KIND == EQAT_GATE_SILU) slope = __builtin_fmaf(act, 1.0f - p, p);
-    else slope = __builtin_fmaf(act * (1.0f - p), k2 * __builtin_fmaf(0.134145f * g, g, 1.0f), p);
+    else slope = __builtin_fmaf(act * (1.0f - p), slope_of_t(g), p);
     return Gated{act * u, d * u * slope, du};
 }
 // of one element: act(g) u, and with the gradient d of it d u act'(g), d act(g)

@@ -85,6 +85,15 @@ def test_fp32(bits, I, F, group):
         layer.check(T, dtype=torch.float32, kind=T % 2)
 
 
+@pytest.mark.parametrize("tokens, I, F, bits, group", [((1, 2, 3, 5, 16), 4096, 2816, 2, 64), ((1, 3, 6), 1056, 16424, 3, 32), ((1, 2, 3), 8192, 136, 4, 128), ((1, 3), 36352, 8, 2, 64),
+                                                       ((1, 3), 36384, 8, 4, 32)])
+def test_few_tokens_in_fp32(tokens, I, F, bits, group):
+    """up to 16 of large layers, more couples of rows than a launch has waves, inputs of which LDS holds four tokens, one or none"""
+    layer = Layer(F, I, F, bits, group)
+    for T in tokens:
+        layer.check(T, dtype=torch.float32, kind=T % 2)
+
+
 @pytest.mark.parametrize("T", (1, 8, 100, 2000))
 def test_against_the_weights_that_the_layer_stands_for(T):
     """Beside the bounds above each weight is rounded once: at most 2^-8 of it, independent of the others, so the 2-norm of G's error is at most 2^-8 of that of its products'
@@ -214,6 +223,34 @@ def test_extremes_of_the_gate():
         inf = big.clone()
         inf[0, 0] = float("inf")
         assert eq.eqat_gate_fwd(inf, kind)[0, 0] == float("inf")
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float32))
+def test_extremes_of_the_gradient(dtype):
+    """act' is 1 or 0 far out, also where the square of G is no binary32 number; |act(g)| < 2e38 for the G below"""
+    Y = torch.tensor([[1e18, -1e18, 1e20, -1e20, 1e38, -1e38, 1e6, -1e6] + [2.0] * 8], device="cuda").to(dtype)
+    dH = torch.ones((1, 8), dtype=dtype, device="cuda")
+    for kind in (0, 1):
+        dY = eq.eqat_gate_bwd(Y, dH, kind)["dY"][0]
+        assert torch.equal(dY[:8], torch.tensor([2.0, 0.0] * 4, device="cuda").to(dtype) + 0.0)
+        assert torch.equal(dY[8:], Y[0, :8].clamp_min(0.0))
+
+
+@pytest.mark.parametrize("T", (1, 100, 2000))          # (few tokens, few tiles, many)
+def test_extremes_of_the_fused_gradient(T):
+    """the same where G comes out of the products: the first input of every token is 2^67, the other ones 0"""
+    I, F = 64, 2048
+    layer = Layer(9, I, F, 4, 64)
+    X, dH = torch.zeros((T, I), dtype=torch.bfloat16, device="cuda"), torch.ones((T, F), dtype=torch.bfloat16, device="cuda")
+    X[:, 0] = 2.0 ** 67
+    back = eq.eqat_gated_bwd(X, layer.Wp, layer.s, layer.zp, dH, 4, 64, kind=1)
+    y = X.double() @ ref.what(layer.Wp, layer.s, layer.zp, I, 4, rounded=True).t()
+    g, u = y[:, :F], y[:, F:]
+    h = 2.0 ** -8                                     # one product a sum, binary32: exact; the results are rounded once, and the product of two is once more, 2^-23 of it
+    for got, want in ((back["dY"][:, :F], u * (g > 0)), (back["dY"][:, F:], g.clamp_min(0.0)), (back["H"], g.clamp_min(0.0) * u)):
+        some = (g.abs() > 1e6) & (want.abs() < 1e38)  # (0 where a weight stands for 0)
+        assert some.float().mean() > 0.3
+        ref.within(got.double()[some], want[some], ((h + 2.0 ** -20) * want.abs())[some])
 
 
 def test_the_gate_beyond_32_bits():
