@@ -130,11 +130,20 @@ void launch_rotary(const RotaryCall &c, hipStream_t st)
     }
     // blockIdx.y has 16 bits
     a.block_heads = std::max(a.block_heads, (a.heads + 65534) / 65535);
-    const dim3 grid((unsigned)((c.tokens + a.block_tokens - 1) / a.block_tokens), (unsigned)((a.heads + a.block_heads - 1) / a.block_heads));
     const size_t lds = (size_t)a.block_tokens * a.half * sizeof(floatx2);
     // Past the caches from this many bytes on: 8192 tokens of 72 heads of 128, 302 MB, graph replays over three states 58 -> 52 us, 151 MB 31.9 -> 27.6, 75 MB 13.6 -> 15.6
     const bool once = 2 * c.tokens * a.heads * c.head_dim * (c.act_bf16 ? 2 : 4) > (int64_t)96 << 20;
-    auto go = [&](auto kern) { kern<<<grid, kThreads, lds, st>>>(a); };
+    const int64_t size = c.act_bf16 ? 2 : 4, most = ((int64_t)1 << 31) / kThreads * a.block_tokens;          // a launch has fewer than 2^32 threads
+    auto go = [&](auto kern) {
+        for (int64_t done = 0; done < c.tokens; done += most) {
+            RotaryArgs b = a;
+            auto from = [&](KvRows &r) { if (r.p != nullptr) r.p = static_cast<char *>(r.p) + done * r.token_stride * size; };
+            from(b.q); from(b.k); from(b.q_out); from(b.k_out);
+            b.pos += done;
+            b.tokens = std::min(c.tokens - done, most);
+            kern<<<dim3((unsigned)((b.tokens + a.block_tokens - 1) / a.block_tokens), (unsigned)((a.heads + a.block_heads - 1) / a.block_heads)), kThreads, lds, st>>>(b);
+        }
+    };
 #define EQAT_ROTARY(T, V) do { if (c.turn.interleaved) { if (once) go(k_rotary<T, V, true, true>); else go(k_rotary<T, V, true, false>); } \
                                else if (once) go(k_rotary<T, V, false, true>); else go(k_rotary<T, V, false, false>); } while (0)
     if (c.act_bf16) {

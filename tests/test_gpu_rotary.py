@@ -230,3 +230,18 @@ def test_offsets_beyond_32_bits():
     rot = eq.Rotary(freq(D), D)
     eq.eqat_rotary(rot, pos, q, q_out=q)
     assert torch.equal(q[-2:], eq.eqat_rotary(rot, pos[-2:].clone(), tail)[0]) and not q[:-2].any()
+
+
+def test_more_workgroups_than_a_launch_holds():
+    """68 tokens to a workgroup, and 2^24 workgroups of 256 threads are 2^32 threads: 37 GB, in place"""
+    T, D, part = 1_150_000_000, 16, 2
+    q = torch.zeros((T, 1, D), dtype=torch.bfloat16, device="cuda")
+    pos = torch.zeros(T, dtype=torch.int32, device="cuda")
+    some = torch.tensor([0, 1, 570_425_343, 570_425_344, 1_140_850_687, 1_140_850_688, T - 1], device="cuda")
+    rows = heads(3, some.numel(), 1, D, torch.bfloat16)
+    q[some], pos[some] = rows, torch.arange(1, 8, dtype=torch.int32, device="cuda")
+    rot = eq.Rotary(freq(part), D)
+    want = eq.eqat_rotary(rot, pos[some], rows)[0]
+    eq.eqat_rotary(rot, pos, q, q_out=q)
+    assert torch.equal(q[some], want)
+    assert int(torch.stack([c.ne(0).sum() for c in q.view(torch.int16).view(-1).chunk(16)]).sum()) == int(want.ne(0).sum())
