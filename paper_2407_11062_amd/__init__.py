@@ -667,6 +667,8 @@ def eqat_norm_bwd(S, W, eps, dY, dS=None, want=("dX", "dW"), out=None, ws=None):
 def rotary_frequencies(part, base=10000.0, stretch=1.0, short=256.0, long=2048.0):
     """fp32 frequencies base^(-2 i / part) of `part` / 2 pairs (on the host).  stretch > 1, for contexts that many times longer: wave lengths of `long` tokens and more are stretched by it,
     those below `short` tokens are kept, between the two in proportion to their logarithm."""
+    if part % 2 or not (base > 0 and stretch >= 1.0 and 0.0 < short < long):
+        raise ValueError("part is even, base positive, stretch 1 or more, 0 < short < long")
     i = torch.arange(int(part) // 2, dtype=torch.float64)
     f = float(base) ** (-2.0 * i / int(part))
     if stretch > 1.0:

@@ -187,3 +187,15 @@ def test_binding_looks_at_the_layer():
     for n, s_ in ((need - 1, s), (need, s[:30])):
         with pytest.raises(ValueError, match="prepared layer"):
             eq.eqat_gated_fwd_prepared(X, torch.zeros(n, dtype=torch.uint8), s_, 16, 2, 32)
+
+
+def test_rotary_frequencies():
+    import paper_2407_11062_amd as eq
+    for kw in ({"part": 7}, {"part": 8, "base": 0.0}, {"part": 8, "stretch": 0.5}, {"part": 8, "stretch": 2.0, "short": 64.0, "long": 64.0}, {"part": 8, "short": 0.0}):
+        with pytest.raises(ValueError):
+            eq.rotary_frequencies(**kw)
+    f = eq.rotary_frequencies(128, base=10000.0).double()
+    assert len(f) == 64 and all(abs(float(f[i]) * 10000.0 ** (i / 64) - 1.0) < 1e-7 for i in range(64))
+    g = eq.rotary_frequencies(128, stretch=8.0).double()
+    waves = 2 * 3.141592653589793 / f
+    assert (g[waves < 256.0] == f[waves < 256.0]).all() and ((g * 8.0 - f)[waves > 2048.0].abs() <= 1e-7 * f[waves > 2048.0]).all() and (g <= f).all() and (g >= f / 8.0 * (1 - 1e-7)).all()
