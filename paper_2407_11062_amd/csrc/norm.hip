@@ -309,7 +309,9 @@ __global__ __launch_bounds__(256) void k_norm_dw(const float *__restrict__ part,
 // states, us, through the caches / past them: norm 67 MB 13.4 / 13.8, 134 MB 29.5 / 25.6, 269 MB 58 / 51, 537 MB 103 / 96; its gradients 67 MB 18.7 / 20.7, 134 MB 34.0 / 30.0, 269 MB 57 / 50.
 constexpr int64_t kOnceBytes = (int64_t)96 << 20;
 
-constexpr int kNormParts = 512;         // workgroups of a backward pass at most
+// Workgroups of a backward pass at most: two a compute unit.  One each where few of them would have two rows and the others one, and where waves of a row fill a compute unit; the second launch has
+// half the parts then.  us, 512 / 256: 512 rows of 4096, fp32, 13.8 / 12.0; 600 of 16384 35 / 27; 1500 of 20000 93 / 80; 1024 of 8192 21.0 / 21.5; 2048 of 8192 32.6 / 36.
+constexpr int kNormParts = 512;
 
 // Lanes and vectors a lane of a row.  Few vectors a lane where the chip has waves to spare: a row is a chain of a fetch, a sum, the results, and the shorter its links the better; with more rows than
 // compute units whole workgroups hide each other's.  Forward, us, 256 lanes / 512 / 1024: one row of 4096 3.3 / 2.9, 515 rows 5.5 / 5.3, one of 8192 4.5 / 3.5 / 3.1, 256 rows 6.4 / 5.2 / 4.9, 515 rows
@@ -343,7 +345,7 @@ int bwd_blocks(int64_t rows, int width)
     int per = 1;
     by_width<true>(rows, width, [&](auto lanes, auto) { per = decltype(lanes)::value < 256 ? 256 / decltype(lanes)::value : 1; });
     const int64_t n = (rows + per - 1) / per;
-    return (int)std::min<int64_t>(n, kNormParts);
+    return (int)std::min<int64_t>(n, n <= 768 || width > 16384 ? kNormParts / 2 : kNormParts);
 }
 
 }  // namespace
