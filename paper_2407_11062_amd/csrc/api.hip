@@ -673,7 +673,7 @@ static eqat_status gated_any(const eqat_desc *d, int kind, const void *X, const 
     case GATED_GEMV: { ProfScope ps(eqat::PK_GEMV, st); eqat::launch_gemv_gated(p, kind, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, H, st); break; }
     case GATED_MID: { ProfScope ps(eqat::PK_GEMM_FWD, st); eqat::launch_mid_gated(p, tokens, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); break; }
     default: {
-        qlinear_prepare_into(p, nullptr, s, zpacked, zb, nullptr, w8 + l.sz, nullptr, 0, st);
+        { ProfScope ps(eqat::PK_PREPARE, st); eqat::launch_gated_pairs(p, s, zpacked, zb, w8 + l.sz, st); }
         ProfScope ps(eqat::PK_GEMM_FWD, st);
         eqat::launch_tiles_gated(p, tokens, !prepared, out, X, prepared ? p8 + pl.codes : p8, w8 + l.sz, st);
     }

@@ -104,6 +104,8 @@ struct GatedOut { void *H; const void *dH; void *dY; int kind; };
 double mid_gated_us(const Problem &p, bool packed, int *tokens);
 double tiles_gated_us(const Problem &p, int *tokens);
 void launch_mid_gated(const Problem &p, int tokens, const GatedOut &out, const void *X, const void *codes, const float *s, const void *zpacked, const float *z, hipStream_t st);
+// the (s, z) pairs that launch_tiles_gated reads, of packed zero points or of a prepared layer's
+void launch_gated_pairs(const Problem &p, const float *s, const void *zpacked, const float *z, void *sz, hipStream_t st);
 // codes in the working layout or, `dense`, as packed; (s, z) pairs
 void launch_tiles_gated(const Problem &p, int tokens, bool dense, const GatedOut &out, const void *X, const void *codes, const void *sz, hipStream_t st);
 
