@@ -11,6 +11,8 @@
 //
 // eqat_kv_rotary_write is the same launch with the keys turned on their way in (rounded to the activations' type, as eqat_rotary leaves them, so that what is written is
 // bitwise what the two calls write) and workgroups beside it that turn the queries.  A workgroup makes the cosines and sines of its record's tokens in LDS first.
+// us of a graph's step, one launch / the two: 16 sequences, 64 heads on 8 of 128, 6.0 / 8.5; one token of 32 heads 5.7 / 7.8; 333 tokens of 32 heads 11.3 / 12.0; 8192 79 / 87; 8192 of 64 heads on 8
+// 69 / 67; fp32, 4 x 2000 of 40 heads, 176 / 182.
 #include "layer.h"
 #include "turn.h"
 
@@ -176,7 +178,7 @@ struct TurnArgs {
     const float *freq;
     KvRows q, q_out;
     float amplitude;
-    int half, part, interleaved, q_heads, block_heads, kv_blocks;
+    int half, part, interleaved, q_heads, block_heads, kv_blocks, once;
 };
 __device__ __forceinline__ void turn(float &x, float &y, floatx2 cs)
 {
@@ -230,47 +232,70 @@ template <int NS, typename T> __device__ __forceinline__ void turn_key(const Tur
         for (int e = 0; e < 8; ++e) x[j][e] = to_float((T)x[j][e]);
 }
 
-// The queries of a record's rows, heads head0 ..: a unit of work is eight neighbouring elements, or two times eight that are partners; pairs and single elements where eight do
-// not divide half of what is turned.  Both of a pair are read before either is written.
-template <int NS, typename T> __device__ __forceinline__ void turn_queries(const TurnArgs &r, const floatx2 *turns, const Place &at, int head0)
+// The queries of a record's rows, heads head0 ..: a unit of work is eight neighbouring elements, or two times eight that are partners, two units on their way at a time; pairs and single
+// elements where eight do not divide half of what is turned.  Both of a pair are read before either is written.
+template <int NS, typename T, bool ONCE> __device__ __forceinline__ void turn_queries(const TurnArgs &r, const floatx2 *turns, const Place &at, int head0)
 {
     constexpr int D = 32 * NS, kThreads = kCacheWaves * 64;
     const int heads = min(r.block_heads, r.q_heads - head0), tokens = at.to - at.from;
     const bool by_eight = r.interleaved || r.half % 8 == 0;
-    const int turned = r.interleaved ? D / 8 : by_eight ? r.half / 8 : r.half, units = r.interleaved ? D / 8 : by_eight ? (D - r.half) / 8 : D - r.half;
-    for (int u = threadIdx.x; u < tokens * heads * units; u += kThreads) {
-        const int th = quotient(u, units), p = u - th * units, t = quotient(th, heads), h = head0 + (th - t * heads);
+    const int turned = r.interleaved ? D / 8 : by_eight ? r.half / 8 : r.half, units = r.interleaved ? D / 8 : by_eight ? (D - r.half) / 8 : D - r.half, n = tokens * heads * units;
+    struct Unit { const T *from; T *to; const floatx2 *cs; int p; Eight<T> x, y; };
+    auto place = [&](int u) {
+        Unit w;
+        const int th = quotient(u, units), t = quotient(th, heads), h = head0 + (th - t * heads);
         const int64_t row = at.row + t;
-        const T *from = static_cast<const T *>(r.q.p) + row * r.q.token_stride + h * r.q.head_stride;
-        T *to = static_cast<T *>(r.q_out.p) + row * r.q_out.token_stride + h * r.q_out.head_stride;
-        const floatx2 *cs = turns + t * r.half;
-        if (!by_eight) {
-            if (p < turned) {
-                float x = to_float(from[p]), y = to_float(from[p + r.half]);
-                turn(x, y, cs[p]);
-                to[p] = (T)x; to[p + r.half] = (T)y;
+        w.p = u - th * units;
+        w.from = static_cast<const T *>(r.q.p) + row * r.q.token_stride + h * r.q.head_stride;
+        w.to = static_cast<T *>(r.q_out.p) + row * r.q_out.token_stride + h * r.q_out.head_stride;
+        w.cs = turns + t * r.half;
+        return w;
+    };
+    if (!by_eight) {
+        for (int u = threadIdx.x; u < n; u += kThreads) {
+            const Unit w = place(u);
+            if (w.p < turned) {
+                float x = to_float(w.from[w.p]), y = to_float(w.from[w.p + r.half]);
+                turn(x, y, w.cs[w.p]);
+                w.to[w.p] = (T)x; w.to[w.p + r.half] = (T)y;
             } else {
-                to[p + r.half] = from[p + r.half];
+                w.to[w.p + r.half] = w.from[w.p + r.half];
             }
-            continue;
         }
+        return;
+    }
+    auto take = [&](int u) {
+        Unit w = place(min(u, n - 1));
+        const bool two = !r.interleaved && w.p < turned;
+        const T *from = w.from + 8 * w.p;
+        w.x.template load<ONCE>(r.interleaved || two ? from : from + r.half);
+        if (two) w.y.template load<ONCE>(from + r.half);
+        return w;
+    };
+    auto put = [&](Unit &w) {
         float x[8], y[8];
+        T *to = w.to + 8 * w.p;
         if (r.interleaved) {
-            load8(from + 8 * p, x);
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) if (8 * p + e < r.part) turn(x[e], x[e + 1], cs[4 * p + e / 2]);
-            store8(to + 8 * p, x);
-        } else if (p < turned) {
-            load8(from + 8 * p, x);
-            load8(from + 8 * p + r.half, y);
+            for (int e = 0; e < 8; ++e) x[e] = w.x.get(e);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) turn(x[e], y[e], cs[8 * p + e]);
-            store8(to + 8 * p, x);
-            store8(to + 8 * p + r.half, y);
+            for (int e = 0; e < 8; e += 2) if (8 * w.p + e < r.part) turn(x[e], x[e + 1], w.cs[4 * w.p + e / 2]);
+            w.x.set(x);
+        } else if (w.p < turned) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { x[e] = w.x.get(e); y[e] = w.y.get(e); turn(x[e], y[e], w.cs[8 * w.p + e]); }
+            w.x.set(x);
+            w.y.set(y);
+            w.y.template store<ONCE>(to + r.half);
         } else {
-            load8(from + 8 * p + r.half, x);
-            store8(to + 8 * p + r.half, x);
+            to += r.half;
         }
+        w.x.template store<ONCE>(to);
+    };
+    for (int u = threadIdx.x; u < n; u += 2 * kThreads) {
+        Unit v = take(u), w = take(u + kThreads);
+        put(v);
+        if (u + kThreads < n) put(w);
     }
 }
 
@@ -290,7 +315,8 @@ template <int NS, int SG, typename T, bool TURN> __device__ __forceinline__ void
         }
         __syncthreads();
         if ((int)blockIdx.y >= turned.kv_blocks) {
-            turn_queries<NS, T>(turned, turns, all, ((int)blockIdx.y - turned.kv_blocks) * turned.block_heads);
+            const int head0 = ((int)blockIdx.y - turned.kv_blocks) * turned.block_heads;
+            if (turned.once) turn_queries<NS, T, true>(turned, turns, all, head0); else turn_queries<NS, T, false>(turned, turns, all, head0);
             return;
         }
     }
@@ -444,6 +470,9 @@ template <int NS, int SG> void launch(const KvShape &s, const CacheArgs &a, int 
     if (turned != nullptr) {
         TurnArgs r = *turned;
         r.kv_blocks = (int)grid.y;
+        // Queries of `block_heads` heads to a workgroup, or of as few as four where that leaves compute units idle
+        r.block_heads = std::min(r.block_heads, std::max(4, (int)((int64_t)r.q_heads * records / 512)));
+        r.block_heads = std::max(r.block_heads, (r.q_heads + 16383) / 16384);
         grid.y += (unsigned)((r.q_heads + r.block_heads - 1) / r.block_heads);
         const size_t lds = (size_t)std::min(a.b.max_new, kKvRecord) * r.half * sizeof(floatx2);
         if (s.act_bf16) k_kv_rotary_write<NS, SG, bf16_t><<<grid, kCacheWaves * 64, lds, st>>>(a, r);
@@ -491,7 +520,7 @@ void launch_kv_rotary_write(const KvShape &s, const KvBatch &b, const Rotary &tu
     r.q_heads = q_heads;
     // A record's tokens of 16 heads, so that a prompt's cosines and sines are a fraction of the work; where a sequence has a token or a few, all the heads that 256 lanes turn at once
     r.block_heads = std::max(16, 512 / (std::max(1, std::min(b.max_new, kKvRecord)) * s.head_dim / 8));
-    r.block_heads = std::max(r.block_heads, (q_heads + 16383) / 16384);
+    r.once = 2 * b.tokens * q_heads * s.head_dim * (s.act_bf16 ? 2 : 4) > (int64_t)96 << 20;          // (see launch_rotary)
     launch_any(s, b, k, v, pool, true, &r, st);
 }
 
