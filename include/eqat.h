@@ -542,7 +542,7 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *   Y, dY [tokens, 2 F], H, dH [tokens, F] in `dtype`, contiguous; F a multiple of 8, tokens x F below 2^34.  dY = [dH U act'(G) | dH act(G)].  In the backward pass H, or dY, may be NULL (skipped); dY
  *   may be Y itself, H may be dH itself; no other overlap.
  *
- * eqat_gated_fwd / _bwd: both projections from the packed layer, the activation and the product in one kernel where activations are bf16 (G and U are not rounded and not stored):
+ * eqat_gated_fwd / _bwd: both projections from the packed layer, the activation and the product in one kernel (G and U are not rounded and not stored):
  *   d          the stacked layer: out_features = 2 F, F a multiple of 8; tokens, in_features, bits, group, act_dtype as for eqat_qlinear_fwd (w_dtype is ignored).
  *   forward    X -> H [tokens, F].
  *   backward   X, dH -> dY = [dH U act'(G) | dH act(G)] [tokens, 2 F], and H again (either may be NULL): both projections are made anew, so that a training step keeps X
@@ -551,7 +551,7 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *   No tensor may overlap another.
  *   ws         eqat_gated_workspace_bytes(d) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
  *              Calls that share one must not overlap in time.
- * With fp32 activations a few tokens (4; 16 of a large layer) are one launch, too; more are the projections of eqat_qlinear_fwd, in the workspace, and the gate a launch of its own.
+ * With fp32 activations all of it is binary32.
  * EQAT_ERR_HYPER for an unknown kind.
  */
 typedef enum { EQAT_GATE_SILU = 0, EQAT_GATE_GELU = 1 } eqat_gate_kind;

@@ -611,8 +611,6 @@ eqat_status eqat_qlinear_bwd_prepared_kept(const eqat_desc *d, const void *X, co
 }
 
 // ---- gated feed-forward (d: the stacked projection, out_features = 2 F) ----------------------------------------------
-// (s, z) pairs; with fp32 activations the projections, too
-struct GatedWs { size_t y, sz, total; };
 // which kernel: matrix-vector (forward), the one for few output tiles, the tiles
 enum GatedKernel { GATED_GEMV, GATED_MID, GATED_TILES };
 static GatedKernel gated_kernel(const Problem &p, bool prepared, bool backward, int *tokens)
@@ -624,18 +622,8 @@ static GatedKernel gated_kernel(const Problem &p, bool prepared, bool backward, 
     *tokens = mid;
     return GATED_MID;
 }
-static GatedWs gated_ws(const Problem &p)
-{
-    GatedWs l{};
-    size_t off = 0;
-    auto take = [&](size_t bytes) { const size_t at = off; off += align256(bytes); return at; };
-    if (eqat::gated_few_f32_applies(p)) return l;
-    if (!p.act_bf16) l.y = take((size_t)p.T * p.O * 4);
-    else if (p.T <= 64 && eqat::group_by_magic(p)) return l;          // no kernel for so few tokens has anything in it
-    l.sz = take((size_t)p.O * p.G * 8);
-    l.total = off;
-    return l;
-}
+// the workspace: (s, z) pairs; what runs in fp32 and with so few tokens has nothing in it
+static size_t gated_ws(const Problem &p) { return !p.act_bf16 || (p.T <= 64 && eqat::group_by_magic(p)) ? 0 : align256((size_t)p.O * p.G * 8); }
 static eqat_status gated_any(const eqat_desc *d, int kind, const void *X, const void *layer, const float *s, const uint8_t *zpacked, bool prepared, const void *dH, void *dY, void *H,
                              bool backward, void *ws, size_t ws_bytes, void *stream)
 {
@@ -652,30 +640,24 @@ static eqat_status gated_any(const eqat_desc *d, int kind, const void *X, const 
     if (p.T > 0 && wanted) { EQAT_REQUIRE(X); if (backward) EQAT_REQUIRE(dH); else EQAT_REQUIRE(H); }
     EQAT_ALIGNED(X); EQAT_ALIGNED(s); EQAT_ALIGNED(zpacked); EQAT_ALIGNED(dH); EQAT_ALIGNED(dY); EQAT_ALIGNED(H);
     if (!aligned(layer, prepared ? 256 : 16)) return EQAT_ERR_ALIGN;
-    const GatedWs l = gated_ws(p);
-    if (l.total > 0 && (ws == nullptr || ws_bytes < l.total)) return EQAT_ERR_WORKSPACE;
+    const size_t need = gated_ws(p);
+    if (need > 0 && (ws == nullptr || ws_bytes < need)) return EQAT_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return EQAT_ERR_ALIGN;
     if (p.T == 0 || !wanted) return EQAT_OK;
     hipStream_t st = (hipStream_t)stream;
-    char *w8 = (char *)ws;
     const PreparedLayout pl = prepared ? prepared_layout(p) : PreparedLayout{};
     const char *p8 = (const char *)layer;
     const float *zb = prepared ? (const float *)(p8 + pl.zb) : nullptr;
     const eqat::GatedOut out{H, dH, dY, kind};
-    if (eqat::gated_few_f32_applies(p)) { ProfScope ps(eqat::PK_F32, st); eqat::launch_gated_few_f32(p, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); return launch_status(); }
-    if (!p.act_bf16) {
-        qlinear_prepare_into(p, nullptr, s, zpacked, zb, nullptr, w8 + l.sz, nullptr, 0, st);
-        { ProfScope ps(eqat::PK_F32, st); eqat::launch_f32_fwd(p, true, X, prepared ? p8 + pl.codes : p8, s, w8 + l.sz, w8 + l.y, st); }
-        return backward ? eqat_gate_bwd(p.T, p.O / 2, EQAT_F32, kind, w8 + l.y, dH, dY, H, stream) : eqat_gate_fwd(p.T, p.O / 2, EQAT_F32, kind, w8 + l.y, H, stream);
-    }
+    if (!p.act_bf16) { ProfScope ps(eqat::PK_F32, st); eqat::launch_gated_f32(p, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); return launch_status(); }
     int tokens = 0;
     switch (gated_kernel(p, prepared, backward, &tokens)) {
     case GATED_GEMV: { ProfScope ps(eqat::PK_GEMV, st); eqat::launch_gemv_gated(p, kind, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, H, st); break; }
     case GATED_MID: { ProfScope ps(eqat::PK_GEMM_FWD, st); eqat::launch_mid_gated(p, tokens, out, X, prepared ? p8 + pl.codes : p8, s, zpacked, zb, st); break; }
     default: {
-        { ProfScope ps(eqat::PK_PREPARE, st); eqat::launch_gated_pairs(p, s, zpacked, zb, w8 + l.sz, st); }
+        { ProfScope ps(eqat::PK_PREPARE, st); eqat::launch_gated_pairs(p, s, zpacked, zb, ws, st); }
         ProfScope ps(eqat::PK_GEMM_FWD, st);
-        eqat::launch_tiles_gated(p, tokens, !prepared, out, X, prepared ? p8 + pl.codes : p8, w8 + l.sz, st);
+        eqat::launch_tiles_gated(p, tokens, !prepared, out, X, prepared ? p8 + pl.codes : p8, ws, st);
     }
     }
     return launch_status();
@@ -688,7 +670,7 @@ size_t eqat_gated_workspace_bytes(const eqat_desc *d)
     eqat_desc as_packed = *d;
     as_packed.w_dtype = EQAT_BF16;
     if (check_desc(&as_packed, true, &p) != EQAT_OK || p.O % 16 != 0) return 0;
-    return std::max<size_t>(gated_ws(p).total, 256);
+    return std::max<size_t>(gated_ws(p), 256);
 }
 
 eqat_status eqat_gated_fwd(const eqat_desc *d, int kind, const void *X, const uint8_t *Wpacked, const float *s, const uint8_t *zpacked, void *H, void *ws, size_t ws_bytes, void *stream)

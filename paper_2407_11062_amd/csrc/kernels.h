@@ -109,9 +109,8 @@ void launch_gated_pairs(const Problem &p, const float *s, const void *zpacked, c
 // codes in the working layout or, `dense`, as packed; (s, z) pairs
 void launch_tiles_gated(const Problem &p, int tokens, bool dense, const GatedOut &out, const void *X, const void *codes, const void *sz, hipStream_t st);
 
-// gated_f32.hip: a few tokens in fp32, the codes as packed; zpacked, or zero points as floats
-bool gated_few_f32_applies(const Problem &p);
-void launch_gated_few_f32(const Problem &p, const GatedOut &out, const void *X, const void *codes, const float *s, const void *zpacked, const float *z, hipStream_t st);
+// gated_f32.hip: fp32, the codes as packed; zpacked, or zero points as floats
+void launch_gated_f32(const Problem &p, const GatedOut &out, const void *X, const void *codes, const float *s, const void *zpacked, const float *z, hipStream_t st);
 
 // whether mulhi(segment, ceil(2^32 / (g / 32))) is the group of every segment of a row
 inline bool group_by_magic(const Problem &p) { return (p.I / 32) * (p.g / 32) < ((int64_t)1 << 32); }

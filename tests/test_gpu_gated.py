@@ -85,6 +85,13 @@ def test_fp32(bits, I, F, group):
         layer.check(T, dtype=torch.float32, kind=T % 2)
 
 
+# tiles of 16 x 16, 32 x 16, 32 x 32 and 64 x 32 tokens and rows, fewer segments than waves of a tile, groups of one segment to all of them
+@pytest.mark.parametrize("bits", (2, 3, 4))
+@pytest.mark.parametrize("T, I, F, group", [(17, 4096, 136, 64), (20, 256, 8000, 32), (130, 1056, 1000, 96), (600, 512, 2760, 128), (1000, 480, 5504, -1), (40, 64, 24, 64), (1030, 96, 4104, 96)])
+def test_tiles_in_fp32(T, I, F, group, bits):
+    Layer(T + I, I, F, bits, group).check(T, dtype=torch.float32, kind=bits % 2)
+
+
 @pytest.mark.parametrize("tokens, I, F, bits, group", [((1, 2, 3, 5, 16), 4096, 2816, 2, 64), ((1, 3, 6), 1056, 16424, 3, 32), ((1, 2, 3), 8192, 136, 4, 128), ((1, 3), 36352, 8, 2, 64),
                                                        ((1, 3), 36384, 8, 4, 32)])
 def test_few_tokens_in_fp32(tokens, I, F, bits, group):
