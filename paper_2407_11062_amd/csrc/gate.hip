@@ -1,6 +1,7 @@
 // The gate of the feed-forward, element by element, for projections of any kind: H = act(G) U and its backward pass, [G | U] the rows of the stacked projection.
 //
 // Bound by bytes (the activation is some twenty instructions an element): eight neighbouring elements of both halves to a lane.
+// 2048 tokens, F 28672, bf16: 60 us for 352 MB (5.9 TB/s), backward 102; 333 tokens, F 13824, 6.4 and 9.2.
 #include "layer.h"
 
 #include <algorithm>

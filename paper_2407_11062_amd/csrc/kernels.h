@@ -84,7 +84,7 @@ enum FwdKernel { FWD_TILES, FWD_MID, FWD_GEMV_WIDE, FWD_GEMV_ANY, FWD_GEMV_RUN, 
                  FWD_RELAY_MID /* the codes re-laid, then FWD_MID from the working layout */ };
 struct FwdRoute { FwdKernel kernel; int tokens, rows; };
 
-// ---- gemv.hip (E2E-QP forward for a few tokens, straight from the dense packed stream) -----------
+// ---- gemv.hip, gemv.h (E2E-QP forward for a few tokens, straight from the dense packed stream) -----------
 bool gemv_applies(const Problem &p);
 FwdRoute gemv_route(const Problem &p, bool floatz);         // where one of the two predicates holds
 // The same on the working layout and the (s, z) pairs, bitwise the same results: calls that hold those take it where this applies.
@@ -123,7 +123,7 @@ bool ksplit_item_for_test(const Problem &p, bool bt, const SkScratch &sk, int bl
 void launch_ksplit(const Problem &p, bool bt, const void *A, const void *codes, const void *sz, void *C, const SkScratch &sk,
                    int parts, hipStream_t st);
 
-// ---- gemm_mid.hip (forward for few output tiles) --------------------------------------------
+// ---- gemm_mid.hip, gemm_mid.h (forward for few output tiles) --------------------------------------------
 bool mid_applies(const Problem &p);
 FwdRoute mid_route(const Problem &p, bool from_packed);
 double mid_us(const Problem &p);                  // what it takes, as the rules of dispatch estimate it

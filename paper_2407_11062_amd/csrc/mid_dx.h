@@ -1,6 +1,6 @@
 // dX for few output tiles (short training batches): dX[T,I] = dY[T,O] * What[O,I].
 //
-// The forward's kernel for these sizes (gemm_mid.hip) with the weights turned round: eight waves are 2 (64 in-features each) x 4 (a
+// The forward's kernel for these sizes (gemm_mid.h) with the weights turned round: eight waves are 2 (64 in-features each) x 4 (a
 // quarter of every 128-wide step along O each), a wave owns its weights alone, tokens come two steps ahead straight into LDS (three
 // stages) and the barrier of a step, in its middle, waits for a count and not for the loads of the steps to come.
 // The contraction runs along O, the codes and the groups along I: a lane rebuilds one 32-code segment per step, with the step size of its own

@@ -1,4 +1,4 @@
-// Tiles of the kernels for few output tiles (gemm_mid.hip: forward, gemm_mid_dx.hip: dX): a workgroup of eight waves, 2 (64 weight rows each) x 4
+// Tiles of the kernels for few output tiles (gemm_mid.h: forward, gemm_mid_dx.hip: dX): a workgroup of eight waves, 2 (64 weight rows each) x 4
 // (a quarter of every K step each), computes 128 weight rows for a tile of tokens.
 #pragma once
 #include "common.h"

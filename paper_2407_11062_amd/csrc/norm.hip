@@ -6,6 +6,9 @@
 // Bound by bytes: every row is read once and kept in registers, eight neighbouring elements to a lane, LANES lanes to a row: part of a wave, a wave, or a workgroup that
 // meets in LDS once (a row's maximum, for 8 bits with one scale a row, a second time).  Sums, means and products are binary32; S is what stands in memory, so that the
 // backward pass, which makes rstd from S again, is that of what the forward computed.
+//
+// us over three states that take turns: 8192 rows of 8192 with a residual 93 (537 MB, 5.7 TB/s), their like of 4096 backward 49 (268 MB, 5.5); one row of 4096 2.7 in a graph, 515 rows of 5120 to 8 bits 6.3,
+// 333 rows of 4096 backward, fp32, 8.2 and 2.4 for the second launch.
 #include "layer.h"
 
 #include <algorithm>
