@@ -198,6 +198,14 @@ def _stream():
     return _raw_stream(_device())
 
 
+def _stream_of(t):
+    """The same for a call whose tensors are on t's device, which has to be the current one."""
+    device = _device()
+    if t.get_device() != device:
+        raise ValueError(f"tensors on {t.device}, the current device is {device}")
+    return _raw_stream(device)
+
+
 def _check(fn, status):
     if status != 0:
         raise EqatError(fn, status)
@@ -629,7 +637,7 @@ def eqat_norm_fwd(X, W, eps, R=None, group=0, want=None, out=None):
     else:
         group = -1
     w, w_type = _like_w(W, n)
-    status = lib().eqat_norm_fwd(_norm_ref(T, n, group, act, w_type, eps), _p(X), _like("R", R, shape, dtype), w, S, Y, codes, scales, _stream())
+    status = lib().eqat_norm_fwd(_norm_ref(T, n, group, act, w_type, eps), _p(X), _like("R", R, shape, dtype), w, S, Y, codes, scales, _stream_of(X))
     if status:
         _check("eqat_norm_fwd", status)
     return out
@@ -658,7 +666,7 @@ def eqat_norm_bwd(S, W, eps, dY, dS=None, want=("dX", "dW"), out=None, ws=None):
         if ws is None: ws = norm_workspace(T, n, dtype, S.device)
     w, w_type = _like_w(W, n)
     status = lib().eqat_norm_bwd(_norm_ref(T, n, -1, act, w_type, eps), _p(S), w, _like("dY", dY, shape, dtype), _like("dS", dS, shape, dtype), dX, dW,
-                                 _p(ws), 0 if ws is None else ws.numel(), _stream())
+                                 _p(ws), 0 if ws is None else ws.numel(), _stream_of(S))
     if status:
         _check("eqat_norm_bwd", status)
     return out
@@ -726,7 +734,7 @@ def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, 
     ref = rot.refs.get(dtype)
     if ref is None:
         raise TypeError(f"unsupported dtype {dtype}")
-    status = lib().eqat_rotary(ref, T, _p(positions), *_turned(rot, q, q_out, T, dtype), *_turned(rot, k, k_out, T, dtype), 1 if inverse else 0, _stream())
+    status = lib().eqat_rotary(ref, T, _p(positions), *_turned(rot, q, q_out, T, dtype), *_turned(rot, k, k_out, T, dtype), 1 if inverse else 0, _stream_of(positions))
     if status:
         _check("eqat_rotary", status)
     return q_out, k_out
@@ -738,7 +746,7 @@ def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q
         raise ValueError(f"heads of {rot.head_dim} in a cache of heads of {cache.head_dim}")
     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
     (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
-    status = lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[cache.dtype], *_turned(rot, q, q_out, batch.tokens, cache.dtype), kp, ks[0], vp, vs[0], _p(cache.pool), _stream())
+    status = lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[cache.dtype], *_turned(rot, q, q_out, batch.tokens, cache.dtype), kp, ks[0], vp, vs[0], _p(cache.pool), _stream_of(q))
     if status:
         _check("eqat_kv_rotary_write", status)
     return q_out
@@ -748,7 +756,7 @@ def eqat_gate_fwd(Y, kind=GATE_SILU, H=None):
     """H [tokens, F] = act(G) U of Y = [G | U] [tokens, 2 F]."""
     T, F = Y.shape[0], Y.shape[1] // 2
     H = torch.empty((T, F), dtype=Y.dtype, device=Y.device) if H is None else H
-    _check("eqat_gate_fwd", lib().eqat_gate_fwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype), _like("H", H, (T, F), Y.dtype), _stream()))
+    _check("eqat_gate_fwd", lib().eqat_gate_fwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype), _like("H", H, (T, F), Y.dtype), _stream_of(Y)))
     return H
 
 
@@ -760,7 +768,7 @@ def eqat_gate_bwd(Y, dH, kind=GATE_SILU, want=("dY",), out=None):
     if "H" in want and "H" not in out: out["H"] = torch.empty((T, F), dtype=Y.dtype, device=Y.device)
     get = lambda name: out.get(name) if name in want else None
     _check("eqat_gate_bwd", lib().eqat_gate_bwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype), _like("dH", dH, (T, F), Y.dtype), _like("dY", get("dY"), Y.shape, Y.dtype),
-                                                _like("H", get("H"), (T, F), Y.dtype), _stream()))
+                                                _like("H", get("H"), (T, F), Y.dtype), _stream_of(Y)))
     return out
 
 
@@ -810,7 +818,7 @@ def _gated(name, X, F, bits, group, layer, kind, dH, want, out, ws, prepared):
         back = _like("dY", back, y, dtype)
     back = () if dH is None else (_like("dH", dH, h, dtype), back)
     ws = gated_workspace(T, I, F, bits, group, dtype, prepared, X.device) if ws is None else ws
-    status = getattr(lib(), name)(_desc_ref(T, I, 2 * F, bits, group, _dt(X), BF16), kind, _p(X), *layer, *back, H, _p(ws), ws.numel(), _stream())
+    status = getattr(lib(), name)(_desc_ref(T, I, 2 * F, bits, group, _dt(X), BF16), kind, _p(X), *layer, *back, H, _p(ws), ws.numel(), _stream_of(X))
     if status:
         _check(name, status)
     return out

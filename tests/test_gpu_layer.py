@@ -101,3 +101,23 @@ def test_a_serving_step_replayed():
             at += n
         x.copy_(torch.randn((B, hidden), device="cuda"))
         lens.add_(1)
+
+
+def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch):
+    """a launch would go to the current device's stream with addresses of the other one; nothing is launched here"""
+    X, w = torch.ones((2, 64), dtype=torch.bfloat16, device="cuda"), torch.ones(64, device="cuda")
+    q, pos = torch.ones((2, 1, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    rot, layer = eq.Rotary(eq.rotary_frequencies(64).cuda(), 64), eq.eqat_pack(torch.ones((32, 64), device="cuda"), torch.ones((32, 1), device="cuda"), torch.zeros((32, 1), device="cuda"), 2, 64)
+    s, cache = torch.ones((32, 1), device="cuda"), eq.KvCache(1, 64, 64, 32, 1)
+    batch = eq.KvBatch(torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.full((1,), 2, dtype=torch.int32, device="cuda"), torch.tensor([0, 2], dtype=torch.int32, device="cuda"), tokens=2, max_new=2, max_len=2)
+    ready = eq.eqat_qlinear_prepare(*layer, 64, 2, 64)
+    dH = torch.ones((2, 16), dtype=torch.bfloat16, device="cuda")
+    before = cache.pool.clone()
+    monkeypatch.setattr(eq, "_device", lambda: 1)
+    for call in (lambda: eq.eqat_norm_fwd(X, w, 1e-5), lambda: eq.eqat_norm_bwd(X, w, 1e-5, X), lambda: eq.eqat_rotary(rot, pos, q), lambda: eq.eqat_kv_rotary_write(cache, batch, rot, q, q, q),
+                 lambda: eq.eqat_gate_fwd(X), lambda: eq.eqat_gate_bwd(X, X[:, :32].contiguous()), lambda: eq.eqat_gated_fwd(X, layer[0], s, layer[1], 2, 64),
+                 lambda: eq.eqat_gated_bwd(X, layer[0], s, layer[1], dH, 2, 64), lambda: eq.eqat_gated_fwd_prepared(X, ready, s, 16, 2, 64), lambda: eq.eqat_gated_bwd_prepared(X, ready, s, dH, 2, 64)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    torch.cuda.synchronize()
+    assert torch.equal(cache.pool, before)
