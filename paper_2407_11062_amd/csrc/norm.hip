@@ -170,7 +170,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const No
     constexpr int kThreads = LANES > 256 ? LANES : 256, kRows = kThreads / LANES;
     constexpr bool kHold = LANES < 1024;                      // 16 waves leave no registers for w and dw (in LDS instead), and dS is fetched where it is wanted
     __shared__ float part[2][2][kThreads / 64];
-    extern __shared__ __attribute__((aligned(16))) float sums[];              // [width], where several rows are in the workgroup, or rows are wide, and dw is wanted
+    extern __shared__ __attribute__((aligned(16))) float sums[];              // [kRows][width], where several rows are in the workgroup, or rows are wide, and dw is wanted
     const int lane = threadIdx.x % LANES;
     float w[kHold ? NV : 1][8], dw[kHold ? NV : 1][8];
 #pragma unroll
@@ -261,20 +261,23 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const No
     }
     if (a.part == nullptr) return;
     float *to = a.part + (int64_t)blockIdx.x * a.width;
-    if constexpr (kRows > 1) {                                // the rows' parts one after the other: a fixed order
-        for (int v = 0; v < kRows; ++v) {
-            if ((int)threadIdx.x / LANES == v) {
+    if constexpr (kRows > 1) {                                // the rows' parts meet in a fixed order
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int at = (k * LANES + lane) * 8 + e;
-                        if (at < a.width) sums[at] = v == 0 ? dw[kHold ? k : 0][e] : sums[at] + dw[kHold ? k : 0][e];
-                    }
+        for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * 8;
+            if (at < a.width) {
+                Eight<float> o;
+                o.set(dw[kHold ? k : 0]);
+                o.store(sums + (int)threadIdx.x / LANES * a.width + at);
             }
-            __syncthreads();
         }
-        for (int i = threadIdx.x; i < a.width; i += kThreads) to[i] = sums[i];
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.width; i += kThreads) {
+            float v = sums[i];
+#pragma unroll
+            for (int k = 1; k < kRows; ++k) v += sums[k * a.width + i];
+            to[i] = v;
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -392,7 +395,7 @@ void launch_norm_bwd(const NormBwd &n, void *ws, hipStream_t st)
     a.width = n.width; a.w_bf16 = n.w_bf16; a.eps = n.eps; a.per_width = 1.0f / (float)n.width;
     if (blocks > 0) by_width<true>(n.rows, n.width, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, N = decltype(nv)::value, kThreads = L > 256 ? L : 256;
-        const size_t lds = (L < 256 || L == 1024) && n.dw != nullptr ? (size_t)n.width * sizeof(float) : 0;
+        const size_t lds = (L < 256 || L == 1024) && n.dw != nullptr ? (size_t)(kThreads / L) * n.width * sizeof(float) : 0;          // up to 16 KiB; 128 KiB
         if constexpr (L == 1024) {      // more than the default limit: once per device
             static std::atomic<uint64_t> allowed{0};
             int dev = 0;
