@@ -147,7 +147,7 @@ template <int BITS, bool FLOATZ, int TT> __global__ __launch_bounds__(64 * kWave
 // ---- more tokens: v_mfma_f32_32x32x2_f32, v_mfma_f32_16x16x4_f32 ---------------------------------------
 // A workgroup's tile is MB blocks of R tokens (32 or 16) of R rows of the gate and their partners, which meet in the same registers.  Four waves share it, each a run of segments of 32 inputs, of which a
 // group of R lanes multiplies a part; the next segment's inputs and codes, and step sizes and zero points where its group begins, are on their way while one is multiplied.  Operands go straight from memory
-// into registers; what bounds it is the matrix cores (512 tokens, 4096 -> 2 x 11008, 2 bit: 763 us, 121 TFLOP/s of 157), with few tokens the lines that a wave's lanes touch for it.  A weight is
+// into registers; what bounds it is the matrix cores (512 tokens, 4096 -> 2 x 11008, 2 bit: 763 us, 121 TFLOP/s of 157), where tiles are few the length of a tile's chain.  A weight is
 // (q - z) s, rounded once.  Against the fp32 GEMM, a pairing launch before and a gate behind it: 512 tokens 918 -> 763 us, 64 193 -> 127, 17 (4 bit) 173 -> 70; 105 tokens, 6016 -> 2 x 656, backward 54 -> 43; 16
 // tokens, 1024 -> 2 x 2752 14.3 -> 8.9.
 struct TilesArgs {
