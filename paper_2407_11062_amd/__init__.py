@@ -198,14 +198,6 @@ def _stream():
     return _raw_stream(_device())
 
 
-def _stream_of(t):
-    """The same for a call whose tensors are on t's device, which has to be the current one."""
-    device = _device()
-    if t.get_device() != device:
-        raise ValueError(f"tensors on {t.device}, the current device is {device}")
-    return _raw_stream(device)
-
-
 def _check(fn, status):
     if status != 0:
         raise EqatError(fn, status)
@@ -585,47 +577,85 @@ def _norm_ref(tokens, width, group, act_dtype, w_dtype, eps):
     return ctypes.byref(NormDesc(tokens, _i32("width", width), _i32("group", group), act_dtype, w_dtype, eps))
 
 
-# As above, what happens here is what bounds the smallest calls: shapes are compared as they are, and what a call goes by is looked up once.
-def _like(name, t, shape, dtype):
+# As above, what happens here is what bounds the smallest calls (a launch is 3 us of their 6): shapes are compared as they are, what a call goes by is looked up once, and the calls of a decoding step
+# look at their tensors in place.  All tensors of a call are on one device, which has to be the current one: the call goes to its current stream.
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _unlike(name, t, shape, dtype, device):
+    raise ValueError(f"{name}: expected a contiguous {dtype} tensor {list(shape)} on device {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+
+
+def _stream_at(device):
+    """The current stream of the device that a call's tensors are on (-1: the host)."""
+    if device < 0 or device != _device():
+        raise ValueError(f"tensors of device {device} (-1: the host) that is not the current device")
+    return _raw_stream(device)
+
+
+def _like(name, t, shape, dtype, device):
     """The pointer of a tensor whose shape and type the call goes by; None stays None."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} device tensor {list(shape)}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        _unlike(name, t, shape, dtype, device)
     return t.data_ptr()
 
 
-def _like_w(W, n):
+def _like_w(W, n, device):
     """(pointer, type) of a norm's weights; None stays None."""
     if W is None:
         return None, F32
-    code = _dt(W)
-    return _like("W", W, (n,), W.dtype), code
+    dtype = W.dtype
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    if W.shape != (n,) or W.get_device() != device or not W.is_contiguous():
+        _unlike("W", W, (n,), dtype, device)
+    return W.data_ptr(), code
 
 
-def _codes_ptr(codes, shape):
+def _codes_ptr(codes, shape, device):
     if codes.dtype is not torch.uint8 and codes.dtype is not torch.float8_e4m3fn:
         raise ValueError(f"codes: expected float8_e4m3fn or uint8, got {codes.dtype}")
-    return _like("codes", codes, shape, codes.dtype)
+    return _like("codes", codes, shape, codes.dtype, device)
+
+
+_Y, _S_AND_Y, _CODED, _S_AND_CODED = ("Y",), ("S", "Y"), ("codes",), ("S", "codes")
 
 
 def eqat_norm_fwd(X, W, eps, R=None, group=0, want=None, out=None):
     """Root-mean-square norm of S = X + R (R None: of X) over the rows of [tokens, width]; W [width] or None.  `want`: which of "S", "Y", "codes" (float8_e4m3fn, with "scales", one
     for `group` neighbouring elements, -1: a row) to make, by default Y, or the codes where a group is given, and S where R is; tensors in `out` are filled."""
-    shape, dtype, act = X.shape, X.dtype, _dt(X)
+    shape, dtype, device = X.shape, X.dtype, X.get_device()
     T, n = shape
+    act = _CODES.get(dtype)
+    if act is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    if not X.is_contiguous():
+        _unlike("X", X, shape, dtype, device)
     if want is None:
-        want = (("S",) if R is not None else ()) + (("codes",) if group else ("Y",))
-    out = {} if out is None else out
-    S = Y = codes = scales = None
+        want = (_Y if R is None else _S_AND_Y) if not group else _CODED if R is None else _S_AND_CODED
+    if out is None: out = {}
+    r = s = y = codes = scales = None
+    if R is not None:
+        if R.shape != shape or R.dtype is not dtype or R.get_device() != device or not R.is_contiguous():
+            _unlike("R", R, shape, dtype, device)
+        r = R.data_ptr()
     if "S" in want:
         S = out.get("S")
-        if S is None: S = out["S"] = torch.empty_like(X)
-        S = _like("S", S, shape, dtype)
+        if S is None:
+            S = out["S"] = torch.empty_like(X)
+        elif S.shape != shape or S.dtype is not dtype or S.get_device() != device or not S.is_contiguous():
+            _unlike("S", S, shape, dtype, device)
+        s = S.data_ptr()
     if "Y" in want:
         Y = out.get("Y")
-        if Y is None: Y = out["Y"] = torch.empty_like(X)
-        Y = _like("Y", Y, shape, dtype)
+        if Y is None:
+            Y = out["Y"] = torch.empty_like(X)
+        elif Y.shape != shape or Y.dtype is not dtype or Y.get_device() != device or not Y.is_contiguous():
+            _unlike("Y", Y, shape, dtype, device)
+        y = Y.data_ptr()
     if "codes" in want or "scales" in want:
         group = _i32("group", group)
         if group == 0:
@@ -633,11 +663,11 @@ def eqat_norm_fwd(X, W, eps, R=None, group=0, want=None, out=None):
         per = n // group if group > 0 else 1
         if "codes" not in out: out["codes"] = torch.empty((T, n), dtype=torch.float8_e4m3fn, device=X.device)
         if "scales" not in out: out["scales"] = torch.empty((T, per), dtype=torch.float32, device=X.device)
-        codes, scales = _codes_ptr(out["codes"], shape), _like("scales", out["scales"], (T, per), torch.float32)
+        codes, scales = _codes_ptr(out["codes"], shape, device), _like("scales", out["scales"], (T, per), torch.float32, device)
     else:
         group = -1
-    w, w_type = _like_w(W, n)
-    status = lib().eqat_norm_fwd(_norm_ref(T, n, group, act, w_type, eps), _p(X), _like("R", R, shape, dtype), w, S, Y, codes, scales, _stream_of(X))
+    w, w_type = _like_w(W, n, device)
+    status = lib().eqat_norm_fwd(_norm_ref(T, n, group, act, w_type, eps), X.data_ptr(), r, w, s, y, codes, scales, _stream_at(device))
     if status:
         _check("eqat_norm_fwd", status)
     return out
@@ -651,22 +681,23 @@ def norm_workspace(tokens, width, dtype=torch.bfloat16, device="cuda") -> torch.
 
 def eqat_norm_bwd(S, W, eps, dY, dS=None, want=("dX", "dW"), out=None, ws=None):
     """Gradients of eqat_norm_fwd from S (what it left, or its X): dX (also that of R) in S's type, dW fp32 [width].  dS: the gradient that reaches S along the residual."""
-    shape, dtype, act = S.shape, S.dtype, _dt(S)
+    shape, dtype, device = S.shape, S.dtype, S.get_device()
     T, n = shape
+    act = _dt(S)
     out = {} if out is None else out
     dX = dW = None
     if "dX" in want:
         dX = out.get("dX")
         if dX is None: dX = out["dX"] = torch.empty_like(S)
-        dX = _like("dX", dX, shape, dtype)
+        dX = _like("dX", dX, shape, dtype, device)
     if "dW" in want:
         dW = out.get("dW")
         if dW is None: dW = out["dW"] = torch.empty(n, dtype=torch.float32, device=S.device)
-        dW = _like("dW", dW, (n,), torch.float32)
+        dW = _like("dW", dW, (n,), torch.float32, device)
         if ws is None: ws = norm_workspace(T, n, dtype, S.device)
-    w, w_type = _like_w(W, n)
-    status = lib().eqat_norm_bwd(_norm_ref(T, n, -1, act, w_type, eps), _p(S), w, _like("dY", dY, shape, dtype), _like("dS", dS, shape, dtype), dX, dW,
-                                 _p(ws), 0 if ws is None else ws.numel(), _stream_of(S))
+    w, w_type = _like_w(W, n, device)
+    status = lib().eqat_norm_bwd(_norm_ref(T, n, -1, act, w_type, eps), _like("S", S, shape, dtype, device), w, _like("dY", dY, shape, dtype, device), _like("dS", dS, shape, dtype, device), dX, dW,
+                                 _p(ws), 0 if ws is None else ws.numel(), _stream_at(device))
     if status:
         _check("eqat_norm_bwd", status)
     return out
@@ -699,42 +730,52 @@ class Rotary:
 
 
 @functools.lru_cache(maxsize=1024)
-def _rows_of(shape, stride, tokens, head_dim):
-    """(heads, address of the {token, head} strides in memory, their array) of a [tokens, heads, head_dim] tensor; the cache is by value"""
+def _both_rows(shape, stride, out_stride, tokens, head_dim):
+    """(heads, addresses of the {token, head} strides in memory of a [tokens, heads, head_dim] tensor and of where it goes, their arrays); the cache is by value"""
     if len(shape) != 3:
         raise ValueError("expected [tokens, heads, head_dim]")
-    at, both = _kv_strides(shape, stride, tokens, shape[1], head_dim)
-    return shape[1], at, both
+    here, there = (_kv_strides(shape, x, tokens, shape[1], head_dim) for x in (stride, out_stride))
+    return shape[1], here[0], there[0], here[1], there[1]
 
 
-def _turned(rot, t, out, tokens, dtype):
+_NOTHING = (None, None, 0, None, None)
+
+
+def _turned(t, out, tokens, dtype, head_dim, device):
     """(pointer, strides, heads, pointer, strides) of what is turned and of where it goes"""
-    if t is None:
-        if out is not None:
-            raise ValueError("an output without its input")
-        return None, None, 0, None, None
-    if t.dtype is not dtype or out.dtype is not dtype or not t.is_cuda or not out.is_cuda:
-        raise ValueError(f"expected {dtype} device tensors, got {t.dtype} on {t.device} and {out.dtype} on {out.device}")
-    if out.shape != t.shape:
-        raise ValueError(f"expected {list(t.shape)}, got {list(out.shape)}")
-    heads, at, _ = _rows_of(t.shape, t.stride(), tokens, rot.head_dim)
-    return t.data_ptr(), at, heads, out.data_ptr(), _rows_of(out.shape, out.stride(), tokens, rot.head_dim)[1]
+    shape = t.shape
+    if t.dtype is not dtype or out.dtype is not dtype or t.get_device() != device or out.get_device() != device:
+        raise ValueError(f"expected {dtype} tensors on device {device}, got {t.dtype} on {t.device} and {out.dtype} on {out.device}")
+    if out.shape != shape:
+        raise ValueError(f"expected {list(shape)}, got {list(out.shape)}")
+    heads, here, there, _, _ = _both_rows(shape, t.stride(), out.stride(), tokens, head_dim)
+    return t.data_ptr(), here, heads, out.data_ptr(), there
 
 
 def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, inverse=False):
     """(q, k) [tokens, heads, head_dim] (any token and head strides) turned by their tokens' positions (int32 [tokens]); into q_out, k_out (which may be q and k themselves)."""
+    device = positions.get_device()
     if positions.dtype is not torch.int32 or positions.dim() != 1:
         raise TypeError("positions are int32 [tokens]")
+    if not positions.is_contiguous():
+        _unlike("positions", positions, positions.shape, torch.int32, device)
+    if (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("an output without its input")
     T, like = positions.numel(), q if q is not None else k
     if like is None:
         return None, None
-    if q is not None and q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None: k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    dtype = like.dtype
+    dtype, head_dim = like.dtype, rot.head_dim
     ref = rot.refs.get(dtype)
     if ref is None:
         raise TypeError(f"unsupported dtype {dtype}")
-    status = lib().eqat_rotary(ref, T, _p(positions), *_turned(rot, q, q_out, T, dtype), *_turned(rot, k, k_out, T, dtype), 1 if inverse else 0, _stream_of(positions))
+    of_q = of_k = _NOTHING
+    if q is not None:
+        if q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        of_q = _turned(q, q_out, T, dtype, head_dim, device)
+    if k is not None:
+        if k_out is None: k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        of_k = _turned(k, k_out, T, dtype, head_dim, device)
+    status = lib().eqat_rotary(ref, T, positions.data_ptr(), *of_q, *of_k, 1 if inverse else 0, _stream_at(device))
     if status:
         _check("eqat_rotary", status)
     return q_out, k_out
@@ -742,11 +783,15 @@ def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, 
 
 def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q_out=None):
     """The newest tokens' queries turned (returned, into q_out if given, which may be q itself), their keys turned and values into the cache: eqat_rotary and eqat_kv_write in one launch."""
-    if rot.head_dim != cache.head_dim:
-        raise ValueError(f"heads of {rot.head_dim} in a cache of heads of {cache.head_dim}")
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    (kp, ks), (vp, vs) = _kv_rows(cache, batch, k, cache.heads), _kv_rows(cache, batch, v, cache.heads)
-    status = lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[cache.dtype], *_turned(rot, q, q_out, batch.tokens, cache.dtype), kp, ks[0], vp, vs[0], _p(cache.pool), _stream_of(q))
+    device, dtype, tokens, head_dim = cache.pool.get_device(), cache.dtype, batch.tokens, cache.head_dim
+    if rot.head_dim != head_dim:
+        raise ValueError(f"heads of {rot.head_dim} in a cache of heads of {head_dim}")
+    if q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k.dtype is not dtype or v.dtype is not dtype or k.get_device() != device or v.get_device() != device:
+        raise ValueError(f"expected {dtype} tensors on device {device}, got {k.dtype} on {k.device} and {v.dtype} on {v.device}")
+    ks, vs = _kv_strides(k.shape, k.stride(), tokens, cache.heads, head_dim), _kv_strides(v.shape, v.stride(), tokens, cache.heads, head_dim)
+    status = lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[dtype], *_turned(q, q_out, tokens, dtype, head_dim, device), k.data_ptr(), ks[0], v.data_ptr(), vs[0], cache.pool.data_ptr(),
+                                        _stream_at(device))
     if status:
         _check("eqat_kv_rotary_write", status)
     return q_out
@@ -754,21 +799,21 @@ def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q
 
 def eqat_gate_fwd(Y, kind=GATE_SILU, H=None):
     """H [tokens, F] = act(G) U of Y = [G | U] [tokens, 2 F]."""
-    T, F = Y.shape[0], Y.shape[1] // 2
+    T, F, device = Y.shape[0], Y.shape[1] // 2, Y.get_device()
     H = torch.empty((T, F), dtype=Y.dtype, device=Y.device) if H is None else H
-    _check("eqat_gate_fwd", lib().eqat_gate_fwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype), _like("H", H, (T, F), Y.dtype), _stream_of(Y)))
+    _check("eqat_gate_fwd", lib().eqat_gate_fwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype, device), _like("H", H, (T, F), Y.dtype, device), _stream_at(device)))
     return H
 
 
 def eqat_gate_bwd(Y, dH, kind=GATE_SILU, want=("dY",), out=None):
     """The gradient dY of Y = [G | U] from that of H, and H itself where it is wanted."""
-    T, F = Y.shape[0], Y.shape[1] // 2
+    T, F, device = Y.shape[0], Y.shape[1] // 2, Y.get_device()
     out = {} if out is None else out
     if "dY" in want and "dY" not in out: out["dY"] = torch.empty_like(Y)
     if "H" in want and "H" not in out: out["H"] = torch.empty((T, F), dtype=Y.dtype, device=Y.device)
-    get = lambda name: out.get(name) if name in want else None
-    _check("eqat_gate_bwd", lib().eqat_gate_bwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype), _like("dH", dH, (T, F), Y.dtype), _like("dY", get("dY"), Y.shape, Y.dtype),
-                                                _like("H", get("H"), (T, F), Y.dtype), _stream_of(Y)))
+    get = lambda name, shape: _like(name, out.get(name) if name in want else None, shape, Y.dtype, device)
+    _check("eqat_gate_bwd", lib().eqat_gate_bwd(T, F, _dt(Y), int(kind), _like("Y", Y, (T, 2 * F), Y.dtype, device), _like("dH", dH, (T, F), Y.dtype, device), get("dY", Y.shape), get("H", (T, F)),
+                                                _stream_at(device)))
     return out
 
 
@@ -787,9 +832,11 @@ def _packed_ok(w, s, z, I, bits, group):
 
 
 def _packed_layer(X, Wpacked, s, zpacked, bits, group):
-    if Wpacked.dtype is not torch.uint8 or zpacked.dtype is not torch.uint8 or s.dtype is not torch.float32 or not _packed_ok(Wpacked.shape, s.shape, zpacked.shape, X.shape[1], bits, group):
-        raise ValueError(f"not a packed layer of {X.shape[1]} inputs at {bits} bits in groups of {group}: codes {list(Wpacked.shape)}, step sizes {list(s.shape)}, zero points {list(zpacked.shape)}")
-    return _p(Wpacked), _p(s), _p(zpacked)
+    if (Wpacked.dtype is not torch.uint8 or zpacked.dtype is not torch.uint8 or s.dtype is not torch.float32 or not _packed_ok(Wpacked.shape, s.shape, zpacked.shape, X.shape[1], bits, group)
+            or not (Wpacked.is_contiguous() and zpacked.is_contiguous() and s.is_contiguous()) or not Wpacked.get_device() == zpacked.get_device() == s.get_device() == X.get_device()):
+        raise ValueError(f"not a contiguous packed layer of {X.shape[1]} inputs at {bits} bits in groups of {group} on {X.device}: codes {list(Wpacked.shape)}, step sizes {list(s.shape)}, "
+                         f"zero points {list(zpacked.shape)}")
+    return Wpacked.data_ptr(), s.data_ptr(), zpacked.data_ptr()
 
 
 @functools.lru_cache(maxsize=1024)
@@ -799,26 +846,36 @@ def _prepared_bytes(F, I, bits, group, act_dtype):
 
 def _prepared_layer(X, prepared, s, F, bits, group):
     I = X.shape[1]
-    if prepared.dtype is not torch.uint8 or prepared.numel() < _prepared_bytes(F, I, bits, group, _dt(X)) or s.dtype is not torch.float32 or s.shape != (2 * F, _groups(I, group)):
-        raise ValueError(f"not a prepared layer of {I} inputs and 2 x {F} outputs at {bits} bits in groups of {group}: {prepared.numel()} bytes, step sizes {list(s.shape)}")
-    return _p(prepared), _p(s)
+    if (prepared.dtype is not torch.uint8 or prepared.numel() < _prepared_bytes(F, I, bits, group, _dt(X)) or s.dtype is not torch.float32 or s.shape != (2 * F, _groups(I, group))
+            or not (prepared.is_contiguous() and s.is_contiguous()) or not prepared.get_device() == s.get_device() == X.get_device()):
+        raise ValueError(f"not a contiguous prepared layer of {I} inputs and 2 x {F} outputs at {bits} bits in groups of {group} on {X.device}: {prepared.numel()} bytes, step sizes {list(s.shape)}")
+    return prepared.data_ptr(), s.data_ptr()
 
 
 def _gated(name, X, F, bits, group, layer, kind, dH, want, out, ws, prepared):
-    T, I = X.shape
-    dtype, h, y = X.dtype, (T, F), (T, 2 * F)
-    H = back = None
+    (T, I), dtype, device = X.shape, X.dtype, X.get_device()
+    act = _CODES.get(dtype)
+    if act is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    if not X.is_contiguous():
+        _unlike("X", X, X.shape, dtype, device)
+    h = None
+    back = ()
     if "H" in want:
         H = out.get("H")
-        if H is None: H = out["H"] = torch.empty(h, dtype=dtype, device=X.device)
-        H = _like("H", H, h, dtype)
-    if "dY" in want:
-        back = out.get("dY")
-        if back is None: back = out["dY"] = torch.empty(y, dtype=dtype, device=X.device)
-        back = _like("dY", back, y, dtype)
-    back = () if dH is None else (_like("dH", dH, h, dtype), back)
-    ws = gated_workspace(T, I, F, bits, group, dtype, prepared, X.device) if ws is None else ws
-    status = getattr(lib(), name)(_desc_ref(T, I, 2 * F, bits, group, _dt(X), BF16), kind, _p(X), *layer, *back, H, _p(ws), ws.numel(), _stream_of(X))
+        if H is None:
+            H = out["H"] = torch.empty((T, F), dtype=dtype, device=X.device)
+        elif H.shape != (T, F) or H.dtype is not dtype or H.get_device() != device or not H.is_contiguous():
+            _unlike("H", H, (T, F), dtype, device)
+        h = H.data_ptr()
+    if dH is not None:
+        dY = None
+        if "dY" in want:
+            dY = out.get("dY")
+            if dY is None: dY = out["dY"] = torch.empty((T, 2 * F), dtype=dtype, device=X.device)
+        back = (_like("dH", dH, (T, F), dtype, device), _like("dY", dY, (T, 2 * F), dtype, device))
+    if ws is None: ws = gated_workspace(T, I, F, bits, group, dtype, prepared, X.device)
+    status = getattr(lib(), name)(_desc_ref(T, I, 2 * F, bits, group, act, BF16), kind, X.data_ptr(), *layer, *back, h, _p(ws), ws.numel(), _stream_at(device))
     if status:
         _check(name, status)
     return out
