@@ -723,7 +723,7 @@ class Rotary:
     def __init__(self, frequencies, head_dim, interleaved=False, amplitude=1.0):
         if frequencies.dtype != torch.float32 or frequencies.dim() != 1:
             raise TypeError("frequencies are fp32 [pairs]")
-        self.frequencies, self.head_dim = frequencies, _i32("head_dim", head_dim)          # the tensor must outlive the pointer
+        self.frequencies, self.head_dim, self.device = frequencies, _i32("head_dim", head_dim), frequencies.get_device()          # the tensor must outlive the pointer
         at, part = _p(frequencies), 2 * frequencies.numel()
         self.descs = {dt: RotaryDesc(at, self.head_dim, part, 1 if interleaved else 0, code, float(amplitude)) for dt, code in ((torch.float32, F32), (torch.bfloat16, BF16))}
         self.refs = {dt: ctypes.byref(d) for dt, d in self.descs.items()}
@@ -759,6 +759,8 @@ def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, 
         raise TypeError("positions are int32 [tokens]")
     if not positions.is_contiguous():
         _unlike("positions", positions, positions.shape, torch.int32, device)
+    if rot.device != device:
+        raise ValueError(f"frequencies on device {rot.device}, tensors on {device}")
     if (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("an output without its input")
     T, like = positions.numel(), q if q is not None else k
@@ -784,6 +786,8 @@ def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, 
 def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q_out=None):
     """The newest tokens' queries turned (returned, into q_out if given, which may be q itself), their keys turned and values into the cache: eqat_rotary and eqat_kv_write in one launch."""
     device, dtype, tokens, head_dim = cache.pool.get_device(), cache.dtype, batch.tokens, cache.head_dim
+    if rot.device != device:
+        raise ValueError(f"frequencies on device {rot.device}, tensors on {device}")
     if rot.head_dim != head_dim:
         raise ValueError(f"heads of {rot.head_dim} in a cache of heads of {head_dim}")
     if q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

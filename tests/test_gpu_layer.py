@@ -119,5 +119,10 @@ def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch)
                  lambda: eq.eqat_gated_bwd(X, layer[0], s, layer[1], dH, 2, 64), lambda: eq.eqat_gated_fwd_prepared(X, ready, s, 16, 2, 64), lambda: eq.eqat_gated_bwd_prepared(X, ready, s, dH, 2, 64)):
         with pytest.raises(ValueError, match="current device"):
             call()
+    monkeypatch.undo()
+    rot.device = 1                                    # frequencies elsewhere
+    for call in (lambda: eq.eqat_rotary(rot, pos, q), lambda: eq.eqat_kv_rotary_write(cache, batch, rot, q, q, q)):
+        with pytest.raises(ValueError, match="frequencies"):
+            call()
     torch.cuda.synchronize()
     assert torch.equal(cache.pool, before)
