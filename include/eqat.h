@@ -484,6 +484,7 @@ eqat_status eqat_kv_attention(const eqat_kv_desc *d, const eqat_kv_batch *b, con
  *   All tensors are contiguous: X, R, S, Y, dY, dS, dX [tokens, width] in act_dtype, w [width] in w_dtype, codes [tokens, width] bytes, scales [tokens, width / group] and dw [width]
  *   fp32, of any size (offsets are 64 bits).  S may be X or R itself, and so may Y (not the one that S is), dX may be dY, dS or S (a row is read before it is written); no other overlap.
  *   Sums, means and products are binary32: a row whose squares pass binary32 gives zeros, a NaN or infinity stays in its row (and in dw).
+ *   With eps = 0 (allowed) a row of zeros gives NaN, as the formula does, and one whose mean square is below 2^-126 (elements around 2^-63 and less) loses bits of it.
  *   width: a multiple of 8, up to 32768 (a multiple of `group` where codes are asked for); group 32, 64, 128, 256 or 512, or -1: one scale a row.
  *   tokens >= 0 of any number below 2^31; none leaves dw at zero.  eps >= 0, finite (EQAT_ERR_HYPER otherwise).
  *   ws: eqat_norm_workspace_bytes(d) bytes, 256-byte aligned, wanted for dw only; contents undefined before and after; calls that share one must not overlap in time.

@@ -224,7 +224,8 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_bwd(const No
 #pragma unroll
             for (int v = 1; v < LANES / 64; ++v) { ss += part[turn][0][v]; es += part[turn][1][v]; }
         }
-        const float rstd = 1.0f / sqrtf(__builtin_fmaf(ss, a.per_width, a.eps)), c = es * a.per_width * rstd * rstd;
+        // a row that is not there shares a workgroup with others and adds to their dw: its terms are 0 only while rstd is finite, which with eps = 0 the square root of no sum is not
+        const float rstd = kRows > 1 && !there ? 0.0f : 1.0f / sqrtf(__builtin_fmaf(ss, a.per_width, a.eps)), c = es * a.per_width * rstd * rstd;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = (k * LANES + lane) * 8;
