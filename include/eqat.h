@@ -478,7 +478,8 @@ eqat_status eqat_kv_attention(const eqat_kv_desc *d, const eqat_kv_batch *b, con
  * Root-mean-square norm with the residual's addition.
  *   S = X + R, rounded to the activations' type (R NULL: S = X);   Y = w S / sqrt(mean S^2 + eps), the mean over the row's `width` elements of S as it stands (w NULL: ones)
  *   codes, scales   Y in 8 bits instead of, or beside, Y: of `group` neighbouring elements scale = max(max |Y| / 448, 2^-126), codes = e4m3(Y / scale) (the finite-only 8-bit
- *                   float with 4 exponent bits, largest 448), from Y before it is rounded; to nearest, ties to even.
+ *                   float with 4 exponent bits, largest 448), from Y before it is rounded; to nearest, ties to even (max / 448 and the
+ *                   quotient are binary32, each rounded once).
  *   Backward, of S (what the forward left in S, or its X without R), the gradients dY of Y and dS of S (along the residual; NULL: none):
  *                   dX = dS + rstd (w dY - S rstd^2 mean(w dY S)),  which is the gradient of X and of R;   dw = sum over the rows of dY S rstd,   rstd = 1 / sqrt(mean S^2 + eps).
  *   All tensors are contiguous: X, R, S, Y, dY, dS, dX [tokens, width] in act_dtype, w [width] in w_dtype, codes [tokens, width] bytes, scales [tokens, width / group] and dw [width]

@@ -149,12 +149,15 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_fwd(const No
         for (int k = 0; k < NV; ++k) {
             const int at = (k * LANES + lane) * 8;
             if (!there || at >= a.width) continue;
-            const float scale = most_of(most[k] / kFp8Most, kLeastScale), by = 1.0f / scale;
+            const float scale = most_of(most[k] / kFp8Most, kLeastScale), by = 1.0f / scale, finite = scale < __builtin_inff() ? scale : 0.0f;
+            // the quotient y / scale: the product with the reciprocal and, by what that leaves of y, put right (an infinite scale: 0 or NaN as it is; -0 stays).  The product alone falls to the other
+            // side of one tie in some 20000 elements; 515 rows of 5120, bf16, in a graph 4.2 -> 4.4 us, 8192 rows of 8192 44.6 -> 46.7
+            auto quotient_of = [&](float v) { const float q = v * by; return __builtin_fmaf(-__builtin_fmaf(q, finite, -v), by, q); };
             uintx2 code;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][4 * h] * by, y[k][4 * h + 1] * by, 0, false);
-                v = __builtin_amdgcn_cvt_pk_fp8_f32(y[k][4 * h + 2] * by, y[k][4 * h + 3] * by, v, true);
+                int v = __builtin_amdgcn_cvt_pk_fp8_f32(quotient_of(y[k][4 * h]), quotient_of(y[k][4 * h + 1]), 0, false);
+                v = __builtin_amdgcn_cvt_pk_fp8_f32(quotient_of(y[k][4 * h + 2]), quotient_of(y[k][4 * h + 3]), v, true);
                 code[h] = (uint32_t)v;
             }
             *reinterpret_cast<uintx2 *>(static_cast<uint8_t *>(a.codes) + row * a.width + at) = code;
