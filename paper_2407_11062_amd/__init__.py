@@ -507,6 +507,14 @@ class KvBatch:
         self.desc = KvBatchDesc(_p(table), _p(lens), _p(starts), self.tokens, B, _i32("pages of a sequence", table.shape[1]), _i32("max_new", max_new), _i32("max_len", max_len))
         self.ref = ctypes.byref(self.desc)
 
+    @functools.cached_property
+    def device(self):
+        """The device that all three are on."""
+        table, lens, starts = (t.get_device() for t in self.keep)
+        if not table == lens == starts:
+            raise ValueError(f"table, lens and starts on devices {table}, {lens} and {starts}")
+        return table
+
 
 @functools.lru_cache(maxsize=1024)
 def _kv_strides(shape, stride, tokens, heads, head_dim):
@@ -615,6 +623,13 @@ def _like_w(W, n, device):
     return W.data_ptr(), code
 
 
+def _ws_like(ws, device):
+    """The pointer of a call's workspace: on the device of the call's tensors."""
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous tensor on device {device}, got one on {ws.device}")
+    return ws.data_ptr()
+
+
 def _codes_ptr(codes, shape, device):
     if codes.dtype is not torch.uint8 and codes.dtype is not torch.float8_e4m3fn:
         raise ValueError(f"codes: expected float8_e4m3fn or uint8, got {codes.dtype}")
@@ -697,7 +712,7 @@ def eqat_norm_bwd(S, W, eps, dY, dS=None, want=("dX", "dW"), out=None, ws=None):
         if ws is None: ws = norm_workspace(T, n, dtype, S.device)
     w, w_type = _like_w(W, n, device)
     status = lib().eqat_norm_bwd(_norm_ref(T, n, -1, act, w_type, eps), _like("S", S, shape, dtype, device), w, _like("dY", dY, shape, dtype, device), _like("dS", dS, shape, dtype, device), dX, dW,
-                                 _p(ws), 0 if ws is None else ws.numel(), _stream_at(device))
+                                 None if ws is None else _ws_like(ws, device), 0 if ws is None else ws.numel(), _stream_at(device))
     if status:
         _check("eqat_norm_bwd", status)
     return out
@@ -788,6 +803,8 @@ def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q
     device, dtype, tokens, head_dim = cache.pool.get_device(), cache.dtype, batch.tokens, cache.head_dim
     if rot.device != device:
         raise ValueError(f"frequencies on device {rot.device}, tensors on {device}")
+    if batch.device != device:
+        raise ValueError(f"table, lens and starts on device {batch.device}, tensors on {device}")
     if rot.head_dim != head_dim:
         raise ValueError(f"heads of {rot.head_dim} in a cache of heads of {head_dim}")
     if q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -879,7 +896,7 @@ def _gated(name, X, F, bits, group, layer, kind, dH, want, out, ws, prepared):
             if dY is None: dY = out["dY"] = torch.empty((T, 2 * F), dtype=dtype, device=X.device)
         back = (_like("dH", dH, (T, F), dtype, device), _like("dY", dY, (T, 2 * F), dtype, device))
     if ws is None: ws = gated_workspace(T, I, F, bits, group, dtype, prepared, X.device)
-    status = getattr(lib(), name)(_desc_ref(T, I, 2 * F, bits, group, act, BF16), kind, X.data_ptr(), *layer, *back, h, _p(ws), ws.numel(), _stream_at(device))
+    status = getattr(lib(), name)(_desc_ref(T, I, 2 * F, bits, group, act, BF16), kind, X.data_ptr(), *layer, *back, h, _ws_like(ws, device), ws.numel(), _stream_at(device))
     if status:
         _check(name, status)
     return out
