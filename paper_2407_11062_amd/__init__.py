@@ -682,7 +682,7 @@ def eqat_norm_fwd(X, W, eps, R=None, group=0, want=None, out=None):
     else:
         group = -1
     w, w_type = _like_w(W, n, device)
-    status = lib().eqat_norm_fwd(_norm_ref(T, n, group, act, w_type, eps), X.data_ptr(), r, w, s, y, codes, scales, _stream_at(device))
+    status = lib().eqat_norm_fwd(_norm_ref(T, n, group, act, w_type, float(eps)), X.data_ptr(), r, w, s, y, codes, scales, _stream_at(device))
     if status:
         _check("eqat_norm_fwd", status)
     return out
@@ -711,7 +711,7 @@ def eqat_norm_bwd(S, W, eps, dY, dS=None, want=("dX", "dW"), out=None, ws=None):
         dW = _like("dW", dW, (n,), torch.float32, device)
         if ws is None: ws = norm_workspace(T, n, dtype, S.device)
     w, w_type = _like_w(W, n, device)
-    status = lib().eqat_norm_bwd(_norm_ref(T, n, -1, act, w_type, eps), _like("S", S, shape, dtype, device), w, _like("dY", dY, shape, dtype, device), _like("dS", dS, shape, dtype, device), dX, dW,
+    status = lib().eqat_norm_bwd(_norm_ref(T, n, -1, act, w_type, float(eps)), _like("S", S, shape, dtype, device), w, _like("dY", dY, shape, dtype, device), _like("dS", dS, shape, dtype, device), dX, dW,
                                  None if ws is None else _ws_like(ws, device), 0 if ws is None else ws.numel(), _stream_at(device))
     if status:
         _check("eqat_norm_bwd", status)

@@ -1,4 +1,4 @@
-"""The norm where the formula has nothing but its own terms to hold it: eps = 0, in workgroups that its rows do not fill."""
+"""The norm at its edges: eps = 0 in workgroups that its rows do not fill, 8-bit codes at the ties of the quotient and beside infinities, eps as a tensor."""
 import pytest
 import torch
 
@@ -45,3 +45,13 @@ def test_codes_beside_an_infinity():
     assert (out["Y"][:, 5] == float("inf")).all() and (out["scales"][:, 0] == float("inf")).all()
     codes = out["codes"].float()
     assert codes[:, 5].isnan().all() and not codes[:, :5].any() and not codes[:, 6:32].any() and (codes[:, 32:] == 448.0).all()
+
+
+def test_eps_that_is_a_tensor():
+    """goes by its value, at every call"""
+    S, dY = rows(1, 3, 64, torch.float32), rows(2, 3, 64, torch.float32)
+    eps = torch.tensor(1e-5)
+    for value in (1e-5, 100.0):
+        eps.fill_(value)
+        assert torch.equal(eq.eqat_norm_fwd(S, None, eps)["Y"], eq.eqat_norm_fwd(S, None, float(eps))["Y"])
+        assert torch.equal(eq.eqat_norm_bwd(S, None, eps, dY)["dX"], eq.eqat_norm_bwd(S, None, float(eps), dY)["dX"])
