@@ -6,7 +6,8 @@ namespace eqat {
 
 // silu(x) = x / (1 + exp(-x)), and x (1 + tanh(k (x + 0.044715 x^3))) / 2 = x / (1 + exp(-2 k (x + 0.044715 x^3))) with k = sqrt(2 / pi): both x p, p = 1 / (1 + exp(-t)),
 // t = x or t = 2 k (x + 0.044715 x^3), and the derivative is p + x p (1 - p) t'.  Where exp(-t) passes binary32, p is 0, and x p = 0 for every finite x.
-// exp(-t) = 2^(-t log2 e): the product's error, |t| 2^-24 of it, is put right by what a multiply-add leaves of it, so p is good to some 2^-23 for every t.
+// exp(-t) = 2^(-t log2 e): the product's error, |t| 2^-24 of it, is put right by what a multiply-add leaves of it, so p is good to eight roundings (2^-21: the power's and the reciprocal's approximations,
+// the products and sums between them) for every t that leaves it a normal number.  Where 1 + exp(-t) is 2^126 or more, t below -87.3, it may be 0: x p is off by |x| 2^-126 there (silu(-88) 0 for -5e-37).
 struct GateP { float p, q; };                                         // q = 1 - p, as good as p
 __device__ __forceinline__ GateP gate_p(float t)
 {
