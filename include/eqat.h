@@ -545,7 +545,7 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *   may be Y itself, H may be dH itself; no other overlap.
  *
  * eqat_gated_fwd / _bwd: both projections from the packed layer, the activation and the product in one kernel (G and U are not rounded and not stored):
- *   d          the stacked layer: out_features = 2 F, F a multiple of 8; tokens, in_features, bits, group, act_dtype as for eqat_qlinear_fwd (w_dtype is ignored).
+ *   d          the stacked layer: out_features = 2 F, F a multiple of 8; tokens, in_features, bits, group, act_dtype as for eqat_qlinear_fwd (w_dtype is ignored; out_features x in_features below 2^30).
  *   forward    X -> H [tokens, F].
  *   backward   X, dH -> dY = [dH U act'(G) | dH act(G)] [tokens, 2 F], and H again (either may be NULL): both projections are made anew, so that a training step keeps X
  *              alone between its passes (H bitwise that of the forward where both take the same kernel: more than 64 tokens, or fp32); dY is what eqat_qlinear_bwd of the layer takes (dX, ds), H the input of the next linear in its own backward pass.
@@ -553,7 +553,8 @@ eqat_status eqat_kv_rotary_write(const eqat_kv_desc *d, const eqat_kv_batch *b, 
  *   No tensor may overlap another.
  *   ws         eqat_gated_workspace_bytes(d) bytes, 256-byte aligned, contents undefined before and after.  That of more tokens serves fewer, too.
  *              Calls that share one must not overlap in time.
- * With fp32 activations all of it is binary32.
+ * With fp32 activations all of it is binary32.  With bf16 activations the weights that the layer stands for, q s - z s, are rounded to bf16 before the products, as in every other call with bf16
+ * activations; sums, activation and gradient are binary32, and each result is rounded once.
  * EQAT_ERR_HYPER for an unknown kind.
  */
 typedef enum { EQAT_GATE_SILU = 0, EQAT_GATE_GELU = 1 } eqat_gate_kind;

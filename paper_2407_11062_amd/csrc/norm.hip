@@ -7,7 +7,7 @@
 // meets in LDS once (a row's maximum, for 8 bits with one scale a row, a second time).  Sums, means and products are binary32; S is what stands in memory, so that the
 // backward pass, which makes rstd from S again, is that of what the forward computed.
 //
-// us over three states that take turns: 8192 rows of 8192 with a residual 93 (537 MB, 5.7 TB/s), their like of 4096 backward 49 (268 MB, 5.5); one row of 4096 2.7 in a graph, 515 rows of 5120 to 8 bits 6.3,
+// us over three states that take turns: 8192 rows of 8192 with a residual 93 (537 MB, 5.7 TB/s), their like of 4096 backward 49 (268 MB, 5.5); one row of 4096 2.7 in a graph, 515 rows of 5120 to 8 bits 6.6,
 // 333 rows of 4096 backward, fp32, 8.2 and 2.4 for the second launch.
 #include "layer.h"
 
@@ -320,11 +320,12 @@ __global__ __launch_bounds__(256) void k_norm_dw(const float *__restrict__ part,
 constexpr int64_t kOnceBytes = (int64_t)96 << 20;
 
 // Workgroups of a backward pass at most: two a compute unit.  One each where few of them would have two rows and the others one, and where waves of a row fill a compute unit; the second launch has
-// half the parts then.  us, 512 / 256: 512 rows of 4096, fp32, 13.8 / 12.0; 600 of 16384 35 / 27; 1500 of 20000 93 / 80; 1024 of 8192 21.0 / 21.5; 2048 of 8192 32.6 / 36.
+// half the parts then.  us, three states in turn, 512 / 256, bf16: 300 rows of 4096 9.0 / 8.5, 512 12.0 / 10.0, 768 12.8 / 11.1, 600 of 16384 25.6 / 21.1, 1500 of 20000 76 / 64, 1024 of 8192 18.3 / 18.3,
+// 2048 of 8192 28.6 / 31.1; fp32: 512 of 4096 13.6 / 11.4, 768 13.6 / 13.0, 600 of 16384 42 / 37, 1500 of 20000 112 / 104, 1024 of 8192 29.0 / 27.2, 2048 of 8192 47.5 / 48.5 (300 of 4096 10.7 / 10.9).
 constexpr int kNormParts = 512;
 
 // Lanes and vectors a lane of a row.  Few vectors a lane where the chip has waves to spare: a row is a chain of a fetch, a sum, the results, and the shorter its links the better; with more rows than
-// compute units whole workgroups hide each other's.  Forward, us, 256 lanes / 512 / 1024: one row of 4096 3.3 / 2.9, 515 rows 5.5 / 5.3, one of 8192 4.5 / 3.5 / 3.1, 256 rows 6.4 / 5.2 / 4.9, 515 rows
+// compute units whole workgroups hide each other's.  bf16.  Forward with a residual, us, 256 lanes / 512 / 1024: one row of 4096 3.3 / 2.9, 515 rows 5.5 / 5.3, one of 8192 4.5 / 3.5 / 3.1, 256 rows 6.4 / 5.2 / 4.9, 515 rows
 // 9.5 / 8.9 / 9.6, 4096 rows 50.9 / 46.3 / 45.5.  Backward: 1024 rows of 4096 14.1 / 13.2; 64 of 8192 8.6 / 7.9 / 7.9, 333 14.8 / 15.1 / 14.7, 4096 52 / 60 / 68.
 template <bool BACK, typename F> void by_width(int64_t rows, int width, F f)
 {
