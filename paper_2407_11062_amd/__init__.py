@@ -757,14 +757,14 @@ _NOTHING = (None, None, 0, None, None)
 
 
 def _turned(t, out, tokens, dtype, head_dim, device):
-    """(pointer, strides, heads, pointer, strides) of what is turned and of where it goes"""
+    """(pointer, strides, heads, pointer, strides) of what is turned and of where it goes, and what the strides' addresses live in, which has to be held until the call returns"""
     shape = t.shape
     if t.dtype is not dtype or out.dtype is not dtype or t.get_device() != device or out.get_device() != device:
         raise ValueError(f"expected {dtype} tensors on device {device}, got {t.dtype} on {t.device} and {out.dtype} on {out.device}")
     if out.shape != shape:
         raise ValueError(f"expected {list(shape)}, got {list(out.shape)}")
-    heads, here, there, _, _ = _both_rows(shape, t.stride(), out.stride(), tokens, head_dim)
-    return t.data_ptr(), here, heads, out.data_ptr(), there
+    rows = _both_rows(shape, t.stride(), out.stride(), tokens, head_dim)
+    return (t.data_ptr(), rows[1], rows[0], out.data_ptr(), rows[2]), rows
 
 
 def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, inverse=False):
@@ -788,10 +788,10 @@ def eqat_rotary(rot: Rotary, positions, q=None, k=None, q_out=None, k_out=None, 
     of_q = of_k = _NOTHING
     if q is not None:
         if q_out is None: q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        of_q = _turned(q, q_out, T, dtype, head_dim, device)
+        of_q, q_rows = _turned(q, q_out, T, dtype, head_dim, device)
     if k is not None:
         if k_out is None: k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        of_k = _turned(k, k_out, T, dtype, head_dim, device)
+        of_k, k_rows = _turned(k, k_out, T, dtype, head_dim, device)
     status = lib().eqat_rotary(ref, T, positions.data_ptr(), *of_q, *of_k, 1 if inverse else 0, _stream_at(device))
     if status:
         _check("eqat_rotary", status)
@@ -811,7 +811,8 @@ def eqat_kv_rotary_write(cache: KvCache, batch: KvBatch, rot: Rotary, q, k, v, q
     if k.dtype is not dtype or v.dtype is not dtype or k.get_device() != device or v.get_device() != device:
         raise ValueError(f"expected {dtype} tensors on device {device}, got {k.dtype} on {k.device} and {v.dtype} on {v.device}")
     ks, vs = _kv_strides(k.shape, k.stride(), tokens, cache.heads, head_dim), _kv_strides(v.shape, v.stride(), tokens, cache.heads, head_dim)
-    status = lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[dtype], *_turned(q, q_out, tokens, dtype, head_dim, device), k.data_ptr(), ks[0], v.data_ptr(), vs[0], cache.pool.data_ptr(),
+    of_q, q_rows = _turned(q, q_out, tokens, dtype, head_dim, device)
+    status = lib().eqat_kv_rotary_write(cache.ref, batch.ref, rot.refs[dtype], *of_q, k.data_ptr(), ks[0], v.data_ptr(), vs[0], cache.pool.data_ptr(),
                                         _stream_at(device))
     if status:
         _check("eqat_kv_rotary_write", status)

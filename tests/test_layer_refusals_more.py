@@ -1,4 +1,6 @@
-"""Refusals of the binding that no tensor of one device reaches: workspaces and batches on another device than a call's tensors.  No GPU: nothing is launched."""
+"""Refusals of the binding that no tensor of one device reaches (workspaces and batches on another device than a call's tensors), and what it hands over by address.  No GPU: nothing is launched."""
+import ctypes
+
 import pytest
 import torch
 
@@ -48,3 +50,30 @@ def test_batches_on_another_device():
             eq.eqat_kv_rotary_write(cache, batch(*devices), rot, q, q, q)
     with pytest.raises(ValueError, match="table, lens and starts on device 1"):
         eq.eqat_kv_rotary_write(cache, batch(1, 1, 1), rot, q, q, q)
+
+
+def test_strides_live_until_the_call_returns(monkeypatch):
+    """what a call hands over by address does not go with the entries of a cache that other threads' calls push out"""
+    seen = []
+
+    class Calls:
+        def look(self, *addresses):
+            eq._both_rows.cache_clear()
+            eq._kv_strides.cache_clear()
+            others = [(ctypes.c_int64 * 2)(7, 7) for _ in range(1000)]
+            seen.append([list((ctypes.c_int64 * 2).from_address(a)) for a in addresses])
+            return 0 * len(others)
+
+        def eqat_rotary(self, ref, tokens, pos, q, qs, qh, qo, qos, k, ks, kh, ko, kos, inverse, stream): return self.look(qs, qos, ks, kos)
+        def eqat_kv_rotary_write(self, c, b, r, q, qs, qh, qo, qos, k, ks, v, vs, pool, stream): return self.look(qs, qos, ks, vs)
+
+    cache = eq.KvCache(1, 64, 64, 32, 1, dtype=torch.float32, device="cpu")
+    rot, batch = eq.Rotary.__new__(eq.Rotary), eq.KvBatch.__new__(eq.KvBatch)
+    rot.device, rot.head_dim, rot.refs = -1, 64, {torch.float32: 0}
+    batch.device, batch.tokens, batch.ref = -1, 4, None
+    monkeypatch.setattr(eq, "lib", Calls)
+    monkeypatch.setattr(eq, "_stream_at", lambda device: 0)
+    q, k, out = torch.zeros(4, 5, 64), torch.zeros(4, 1, 96)[..., :64], torch.zeros(4, 5, 72)[..., :64]
+    eq.eqat_rotary(rot, torch.zeros(4, dtype=torch.int32), q, k, q_out=out, k_out=torch.zeros(4, 1, 128)[..., :64])
+    eq.eqat_kv_rotary_write(cache, batch, rot, q, k, k, q_out=out)
+    assert seen == [[[320, 64], [360, 72], [96, 96], [128, 128]], [[320, 64], [360, 72], [96, 96], [96, 96]]]
