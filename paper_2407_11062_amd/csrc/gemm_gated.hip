@@ -4,7 +4,7 @@
 // the registers that they were summed in, binary32.  Against the plain forward and a gate behind it this leaves out 3 T F elements of traffic and a launch, and two roundings.
 // A packed layer's codes are read as packed: the same main loop with another segment load and some more arithmetic, against a re-layout in front of it, us, re-laid / as packed: 333 tokens, 3 bit,
 // 5120 -> 2 x 13824 123 / 111; 2048 tokens, 4 bit, 8192 -> 2 x 28672 1641 / 1572, 2 bit, 4096 -> 2 x 11008 315 / 311; only 3-bit codes lose from some 3000 tokens on (4096 tokens 945 / 958).
-// Whole tiles only: no tile is cut along the contraction, and no scratch is needed.  Bound by the matrix cores: 2048 tokens, 8192 -> 2 x 28672, 4 bit, 1530 to 1610 us (1258 to 1193 TFLOP/s; a plain product
+// Whole tiles only: no tile is cut along the contraction, and no scratch is needed.  Bound by the matrix cores: 2048 tokens, 8192 -> 2 x 28672, 4 bit, 1530 to 1620 us (1258 to 1186 TFLOP/s; a plain product
 // reaches 1303), 333 tokens, 5120 -> 2 x 13824 106 (216 tiles on 256 compute units), backward of 4096 tokens, 4096 -> 2 x 11008 654 (5.4 rounds of tiles).
 // The weights are what all bf16 kernels here multiply with: q s - z s by one multiply-add, rounded to bf16, so that a matrix instruction takes 16 inputs; exact codes would need sums a group of their own.
 #include "common.h"
